@@ -273,6 +273,87 @@ int ouro_lm_head_static(const void *x_dev, const void *lm_head_dev, int32_t rows
  * 0xff between calls; the status word follows, zero unless the last call gave up). */
 int ouro_debug_static_scratch(void **dev_ptr, size_t *slot_bytes);
 
+/* ---- Several continuations of a text: a paged cache, attention over it, token scores -----------------------------------
+ *
+ * (The paper decodes one continuation of one query; these calls are for callers that hold several: beams, n-best lists, several
+ * queries or drafts at once.)  They need no context.  Every call checks what the host can see (OURO_EINVAL with a text in
+ * ouro_last_error(NULL)), enqueues on cuda_stream (a cudaStream_t, NULL = default stream of the current device) and returns;
+ * nothing is allocated.  The first call of each kind on a device sizes its kernel's shared memory: make it outside a stream capture.
+ *
+ * A paged cache holds keys and values of up to max_seqs sequences in pages of page_size tokens.  Key (layer l, page p, row r,
+ * head h) begins at k + l*layer_stride + p*page_stride + r*slot_stride + h*head_stride (elements), its head_dim values side by
+ * side; values likewise.  Sequence s has lens[s] tokens; entries 0 .. ceil(lens[s] / page_size) - 1 of its row of the table name
+ * their pages, the others are -1.  refs[p] counts the entries that name page p: continuations share the pages of what they have in
+ * common, and a page is free when nobody names it.  Pages are given out lowest id first, so a cache's state is a function of the
+ * calls made on it. */
+enum {
+  OURO_MAX_LIST = 1024,   /* sequences in one call */
+  OURO_MAX_SEQS = 65536,  /* rows of a table */
+  OURO_MAX_NEW = 16,      /* newest tokens of a sequence that one call attends for */
+  OURO_MAX_TOP = 32       /* alternatives per row */
+};
+typedef struct {
+  int32_t n_layers, n_pages, page_size, n_kv_heads, head_dim;   /* head_dim: a multiple of 32, <= 128 */
+  int32_t dtype;                                                 /* OURO_F32 or OURO_BF16 */
+  int32_t max_seqs, max_pages;                                   /* the table's rows and entries of a row */
+  int64_t layer_stride, page_stride, slot_stride, head_stride;   /* elements; multiples of 16 bytes */
+  void *k, *v;                                                   /* 16-byte aligned */
+  int32_t *table, *lens, *refs;                                  /* [max_seqs, max_pages], [max_seqs], [n_pages] */
+  int32_t *status;                                               /* [1]: first refusal of a call that found its lists wrong on the device */
+  void *workspace;                                               /* 256-byte aligned, ouro_paged_workspace_bytes() of it */
+  size_t workspace_bytes;
+} ouro_paged_cache;                                              /* all pointers are device memory */
+
+/* Bytes of workspace (0: the description is invalid).  Calls that share a workspace must not overlap on the GPU. */
+size_t ouro_paged_workspace_bytes(const ouro_paged_cache *cache);
+/* No sequences, all pages free, status and workspace cleared.  To be called once before any other call on the cache and its workspace. */
+int ouro_paged_reset(const ouro_paged_cache *cache, void *cuda_stream);
+/* Synchronises and returns the cache's status, which it clears: OURO_OK, or the first refusal since: OURO_EINVAL (a sequence
+ * outside the table, the same one twice, a negative count), OURO_ECAPACITY (no room in a row of the table, too few free pages).  A call
+ * that refuses changes nothing. */
+int ouro_paged_status(const ouro_paged_cache *cache, void *cuda_stream);
+
+/* Lists are device memory, n <= OURO_MAX_LIST.
+ * fork: all at once, sequence dst[i] becomes what src[i] was: it names the same pages; pages nobody names any more are free.  A
+ *   src may be listed often and be another's dst (a beam search's parents), a dst only once.
+ * truncate: sequence seqs[i] keeps its first keep[i] tokens (all, if it has fewer; 0 frees it).
+ * extend: in the order of the list, sequence seqs[i] gets room for new_tokens[i] more (at most width).  If its last page is not full and
+ *   shared when its turn comes, it gets one of its own first, with the rows so far copied in every layer; so the last to ask keeps the
+ *   old one.  slots_dev and positions_dev [n, width] (either may be NULL) receive page * page_size + row and position of each new
+ *   token, -1 beyond new_tokens[i] and after a refusal.
+ * compact: the pages in use come to lie in ids 0 .. live-1: the i-th page in use beyond moves, in all layers, to the i-th free
+ *   id below.  live_dev [1] (may be NULL) receives their number. */
+int ouro_paged_fork(const ouro_paged_cache *cache, const int32_t *src_dev, const int32_t *dst_dev, int32_t n, void *cuda_stream);
+int ouro_paged_truncate(const ouro_paged_cache *cache, const int32_t *seqs_dev, const int32_t *keep_dev, int32_t n, void *cuda_stream);
+int ouro_paged_extend(const ouro_paged_cache *cache, const int32_t *seqs_dev, const int32_t *new_tokens_dev, int32_t n, int32_t width,
+                      int32_t *slots_dev, int32_t *positions_dev, void *cuda_stream);
+int ouro_paged_compact(const ouro_paged_cache *cache, int32_t *live_dev, void *cuda_stream);
+
+/* Rotary positions on half-split pairs for new queries and keys, and the keys and values into the cache.  q [rows, n_heads, head_dim],
+ * k, v [rows, n_kv_heads, head_dim] of the cache's type; consecutive rows lie q_stride / kv_stride elements apart, heads side by side (so
+ * that all three may be parts of one projection).  cos_dev, sin_dev [n_positions, head_dim/2] f32.  The rotated queries go to q_out_dev
+ * [rows, n_heads, head_dim] (may be q itself where q_stride is n_heads * head_dim).  A row whose slot lies outside the cache (-1: padding)
+ * leaves the cache alone; a row whose position lies outside the tables also gives zeros for its queries.  No two rows may have the same slot. */
+int ouro_paged_append(const ouro_paged_cache *cache, int32_t layer, const void *q_dev, int64_t q_stride, const void *k_dev, const void *v_dev,
+                      int64_t kv_stride, int32_t rows, int32_t n_heads, const int32_t *slots_dev, const int32_t *positions_dev,
+                      const float *cos_dev, const float *sin_dev, int32_t n_positions, void *q_out_dev, void *cuda_stream);
+/* Attention of the n_new newest tokens (1 in plain decoding, at most OURO_MAX_NEW) of n sequences, whose keys and values are in the cache
+ * already: token i of sequence s sees the keys 0 .. lens[s] - n_new + i.  seqs_dev [n]: rows of the table (NULL: 0 .. n-1); q [n, n_new,
+ * n_heads, head_dim], tokens q_stride elements apart; out [n, n_new, n_heads, head_dim] of the cache's type; lse_dev [n, n_new, n_heads]
+ * (may be NULL) receives the natural logarithm of the sum of exponentials.  A token that sees no key gives zeros (lse -inf); entries of
+ * the table outside 0 .. n_pages-1 are left out, and so are sequences outside the table.  Sums and maxima are held in 32 bits, probabilities
+ * as two bf16 parts. */
+int ouro_paged_attention(const ouro_paged_cache *cache, int32_t layer, const int32_t *seqs_dev, int32_t n, int32_t n_new, const void *q_dev,
+                         int64_t q_stride, int32_t n_heads, float scale, void *out_dev, float *lse_dev, void *cuda_stream);
+
+/* What a row of logits says about a token: logits [rows, vocab] (OURO_F32 or OURO_BF16), rows row_stride elements apart.
+ *   logprob_dev [rows]: log probability of tokens_dev[row] (-inf where it lies outside the vocabulary); entropy_dev [rows] in nats;
+ *   top_ids_dev, top_logprobs_dev [rows, n_top]: the n_top <= OURO_MAX_TOP best, best first, ties by the lowest id.
+ * Outputs may be NULL (tokens_dev with logprob_dev; the two top arrays together, with n_top 0).  -inf is a token that cannot come; a row of
+ * nothing else gives -inf and entropy 0.  NaN or +inf in a row leaves no distribution: its log probabilities and entropy are NaN, NaN ranks first. */
+int ouro_token_logprobs(const void *logits_dev, int32_t dtype, int64_t row_stride, int32_t rows, int32_t vocab, const int32_t *tokens_dev,
+                        int32_t n_top, float *logprob_dev, float *entropy_dev, int32_t *top_ids_dev, float *top_logprobs_dev, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

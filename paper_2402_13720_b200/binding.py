@@ -22,6 +22,7 @@ _lib = None
 OURO_OK, OURO_EINVAL, OURO_ENOMEM, OURO_ECAPACITY, OURO_ECUDA, OURO_ETIMEOUT, OURO_ESTATE = range(7)
 OURO_F32, OURO_BF16 = 0, 1
 OURO_TARGET, OURO_DRAFT = 0, 1
+OURO_MAX_LIST, OURO_MAX_SEQS, OURO_MAX_NEW, OURO_MAX_TOP = 1024, 65536, 16, 32
 OURO_MAX_ROWS, OURO_MAX_BETA, OURO_MAX_K, OURO_MAX_GAMMA = 128, 16, 16, 32
 OURO_HARVEST_MATCHED, OURO_HARVEST_CANDIDATES, OURO_HARVEST_ACCEPTED, OURO_SEED_PROMPT, OURO_DRAFT_PHRASES = 1, 2, 4, 8, 16
 
@@ -50,8 +51,15 @@ class StatsC(C.Structure):
         return {n: getattr(self, n) for n, _ in self._fields_}
 
 
+class PagedCacheC(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_layers", "n_pages", "page_size", "n_kv_heads", "head_dim", "dtype", "max_seqs", "max_pages")] + \
+               [(n, C.c_int64) for n in ("layer_stride", "page_stride", "slot_stride", "head_stride")] + \
+               [(n, C.c_void_p) for n in ("k", "v", "table", "lens", "refs", "status", "workspace")] + [("workspace_bytes", C.c_size_t)]
+
+
 DRAFTER_FN = C.CFUNCTYPE(C.c_int, C.c_void_p, C.POINTER(C.c_int32), C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_int32))
 
+_PAGED = C.POINTER(PagedCacheC)
 _I32P, _U64P, _F32P = C.POINTER(C.c_int32), C.POINTER(C.c_uint64), C.POINTER(C.c_float)
 _SIGNATURES = {
     "ouro_strerror": (C.c_char_p, [C.c_int]),
@@ -84,6 +92,19 @@ _SIGNATURES = {
     "ouro_debug_set_wait_limit": (C.c_int, [C.c_void_p, C.c_int64]),
     "ouro_debug_counts": (C.c_int, [C.c_void_p, C.POINTER(C.c_uint32), C.c_int32]),
     "ouro_profile_read": (C.c_int, [C.c_void_p, _F32P, _I32P]),
+    "ouro_paged_workspace_bytes": (C.c_size_t, [_PAGED]),
+    "ouro_paged_reset": (C.c_int, [_PAGED, C.c_void_p]),
+    "ouro_paged_status": (C.c_int, [_PAGED, C.c_void_p]),
+    "ouro_paged_fork": (C.c_int, [_PAGED, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]),
+    "ouro_paged_truncate": (C.c_int, [_PAGED, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]),
+    "ouro_paged_extend": (C.c_int, [_PAGED, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "ouro_paged_compact": (C.c_int, [_PAGED, C.c_void_p, C.c_void_p]),
+    "ouro_paged_append": (C.c_int, [_PAGED, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_void_p,
+                                    C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]),
+    "ouro_paged_attention": (C.c_int, [_PAGED, C.c_int32, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_int32, C.c_float,
+                                       C.c_void_p, C.c_void_p, C.c_void_p]),
+    "ouro_token_logprobs": (C.c_int, [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p,
+                                      C.c_void_p, C.c_void_p, C.c_void_p]),
     "ouro_generate": (C.c_int, [C.c_void_p, _I32P, C.c_int32, C.c_int32, C.c_int32, _I32P, _I32P, C.POINTER(StatsC)]),
     "ouro_generate_vanilla": (C.c_int, [C.c_void_p, _I32P, C.c_int32, C.c_int32, _I32P, _I32P, C.POINTER(StatsC)]),
 }
