@@ -310,7 +310,7 @@ size_t ouro_paged_workspace_bytes(const ouro_paged_cache *cache);
 int ouro_paged_reset(const ouro_paged_cache *cache, void *cuda_stream);
 /* Synchronises and returns the cache's status, which it clears: OURO_OK, or the first refusal since: OURO_EINVAL (a sequence
  * outside the table, the same one twice, a negative count), OURO_ECAPACITY (no room in a row of the table, too few free pages).  A call
- * that refuses changes nothing. */
+ * that refuses changes nothing.  OURO_ETIMEOUT: a bounded device-side wait of an attention gave up, its output is wrong. */
 int ouro_paged_status(const ouro_paged_cache *cache, void *cuda_stream);
 
 /* Lists are device memory, n <= OURO_MAX_LIST.

@@ -568,6 +568,7 @@ extern "C" int ouro_paged_status(const ouro_paged_cache *c, void *stream) {
   if (e != cudaSuccess) return paged::refuse(call, cudaGetErrorString(e), OURO_ECUDA);
   if (status == OURO_EINVAL) return paged::refuse(call, "a list named a sequence outside the table or twice, or a negative or too large count");
   if (status == OURO_ECAPACITY) return paged::refuse(call, "no room in a row of the table, or too few free pages", OURO_ECAPACITY);
+  if (status == OURO_ETIMEOUT) return paged::refuse(call, "a bounded device-side wait of an attention gave up", OURO_ETIMEOUT);
   return status;
 }
 
