@@ -338,7 +338,7 @@ int ouro_paged_append(const ouro_paged_cache *cache, int32_t layer, const void *
                       int64_t kv_stride, int32_t rows, int32_t n_heads, const int32_t *slots_dev, const int32_t *positions_dev,
                       const float *cos_dev, const float *sin_dev, int32_t n_positions, void *q_out_dev, void *cuda_stream);
 /* Attention of the n_new newest tokens (1 in plain decoding, at most OURO_MAX_NEW) of n sequences, whose keys and values are in the cache
- * already: token i of sequence s sees the keys 0 .. lens[s] - n_new + i.  seqs_dev [n]: rows of the table (NULL: 0 .. n-1); q [n, n_new,
+ * already: token i of sequence s sees the keys 0 .. lens[s] - n_new + i; scores are scale * q.k, scale > 0.  seqs_dev [n]: rows of the table (NULL: 0 .. n-1); q [n, n_new,
  * n_heads, head_dim], tokens q_stride elements apart; out [n, n_new, n_heads, head_dim] of the cache's type; lse_dev [n, n_new, n_heads]
  * (may be NULL) receives the natural logarithm of the sum of exponentials.  A token that sees no key gives zeros (lse -inf); entries of
  * the table outside 0 .. n_pages-1 are left out, and so are sequences outside the table.  Sums and maxima are held in 32 bits, probabilities

@@ -9,7 +9,7 @@ void ouro_set_global_error(const std::string &msg);
 
 namespace paged {
 
-constexpr int MAX_CTAS = 592;        // of the attention kernel: four per SM at most
+constexpr int MAX_CTAS = 444;        // of the attention kernel: three per SM at most
 constexpr int ROW_TILE = 16;         // query rows a CTA works on at a time at most
 constexpr int TEXT_DIM = 128;        // largest head dim
 

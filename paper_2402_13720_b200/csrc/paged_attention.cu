@@ -9,8 +9,8 @@
 //    cost whatever the lengths are (see Place).  An item that lies in one CTA is finished there; of an item cut between CTAs each leaves
 //    a piece (maximum, sum, unnormalised output, in 32 bits), and the CTA that is last to do so joins the pieces in ascending order
 //    (so the result does not depend on who that is).
-//  - A warp has KW keys of every unit and its own ring of shared memory, which it fills STAGES - 1 units ahead, across the borders of items;
-//    the ids of pages are read one unit before that.  Warps meet only at an item's end.
+//  - A warp fetches KW keys of every unit into its part of a ring in shared memory, STAGES - 1 units ahead, across the borders of items;
+//    the ids of pages are read before that, 32 units' at a time.  A warp works on the keys that it fetched; warps meet only at an item's end.
 //  - bf16: S = Q K^T and O += P V as mma.sync m16n8k16 with Q, P and O in registers (the tensor cores idle most of the time
 //    anyway).  P goes in as two bf16 parts, P = hi + lo up to 2^-17: one part alone would add an error as large as the output's own
 //    rounding.  Up to 8 query rows the parts are the two halves of one 16-row operand, beyond that two contractions.
@@ -32,6 +32,20 @@ constexpr int MIN_RUN = 4;                          // units for which another C
 constexpr float GROWTH = 8.f;                       // (log2) a maximum may grow by this before sums are rescaled: they stay below 2^8 per key
 constexpr uint32_t SPIN_LIMIT = 1u << 22;
 
+// Division of 0 .. 2^31 - 1 by a number that a call does not change: three instructions instead of some thirty, and it is done for every unit.
+struct Div {
+  uint32_t d, mul, shift;
+  void set(uint32_t x) {
+    d = x;
+    uint32_t bits = 0;
+    while (bits < 31 && (1u << bits) < x) ++bits;
+    // ceil(2^(31 + bits) / x) < 2^32, and its excess over the quotient is below 2^-31 of it
+    mul = x == 1 ? 0 : (uint32_t)((((uint64_t)1 << (31 + bits)) + x - 1) / x);
+    shift = bits ? bits - 1 : 0;
+  }
+  __device__ __forceinline__ int quot(int n) const { return mul ? (int)(__umulhi((uint32_t)n, mul) >> shift) : n; }
+};
+
 struct AttnParams {
   const uint8_t *k, *v;                             // of the layer
   const int32_t *table, *lens, *seqs;
@@ -42,7 +56,8 @@ struct AttnParams {
   float *pieces;                                    // [CTA][2][ROW_TILE][D], then [CTA][2][ROW_TILE][2]
   int64_t page_bytes, slot_bytes, head_bytes, q_stride;
   int n, n_new, H, Hkv, group, rows, row_tiles;     // rows = n_new * group
-  int n_pages, page, max_pages, max_seqs, cap, layer;
+  int n_pages, max_pages, max_seqs, cap, layer;
+  Div page, group_of;
   float scale_log2;
 };
 // The pools as five dimensions (dim, head, row, page, layer); boxes of 64 dims x 16 rows.
@@ -118,7 +133,7 @@ struct Cfg {
   static constexpr int OFF_RING = 0;                                      // [warp][stage]
   static constexpr int OFF_Q = WARPS * STAGES * STAGE;                    // f32: [warp][R][D]
   static constexpr int OFF_ML = OFF_Q + (BF ? 0 : WARPS * R * D * 4);     // [warp][R][2]
-  static constexpr int OFF_JOIN = OFF_ML + WARPS * R * 8;                 // [CHUNK][R][2]
+  static constexpr int OFF_JOIN = OFF_ML + WARPS * R * 8;                // [CHUNK][R][2]
   static constexpr int OFF_BAR = OFF_JOIN + CHUNK * R * 8;                // [warp][stage]
   static constexpr int OFF_MASK = OFF_BAR + WARPS * STAGES * 8;           // [warp][stage]
   static constexpr int OFF_LEN = OFF_MASK + WARPS * STAGES * 4;           // [n]
@@ -128,9 +143,9 @@ struct Cfg {
   static_assert(R * D * 4 <= STAGE && R <= paged::ROW_TILE, "a warp's output fits its stage");
 };
 
-// A place in the list of units: sequence, head and row tile, unit of the item; and what is known of the sequence.
+// A place in the list of units: sequence, head, row tile, unit of the item; and what is known of the sequence.
 struct Walk {
-  int s, hr, tile, tiles, len;
+  int s, head, rt, tile, tiles, len;
   const int32_t *row;
 };
 
@@ -196,14 +211,16 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
   auto next = [&](Walk &w) {
     if (++w.tile < w.tiles) return;
     w.tile = 0;
-    if (++w.hr < F) return;
-    w.hr = 0;
+    if (++w.rt < p.row_tiles) return;
+    w.rt = 0;
+    if (++w.head < p.Hkv) return;
+    w.head = 0;
     if (++w.s < p.n) enter(w);
   };
   // Where the c-th run begins: at equal cost; within SNAP units of an item's border at that border.
   auto place = [&](int64_t c) {
     const int64_t at = cost * c / G;
-    Walk w{p.n, 0, 0, 0, 0, nullptr};
+    Walk w{p.n, 0, 0, 0, 0, 0, nullptr};
     if (at >= cost) return w;
     int lo = 0, hi = p.n - 1;
     while (lo < hi) {
@@ -213,8 +230,9 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
     w.s = lo;
     enter(w);
     const int in = (int)(at - (int64_t)s_cum[lo] * F), each = w.tiles + ITEM_COST;   // fits: a sequence's cost is checked on the host
-    w.hr = in / each;
-    const int tile = in - w.hr * each - ITEM_COST;
+    const int hr = in / each, tile = in - hr * each - ITEM_COST;
+    w.head = hr / p.row_tiles;
+    w.rt = hr - w.head * p.row_tiles;
     w.tile = tile <= SNAP ? 0 : tile;
     if (w.tile > 0 && w.tiles - tile <= SNAP) {
       w.tile = w.tiles - 1;
@@ -224,45 +242,66 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
   };
   Walk c = place(blockIdx.x);                                      // the unit being worked on
   const Walk end = place(blockIdx.x + 1);
-  auto at_end = [&](const Walk &w) { return w.s == end.s && w.hr == end.hr && w.tile == end.tile; };
+  auto at_end = [&](const Walk &w) { return w.tile == end.tile && w.rt == end.rt && w.head == end.head && w.s == end.s; };
   if (at_end(c)) return;
 
   // ---- the warp's ring
   uint8_t *ring_p = smem + C::OFF_RING + warp * C::STAGES * C::STAGE;
   const uint32_t ring = smem_u32(ring_p);
-  volatile uint32_t *s_mask = (volatile uint32_t *)(smem + C::OFF_MASK) + warp * C::STAGES;
-  uint32_t phases = 0;                                             // of the stages' barriers
+  volatile uint32_t *s_mask = (volatile uint32_t *)(smem + C::OFF_MASK) + warp * C::STAGES;   // which keys are there
+  uint32_t phases = 0;                                             // of the barriers, a bit each
   Walk f = c;                                                      // the unit to be fetched next
   bool f_on = true;
-  int f_pid, f_row;                                                // page and row in it of this lane's key (lane mod KW; TMA: of the first)
+  // Pages.  Copy engine: of the warp's keys in 32 units from unit ids_base on, one a lane, and in the 32 after that; else of its keys
+  // in the next unit, one a lane.
+  int ids = -1, ids_after = -1, ids_base = 0, ids_seq = -1, f_row = 0;
+  auto ids_from = [&](int tile) {
+    const int key = (tile + lane) * C::TILE + warp * C::KW;
+    return key < f.len ? __ldg(f.row + p.page.quot(key)) : -1;
+  };
   auto read_ids = [&]() {
-    const int key = f.tile * C::TILE + warp * C::KW + (TMA ? 0 : lane & (C::KW - 1));
-    const int pg = (uint32_t)key / (uint32_t)p.page;
-    f_row = key - pg * p.page;
-    f_pid = f_on && key < f.len ? __ldg(f.row + pg) : -1;
+    if (!f_on) return;
+    if constexpr (TMA) {
+      if (f.s != ids_seq || f.tile < ids_base || f.tile >= ids_base + 64) {
+        ids_seq = f.s;
+        ids_base = f.tile;
+        ids = ids_from(f.tile);
+        ids_after = f.tiles > f.tile + 32 ? ids_from(f.tile + 32) : -1;
+      } else if (f.tile == ids_base + 32) {
+        ids_base = f.tile;
+        ids = ids_after;
+        ids_after = f.tiles > f.tile + 32 ? ids_from(f.tile + 32) : -1;
+      }
+    } else {
+      const int key = f.tile * C::TILE + warp * C::KW + (lane & (C::KW - 1)), pg = p.page.quot(key);
+      f_row = key - pg * (int)p.page.d;
+      ids = key < f.len ? __ldg(f.row + pg) : -1;
+    }
   };
   auto fetch = [&](int stage) {
     if (f_on) {
-      const bool there = f_pid >= 0 && f_pid < p.n_pages;
-      const int head = f.hr / p.row_tiles;
+      const int head = f.head;
       const uint32_t dst = ring + stage * C::STAGE;
       if constexpr (TMA) {
-        if (f.tile * C::TILE + warp * C::KW < f.len && !*s_abort) {   // (else the warp has no keys in the unit)
+        const int key = f.tile * C::TILE + warp * C::KW, id = __shfl_sync(0xffffffffu, ids, f.tile - ids_base);
+        if (key < f.len && !*s_abort) {                            // (else the warp has no keys in the unit)
           if (elect_one()) {
+            const bool there = id >= 0 && id < p.n_pages;
             s_mask[stage] = there ? 0xffffu : 0u;
             const uint32_t bar = bars + stage * 8;
             asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(C::STAGE) : "memory");
-            const int page = there ? f_pid : p.n_pages;            // beyond the pool: zeros, nothing is read
+            const int page = there ? id : p.n_pages, row = key - p.page.quot(key) * (int)p.page.d;   // beyond the pool: zeros, nothing is read
 #pragma unroll
             for (int b = 0; b < C::BOXES; ++b) {
-              tma_load(dst + b * C::BOX, &maps.k, bar, b * 64, head, f_row, page, p.layer);
-              tma_load(dst + C::HALF_STAGE + b * C::BOX, &maps.v, bar, b * 64, head, f_row, page, p.layer);
+              tma_load(dst + b * C::BOX, &maps.k, bar, b * 64, head, row, page, p.layer);
+              tma_load(dst + C::HALF_STAGE + b * C::BOX, &maps.v, bar, b * 64, head, row, page, p.layer);
             }
           }
           __syncwarp();
         }
       } else {
-        const int64_t off = there ? (int64_t)f_pid * p.page_bytes + (int64_t)f_row * p.slot_bytes + (int64_t)head * p.head_bytes : -1;
+        const bool there = ids >= 0 && ids < p.n_pages;
+        const int64_t off = there ? (int64_t)ids * p.page_bytes + (int64_t)f_row * p.slot_bytes + (int64_t)head * p.head_bytes : -1;
         const uint32_t mask = __ballot_sync(0xffffffffu, there) & ((1u << C::KW) - 1);
         if (lane == 0) s_mask[stage] = mask;
         constexpr int CH = D * (int)sizeof(T) / 16, N = C::KW * CH;   // 16-byte pieces of a row, of all rows
@@ -303,7 +342,6 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
       __syncwarp();
     }
   };
-  if constexpr (TMA) __syncwarp();                                 // (the barriers are the warp's own)
   read_ids();
 #pragma unroll
   for (int i = 0; i < C::STAGES - 1; ++i) fetch(i);
@@ -320,7 +358,7 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
   int first_tile = 0;                                              // of the item's part that this CTA has
 
   for (int stage = 0;; stage = stage + 1 == C::STAGES ? 0 : stage + 1) {
-    const int rt = c.hr % p.row_tiles, kvh = c.hr / p.row_tiles;
+    const int rt = c.rt, kvh = c.head;
     const int rows = min(R, p.rows - rt * R);                      // of this tile
     if (fresh) {                                                   // (the queries are on their way while the keys are waited for)
       fresh = false;
@@ -329,7 +367,7 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
       for (int i = 0; i < NACC; ++i) acc[i] = 0.f;
 #pragma unroll
       for (int i = 0; i < NST; ++i) {
-        const int r = C::BF ? (lane >> 2) + 8 * i : i, at = rt * R + r, tok = at / p.group;
+        const int r = C::BF ? (lane >> 2) + 8 * i : i, at = rt * R + r, tok = p.group_of.quot(at);
         m[i] = -INFINITY;
         l[i] = 0.f;
         vis[i] = r < rows ? c.len - p.n_new + 1 + tok : 0;
@@ -351,37 +389,39 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
     const bool mine = !TMA || key0 < c.len;                        // the warp has keys in the unit
     if (mine) wait(stage);
     fetch(stage == 0 ? C::STAGES - 1 : stage - 1);
-    const uint32_t kb = ring + stage * C::STAGE, vb = kb + C::HALF_STAGE;
-    uint8_t *vp = ring_p + stage * C::STAGE + C::HALF_STAGE;
     if (mine) {
+      uint8_t *kp = ring_p + stage * C::STAGE, *vp = kp + C::HALF_STAGE;
+      const uint32_t kb = ring + stage * C::STAGE, vb = kb + C::HALF_STAGE;
       const uint32_t mask = s_mask[stage];
       if constexpr (C::BF) {
         if (TMA && key0 + C::KW > c.len) {                         // rows of the page that are not the sequence's: 0 times them must be 0
           for (int e = lane; e < (key0 + C::KW - c.len) * 8 * C::BOXES; e += 32)
             *(uint4 *)(vp + (e & 7) * 16 + ((e >> 3) % C::BOXES) * C::BOX + (C::KW - 1 - (e >> 3) / C::BOXES) * 128) = make_uint4(0, 0, 0, 0);
+          fence_async_smem();                                      // (before the copy engine writes there again)
           __syncwarp();
         }
         const int t2 = (lane & 3) * 2;
         float sc[4 * NST];                                         // [row half][key block of 8][2 keys]
         {
-          float x[2][2][4];                                        // [key block][every second step]
-#pragma unroll
-          for (int i = 0; i < 16; ++i) x[i >> 3][(i >> 2) & 1][i & 3] = 0.f;
-          const int r = (lane & 7) + ((lane & 16) >> 1), sw = ((lane >> 3) ^ lane) & 1, rest_sw = lane & 6;
-          const uint32_t ka = kb + r * 128 + ((rest_sw | sw) << 4);
+          float x[2][4] = {};                                      // [key block]
+          const int r = (lane & 7) + ((lane & 16) >> 1), sw = ((lane >> 3) ^ lane) & 1;
+          const uint32_t ka = kb + r * 128 + (((lane & 6) | sw) << 4);
 #pragma unroll
           for (int j = 0; j < D / 16; ++j) {
             uint32_t b[4];
             ldsm_x4((ka ^ ((2 * j & 6) << 4)) + (j >> 2) * C::BOX, b);
             const uint32_t *q = qf + j * NST * 2;
-            mma16(x[0][j & 1], q[0], NST > 1 ? q[2 * (NST - 1)] : 0u, q[1], NST > 1 ? q[2 * (NST - 1) + 1] : 0u, b[0], b[1]);
-            mma16(x[1][j & 1], q[0], NST > 1 ? q[2 * (NST - 1)] : 0u, q[1], NST > 1 ? q[2 * (NST - 1) + 1] : 0u, b[2], b[3]);
+            mma16(x[0], q[0], NST > 1 ? q[2 * (NST - 1)] : 0u, q[1], NST > 1 ? q[2 * (NST - 1) + 1] : 0u, b[0], b[1]);
+            mma16(x[1], q[0], NST > 1 ? q[2 * (NST - 1)] : 0u, q[1], NST > 1 ? q[2 * (NST - 1) + 1] : 0u, b[2], b[3]);
           }
 #pragma unroll
+          for (int i = 0; i < 4 * NST; ++i) sc[i] = x[(i >> 1) & 1][2 * (i >> 2) + (i & 1)];
+        }
+        if (mask != 0xffffu || key0 + C::KW > c.len - p.n_new + 1) {   // (uniform) not every row sees every key
+#pragma unroll
           for (int i = 0; i < 4 * NST; ++i) {
-            const int h = i >> 2, blk = (i >> 1) & 1, o = i & 1, kk = blk * 8 + t2 + o;
-            const float y = x[blk][0][2 * h + o] + x[blk][1][2 * h + o];
-            sc[i] = (mask >> kk & 1) && key0 + kk < vis[h] ? y * p.scale_log2 : -INFINITY;
+            const int kk = ((i >> 1) & 1) * 8 + t2 + (i & 1);
+            if (!(mask >> kk & 1) || key0 + kk >= vis[i >> 2]) sc[i] = -INFINITY;
           }
         }
         bool grown = false;
@@ -390,7 +430,7 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
         for (int h = 0; h < NST; ++h) {
           float mx = fmaxf(fmaxf(sc[4 * h], sc[4 * h + 1]), fmaxf(sc[4 * h + 2], sc[4 * h + 3]));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2)) * p.scale_log2;
           a[h] = 1.f;
           if (mx > m[h] + GROWTH) {
             a[h] = ex2(m[h] - mx);
@@ -408,7 +448,7 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
         for (int h = 0; h < NST; ++h) {
           const float base = base_of(m[h]);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) sc[4 * h + i] = ex2(sc[4 * h + i] - base);
+          for (int i = 0; i < 4; ++i) sc[4 * h + i] = ex2(fmaf(sc[4 * h + i], p.scale_log2, -base));
           l[h] += (sc[4 * h] + sc[4 * h + 1]) + (sc[4 * h + 2] + sc[4 * h + 3]);
         }
         // A later token's key may lie in the tile although an earlier one does not see it; 0 times what is stored there must be 0
@@ -470,11 +510,10 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
             }
           }
         }
-        if (TMA && key0 + C::KW > c.len) fence_async_smem();       // (the zeros, before the copy engine writes there again)
       } else {
         // scores: a key has four lanes, each a quarter of the dims (every fourth piece of four)
         const int key = lane >> 2, part = lane & 3;
-        const float *kr = (const float *)(ring_p + stage * C::STAGE + key * C::PITCH);
+        const float *kr = (const float *)(kp + key * C::PITCH);
         float s[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) s[r] = 0.f;
@@ -570,9 +609,9 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
       const int slot = first_tile == 0 ? 1 : 0;                    // pieces of a CTA: of an item it begins, of one it goes on with
       float *piece = p.pieces + ((int64_t)blockIdx.x * 2 + slot) * paged::ROW_TILE * D;
       float *mls = p.pieces + (int64_t)MAX_CTAS * 2 * paged::ROW_TILE * D;
-      constexpr int C4 = D / 4, EACH = (R * C4 + THREADS - 1) / THREADS;
+      constexpr int C4 = D / 4, EACH = (R * C4 + THREADS - 1) / THREADS;      // columns of four a row; of them a thread has at a time
       auto finish = [&](int r, int col, float M, float L, const float *o) {       // four columns of a row to the output
-        const int at = rt * R + r, tok = at / p.group, head = kvh * p.group + at - tok * p.group;
+        const int at = rt * R + r, tok = p.group_of.quot(at), head = kvh * p.group + at - tok * p.group;
         const int64_t row = ((int64_t)was.s * p.n_new + tok) * p.H + head;
         const float inv = L == 0.f ? 0.f : 1.f / L;
         if constexpr (C::BF)
@@ -583,16 +622,13 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
       };
       for (int e = tid; e < rows * C4; e += THREADS) {
         const int r = e / C4, col = (e - r * C4) * 4;
-        float mw[WARPS], M = -INFINITY, L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+        float M = -INFINITY, L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < WARPS; ++w) {
-          mw[w] = s_ml[(w * R + r) * 2];
-          M = fmaxf(M, mw[w]);
-        }
+        for (int w = 0; w < WARPS; ++w) M = fmaxf(M, s_ml[(w * R + r) * 2]);
         const float base = base_of(M);
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) {
-          const float a = ex2(mw[w] - base);
+          const float a = ex2(s_ml[(w * R + r) * 2] - base);
           const float4 x = *(const float4 *)(smem + C::OFF_RING + (w * C::STAGES + stage) * C::STAGE + (r * D + (col ^ ((r & 3) * 8))) * 4);
           L = fmaf(a, s_ml[(w * R + r) * 2 + 1], L);
           o[0] = fmaf(a, x.x, o[0]);
@@ -609,7 +645,7 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
       }
       if (!whole) {
         // The cuts inside the item, which are those that place() leaves there; c0 has its beginning, c1 its end.
-        const int64_t item0 = (int64_t)s_cum[was.s] * F + (int64_t)was.hr * (was.tiles + ITEM_COST) + ITEM_COST;
+        const int64_t item0 = (int64_t)s_cum[was.s] * F + (int64_t)(was.head * p.row_tiles + was.rt) * (was.tiles + ITEM_COST) + ITEM_COST;
         const int64_t lo = item0 + SNAP + 1, hi = item0 + was.tiles - SNAP - 1;
         const int c0 = (int)((lo * G + cost - 1) / cost) - 1, c1 = (int)(((hi + 1) * G + cost - 1) / cost) - 1;
         __threadfence();
@@ -620,47 +656,49 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
           if (tid == 0) p.counters[c0] = 0;
           __threadfence();
           float2 *s_join = (float2 *)(smem + C::OFF_JOIN);
-          float M[EACH], L[EACH], o[EACH][4];
-#pragma unroll
-          for (int k = 0; k < EACH; ++k) {
-            M[k] = -INFINITY;
-            L[k] = o[k][0] = o[k][1] = o[k][2] = o[k][3] = 0.f;
-          }
           auto where = [&](int cta) { return ((int64_t)cta * 2 + (cta == c0 ? 1 : 0)) * paged::ROW_TILE; };
-          for (int a0 = c0; a0 <= c1; a0 += C::CHUNK) {
-            const int many = min(C::CHUNK, c1 - a0 + 1);
-            for (int i = tid; i < many * R; i += THREADS)
-              if (i % R < rows) s_join[i] = __ldcg((const float2 *)(mls + (where(a0 + i / R) + i % R) * 2));
-            __syncthreads();
+          {
+            float M[EACH], L[EACH], o[EACH][4];
 #pragma unroll
             for (int k = 0; k < EACH; ++k) {
-              const int e = k * THREADS + tid, r = e / C4, col = (e - r * C4) * 4;
-              if (e >= rows * C4) break;
-              float mx = M[k];
-              for (int j = 0; j < many; ++j) mx = fmaxf(mx, s_join[j * R + r].x);
-              const float base = base_of(mx), a = ex2(M[k] - base);
-              M[k] = mx;
-              L[k] *= a;
-#pragma unroll
-              for (int i = 0; i < 4; ++i) o[k][i] *= a;
-#pragma unroll 8
-              for (int j = 0; j < many; ++j) {
-                const float4 y = __ldcg((const float4 *)(p.pieces + (where(a0 + j) + r) * D + col));
-                const float2 ml = s_join[j * R + r];
-                const float x = ex2(ml.x - base);
-                L[k] = fmaf(x, ml.y, L[k]);
-                o[k][0] = fmaf(x, y.x, o[k][0]);
-                o[k][1] = fmaf(x, y.y, o[k][1]);
-                o[k][2] = fmaf(x, y.z, o[k][2]);
-                o[k][3] = fmaf(x, y.w, o[k][3]);
-              }
+              M[k] = -INFINITY;
+              L[k] = o[k][0] = o[k][1] = o[k][2] = o[k][3] = 0.f;
             }
-            __syncthreads();
-          }
+            for (int a0 = c0; a0 <= c1; a0 += C::CHUNK) {
+              const int many = min(C::CHUNK, c1 - a0 + 1);
+              for (int i = tid; i < many * R; i += THREADS)
+                if (i % R < rows) s_join[i] = __ldcg((const float2 *)(mls + (where(a0 + i / R) + i % R) * 2));
+              __syncthreads();
 #pragma unroll
-          for (int k = 0; k < EACH; ++k) {
-            const int e = k * THREADS + tid, r = e / C4;
-            if (e < rows * C4) finish(r, (e - r * C4) * 4, M[k], L[k], o[k]);
+              for (int k = 0; k < EACH; ++k) {
+                const int e = k * THREADS + tid, r = e / C4, col = (e - r * C4) * 4;
+                if (e >= rows * C4) break;
+                float mx = M[k];
+                for (int j = 0; j < many; ++j) mx = fmaxf(mx, s_join[j * R + r].x);
+                const float base = base_of(mx), a = ex2(M[k] - base);
+                M[k] = mx;
+                L[k] *= a;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[k][i] *= a;
+#pragma unroll 8
+                for (int j = 0; j < many; ++j) {
+                  const float4 y = __ldcg((const float4 *)(p.pieces + (where(a0 + j) + r) * D + col));
+                  const float2 ml = s_join[j * R + r];
+                  const float x = ex2(ml.x - base);
+                  L[k] = fmaf(x, ml.y, L[k]);
+                  o[k][0] = fmaf(x, y.x, o[k][0]);
+                  o[k][1] = fmaf(x, y.y, o[k][1]);
+                  o[k][2] = fmaf(x, y.z, o[k][2]);
+                  o[k][3] = fmaf(x, y.w, o[k][3]);
+                }
+              }
+              __syncthreads();
+            }
+#pragma unroll
+            for (int k = 0; k < EACH; ++k) {
+              const int e = k * THREADS + tid, r = e / C4;
+              if (e < rows * C4) finish(r, (e - r * C4) * 4, M[k], L[k], o[k]);
+            }
           }
         }
       }
@@ -722,8 +760,8 @@ int launch(const AttnParams &p, const Maps &maps, int64_t most_cost, cudaStream_
 template <int D>
 int by_kind(const ouro_paged_cache *c, AttnParams p, bool tma, const Maps &maps, int64_t cost, cudaStream_t s) {
   if (c->dtype == OURO_F32) return launch<float, D, 8, false>(p, maps, cost, s);
-  if (tma) return p.rows <= 8 ? launch<__nv_bfloat16, D, 8, true>(p, maps, cost, s) : launch<__nv_bfloat16, D, 16, true>(p, maps, cost, s);
-  return p.rows <= 8 ? launch<__nv_bfloat16, D, 8, false>(p, maps, cost, s) : launch<__nv_bfloat16, D, 16, false>(p, maps, cost, s);
+  if (p.rows <= 8) return tma ? launch<__nv_bfloat16, D, 8, true>(p, maps, cost, s) : launch<__nv_bfloat16, D, 8, false>(p, maps, cost, s);
+  return tma ? launch<__nv_bfloat16, D, 16, true>(p, maps, cost, s) : launch<__nv_bfloat16, D, 16, false>(p, maps, cost, s);
 }
 
 }  // namespace
@@ -735,6 +773,7 @@ extern "C" int ouro_paged_attention(const ouro_paged_cache *c, int32_t layer, co
   if (n < 0 || n > OURO_MAX_LIST) return paged::refuse(CALL, "n is below 0 or above OURO_MAX_LIST");
   if (n_new < 1 || n_new > OURO_MAX_NEW) return paged::refuse(CALL, "n_new is below 1 or above OURO_MAX_NEW");
   if (n_heads < 1 || n_heads % c->n_kv_heads) return paged::refuse(CALL, "n_heads is not a multiple of the cache's n_kv_heads");
+  if (!(scale > 0.f) || scale > 1e30f) return paged::refuse(CALL, "scale is not a positive number");
   if (n == 0) return OURO_OK;
   if (!q || !out) return paged::refuse(CALL, "q or out is NULL");
   if (!seqs && n > c->max_seqs) return paged::refuse(CALL, "more sequences than the table has");
@@ -758,7 +797,8 @@ extern "C" int ouro_paged_attention(const ouro_paged_cache *c, int32_t layer, co
   p.pieces = (float *)((char *)c->workspace + l.pieces);
   p.page_bytes = c->page_stride * esize; p.slot_bytes = c->slot_stride * esize; p.head_bytes = c->head_stride * esize; p.q_stride = q_stride;
   p.n = n; p.n_new = n_new; p.H = n_heads; p.Hkv = c->n_kv_heads; p.layer = layer;
-  p.n_pages = c->n_pages; p.page = c->page_size; p.max_pages = c->max_pages; p.max_seqs = c->max_seqs;
+  p.page.set(c->page_size); p.group_of.set(p.group);
+  p.n_pages = c->n_pages; p.max_pages = c->max_pages; p.max_seqs = c->max_seqs;
   p.scale_log2 = scale * 1.4426950408889634f;
   // The copy engine fetches 16 rows of a head at a time: where pages are multiples of that.
   Maps maps{};

@@ -552,9 +552,10 @@ def test_refusals_that_need_no_gpu():
                      lambda d: L.ouro_paged_attention(d, 0, None, 1, 1, 256, 128, 2, 1.0, 256, None, None), lambda d: L.ouro_paged_status(d, None)):
             assert call(desc(**bad)) == binding.OURO_EINVAL and L.ouro_last_error(None).startswith(b"ouro_paged_"), bad
     d = desc()
-    att = lambda layer=0, n=1, new=1, q=256, stride=128, heads=2, out=256: L.ouro_paged_attention(d, layer, None, n, new, q, stride, heads, 1.0, out, None, None)
+    att = lambda layer=0, n=1, new=1, q=256, stride=128, heads=2, out=256, scale=1.0: L.ouro_paged_attention(
+        d, layer, None, n, new, q, stride, heads, scale, out, None, None)
     for bad in (dict(layer=1), dict(layer=-1), dict(n=-1), dict(n=1025), dict(new=0), dict(new=17), dict(heads=3), dict(heads=0), dict(q=0), dict(out=0), dict(q=8), dict(stride=124),
-                dict(stride=64), dict(n=3)):
+                dict(stride=64), dict(n=3), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf"))):
         assert att(**bad) == binding.OURO_EINVAL, bad
     assert att(n=0) == binding.OURO_OK
     app = lambda layer=0, q=256, qs=128, k=256, kvs=128, rows=1, heads=2, slots=256, cos=256, np_=4, out=512: L.ouro_paged_append(
