@@ -18,7 +18,7 @@ import math
 import torch
 
 from . import binding
-from .binding import OURO_BF16, OURO_F32, PagedCacheC, _check, lib
+from .binding import OURO_BF16, OURO_F32, PagedCacheC, _check, current_stream, lib
 
 _DTYPES = {torch.float32: OURO_F32, torch.bfloat16: OURO_BF16}
 
@@ -68,10 +68,11 @@ class PagedCache:
             self.reset()
 
     def _stream(self):
-        # (the library launches on the current device; leaving it alone where it is the cache's already saves two calls to the driver)
-        if torch.cuda.current_device() != self.device.index:
-            raise RuntimeError(f"the current device is not the cache's ({self.device}): use torch.cuda.device")
-        return torch.cuda.current_stream(self.device).cuda_stream
+        return current_stream(self.device.index)
+
+    def _like(self, q, contiguous):
+        # (empty_like is the quickest way to a new tensor, but keeps strides)
+        return torch.empty_like(q) if contiguous else torch.empty(q.shape, dtype=q.dtype, device=self.device)
 
     def _list(self, t, name, n=None):
         if t.dtype is not torch.int32 or t.device != self.device or not t.is_contiguous() or (n is not None and t.numel() != n):
@@ -100,11 +101,11 @@ class PagedCache:
     def extend(self, seqs, new_tokens, width: int):
         """Room for new_tokens[i] <= width more tokens of sequence seqs[i].  Returns slots and positions [n, width], -1 where there is none."""
         n = seqs.numel()
-        out = torch.empty((2, n, width), dtype=torch.int32, device=self.device)
-        at = out.data_ptr()
-        _check(self._L.ouro_paged_extend(self._p, self._list(seqs, "seqs"), self._list(new_tokens, "new_tokens", n), n, width, at, at + 4 * n * width,
-                                         self._stream()))
-        return out[0], out[1]
+        slots = torch.empty_strided((n, width), (width, 1), dtype=torch.int32, device=self.device)
+        positions = torch.empty_like(slots)
+        _check(self._L.ouro_paged_extend(self._p, self._list(seqs, "seqs"), self._list(new_tokens, "new_tokens", n), n, width, slots.data_ptr(),
+                                         positions.data_ptr(), self._stream()))
+        return slots, positions
 
     def compact(self):
         """Moves the pages in use to the lowest ids.  Returns their number [1]."""
@@ -140,7 +141,7 @@ class PagedCache:
         if self._rows(v, "v", self.n_kv_heads) != k_stride or k.shape[0] != rows or v.shape[0] != rows:
             raise ValueError("q, k and v need the same number of rows, k and v the same distance between them")
         if out is None:
-            out = torch.empty((rows, heads, self.head_dim), dtype=q.dtype, device=self.device)
+            out = self._like(q, q.is_contiguous())
         elif out.shape != q.shape or not out.is_contiguous() or out.dtype is not q.dtype or out.device != self.device:
             raise ValueError("out has to be like q, and contiguous")
         if cos.dtype is not torch.float32 or cos.shape != sin.shape or cos.shape[-1] * 2 != self.head_dim or not (cos.is_contiguous() and sin.is_contiguous()) \
@@ -160,7 +161,7 @@ class PagedCache:
             raise ValueError("q: [n, heads, head_dim] or [n, t, heads, head_dim] is needed")
         stride = self._rows(q, "q")
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=self.device)
+            out = self._like(q, q.is_contiguous())
         elif out.shape != q.shape or not out.is_contiguous() or out.dtype is not q.dtype or out.device != self.device:
             raise ValueError("out has to be like q, and contiguous")
         lse = torch.empty(q.shape[:-1], dtype=torch.float32, device=self.device) if want_lse else None

@@ -5,7 +5,7 @@ from typing import NamedTuple
 
 import torch
 
-from .binding import OURO_BF16, OURO_F32, _check, lib
+from .binding import OURO_BF16, OURO_F32, _check, current_stream, lib
 
 _DTYPES = {torch.float32: OURO_F32, torch.bfloat16: OURO_BF16}
 
@@ -24,16 +24,13 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None, n_t
         raise ValueError("logits: a CUDA tensor [rows, vocab], f32 or bf16, with dense rows is needed (this library has no CPU path)")
     rows, vocab = logits.shape
     dev = logits.device
-    if torch.cuda.current_device() != dev.index:
-        raise RuntimeError(f"the current device is not that of the logits ({dev}): use torch.cuda.device")
     if tokens is not None and (tokens.dtype is not torch.int32 or tokens.device != dev or tokens.numel() != rows or not tokens.is_contiguous()):
         raise ValueError(f"tokens: a contiguous int32 tensor of {rows} elements on {dev} is needed")
-    out = torch.empty((2, rows), dtype=torch.float32, device=dev)
-    ids = torch.empty((rows, n_top), dtype=torch.int32, device=dev) if n_top > 0 else None
-    top = torch.empty((rows, n_top), dtype=torch.float32, device=dev) if n_top > 0 else None
-    at = out.data_ptr()
+    entropy = torch.empty(rows, dtype=torch.float32, device=dev)
+    logprob = torch.empty_like(entropy) if tokens is not None else None
+    ids = torch.empty_strided((rows, n_top), (n_top, 1), dtype=torch.int32, device=dev) if n_top > 0 else None
+    top = torch.empty_like(ids, dtype=torch.float32) if n_top > 0 else None
     _check(lib().ouro_token_logprobs(logits.data_ptr(), _DTYPES[logits.dtype], logits.stride(0), rows, vocab,
-                                     None if tokens is None else tokens.data_ptr(), n_top, None if tokens is None else at, at + 4 * rows,
-                                     None if ids is None else ids.data_ptr(), None if top is None else top.data_ptr(),
-                                     torch.cuda.current_stream(dev).cuda_stream))
-    return TokenScores(None if tokens is None else out[0], out[1], ids, top)
+                                     None if tokens is None else tokens.data_ptr(), n_top, None if tokens is None else logprob.data_ptr(), entropy.data_ptr(),
+                                     None if ids is None else ids.data_ptr(), None if top is None else top.data_ptr(), current_stream(dev.index)))
+    return TokenScores(logprob, entropy, ids, top)
