@@ -175,9 +175,9 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
     const int per = (p.n + THREADS - 1) / THREADS;
     int sum = 0;
     for (int i = tid * per; i < min(p.n, (tid + 1) * per); ++i) {
-      const int sid = p.seqs ? __ldg(p.seqs + i) : i;
-      int len = 0;
-      if (sid >= 0 && sid < p.max_seqs) len = min(max(__ldg(p.lens + sid), 0), p.cap);
+      const int sid = p.seqs ? p.seqs[i] : i;
+      const bool known = sid >= 0 && sid < p.max_seqs;              // (here and below: addresses are valid whether or not the value is wanted)
+      const int len = known ? min(max(p.lens[known ? sid : 0], 0), p.cap) : 0;
       s_len[i] = len;
       sum += max(1, (len + C::TILE - 1) / C::TILE) + ITEM_COST;
     }
@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
   auto enter = [&](Walk &w) {
     w.len = s_len[w.s];
     w.tiles = s_cum[w.s + 1] - s_cum[w.s] - ITEM_COST;
-    const int sid = p.seqs ? __ldg(p.seqs + w.s) : w.s;
+    const int sid = p.seqs ? p.seqs[w.s] : w.s;
     w.row = p.table + (int64_t)(w.len > 0 ? sid : 0) * p.max_pages;
   };
   auto next = [&](Walk &w) {
@@ -257,7 +257,7 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
   int ids = -1, ids_after = -1, ids_base = 0, ids_seq = -1, f_row = 0;
   auto ids_from = [&](int tile) {
     const int key = (tile + lane) * C::TILE + warp * C::KW;
-    return key < f.len ? __ldg(f.row + p.page.quot(key)) : -1;
+    return key < f.len ? f.row[key < f.len ? p.page.quot(key) : 0] : -1;
   };
   auto read_ids = [&]() {
     if (!f_on) return;
@@ -275,7 +275,7 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
     } else {
       const int key = f.tile * C::TILE + warp * C::KW + (lane & (C::KW - 1)), pg = p.page.quot(key);
       f_row = key - pg * (int)p.page.d;
-      ids = key < f.len ? __ldg(f.row + pg) : -1;
+      ids = key < f.len ? f.row[key < f.len ? pg : 0] : -1;
     }
   };
   auto fetch = [&](int stage) {
@@ -367,7 +367,7 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
       for (int i = 0; i < NACC; ++i) acc[i] = 0.f;
 #pragma unroll
       for (int i = 0; i < NST; ++i) {
-        const int r = C::BF ? (lane >> 2) + 8 * i : i, at = rt * R + r, tok = p.group_of.quot(at);
+        const int r = C::BF ? (lane >> 2) + 8 * i : i, at = rt * R + min(r, rows - 1), tok = p.group_of.quot(at);
         m[i] = -INFINITY;
         l[i] = 0.f;
         vis[i] = r < rows ? c.len - p.n_new + 1 + tok : 0;
@@ -376,11 +376,11 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
           const uint32_t *src = (const uint32_t *)((const __nv_bfloat16 *)p.q + q_at) + (lane & 3);
 #pragma unroll
           for (int j = 0; j < D / 16; ++j) {
-            qf[(j * NST + i) * 2] = r < rows ? __ldg(src + j * 8) : 0u;
-            qf[(j * NST + i) * 2 + 1] = r < rows ? __ldg(src + j * 8 + 4) : 0u;
+            qf[(j * NST + i) * 2] = r < rows ? src[j * 8] : 0u;
+            qf[(j * NST + i) * 2 + 1] = r < rows ? src[j * 8 + 4] : 0u;
           }
         } else {
-          for (int d = lane; d < D; d += 32) s_q[r * D + d] = r < rows ? __ldg((const float *)p.q + q_at + d) : 0.f;
+          for (int d = lane; d < D; d += 32) s_q[r * D + d] = r < rows ? ((const float *)p.q)[q_at + d] : 0.f;
         }
       }
       if (!C::BF) __syncwarp();

@@ -166,7 +166,7 @@ __device__ __forceinline__ void round_of(const CacheDev &c, int base, int *s_cou
 #pragma unroll
   for (int j = 0; j < ROUND; ++j) {
     const int id = base + j * PLAN_THREADS + tid;
-    kind[j] = id < c.n_pages ? c.refs[id] : -1;
+    kind[j] = c.refs[min(id, c.n_pages - 1)];
   }
 #pragma unroll
   for (int j = 0; j < ROUND; ++j) {
@@ -399,14 +399,14 @@ __global__ void __launch_bounds__(COPY_THREADS) copy_kernel(const CacheDev c, co
       int64_t off[UNROLL];
 #pragma unroll
       for (int j = 0; j < UNROLL; ++j) {
-        const int e = e0 + j * 32 + lane;
+        const int e = min(e0 + j * 32 + lane, pieces - 1);         // (always a valid address; stored only where it is meant)
         if (WHOLE) {
           off[j] = (int64_t)e * 16;
         } else {
           const int row = e / per_row, in = e - row * per_row, head = in / p.row_pieces;
           off[j] = row * p.slot_bytes + head * p.head_bytes + (int64_t)(in - head * p.row_pieces) * 16;
         }
-        if (e < pieces) x[j] = __ldcs((const uint4 *)(from + off[j]));
+        x[j] = __ldcs((const uint4 *)(from + off[j]));
       }
 #pragma unroll
       for (int j = 0; j < UNROLL; ++j)

@@ -3,14 +3,17 @@
 //     m = max x,  Z = sum e^(x - m),  T = sum (x - m) e^(x - m)
 //     log p(t) = (x_t - m) - ln Z,    H = ln Z - T / Z
 //
-// Bound by HBM: a logit is read once and costs a dozen instructions.  A row is a CTA's or, where rows are few, a cluster's, whose
-// CTAs join through shared memory: one launch, no workspace.
-//  - A thread keeps (m, Z, T) of what it has seen, in 32 bits, relative to its own maximum, sixteen logits at a time.
-//  - A warp keeps the best alternatives it has seen sorted over its lanes, as 64-bit keys (value in an order-preserving integer image,
-//    then the complement of the id: no two are equal, and the lowest id is first among equals).  The maximum of a thread's sixteen logits, which
-//    the sum needs anyway, is compared to the last of them; only where it is larger does anybody look closer.  Where many lanes have something
-//    to offer (at the beginning, or in rows that ascend), the n-th largest of the lanes' maxima is found first: what is below it cannot be
-//    among the best n.
+// Bound by HBM without alternatives (2048 rows of 64000 f32: 81 us, 6.5 TB/s); with them by what the warps have to issue (20: 114 us, of 67 %
+// of the issue slots; bf16, 5: 88 us for 40.6).  A row is a CTA's or, where rows are few, a cluster's, whose CTAs join through shared
+// memory: one launch, no workspace.
+//  - A thread keeps (m, Z, T) of what it has seen, in 32 bits, relative to its own maximum, sixteen logits at a time, two in an instruction.
+//  - Candidates for the best alternatives go to a buffer of the CTA as 64-bit keys (value in an order-preserving integer image, then the
+//    complement of the id: no two are equal, and the lowest id is first among equals).  After 1, 2, 4, .. batches of THREADS * E logits the
+//    buffer is cut down to the best n; in between only what is larger than the n-th gets in, n for every doubling on average, which
+//    the maximum of a thread's sixteen logits, needed for the sum anyway, mostly rules out for all of them.  In the first batch, k of each
+//    warp make n, so the smallest of the warps' k-th largest maxima bounds the n-th best of all from below; and where many lanes of a warp have
+//    something to offer later (in rows that ascend), so does the n-th largest of the lanes' maxima.  Rows that fill the buffer all the same are done
+//    again with a look at it after every batch.
 #include "paged.h"
 #include "row_ops.cuh"
 
@@ -18,9 +21,10 @@
 
 namespace {
 
-constexpr int THREADS = 256, WARPS = THREADS / 32;
 constexpr int E = 16;                              // logits of a thread at a time
 constexpr int CROWD = 8;                           // lanes with something to offer from which on the maxima are sorted first
+constexpr int GROWTH = 4;                          // the buffer is cut down after this many times as many batches as before
+constexpr int WATER = 256;                         // candidates at which the buffer is cut down where that is looked at; a batch adds THREADS * E at most
 constexpr float LOG2E = 1.4426950408889634f;
 
 struct ScoreParams {
@@ -43,9 +47,39 @@ __device__ __forceinline__ float max_nan(float a, float b) {      // NaN where e
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
   return y;
 }
+__device__ __forceinline__ float max_nan(float a, float b, float c) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
+// Two 32-bit numbers at a time.
+__device__ __forceinline__ u64 pair(float a, float b) {
+  u64 y;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"(a), "f"(b));
+  return y;
+}
+__device__ __forceinline__ void unpair(u64 x, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x)); }
+__device__ __forceinline__ u64 add2(u64 a, u64 b) {
+  u64 y;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b));
+  return y;
+}
+__device__ __forceinline__ u64 mul2(u64 a, u64 b) {
+  u64 y;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b));
+  return y;
+}
+__device__ __forceinline__ u64 fma2(u64 a, u64 b, u64 c) {
+  u64 y;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(y) : "l"(a), "l"(b), "l"(c));
+  return y;
+}
 // Integer image of a logit: larger logit, larger integer; NaN above all, -0 like +0; never 0.
 __device__ __forceinline__ uint32_t image(float x) {
-  const uint32_t u = __float_as_uint(x + 0.f);
+  // (volatile: else the images of sixteen logits are made in front of the branch behind which, rarely, they are wanted: 120 of 250 instructions a batch)
+  float y;
+  asm volatile("add.f32 %0, %1, 0f00000000;" : "=f"(y) : "f"(x));
+  const uint32_t u = __float_as_uint(y);
   return x != x ? 0xffffffffu : u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float value_of(uint32_t im) {
@@ -67,17 +101,23 @@ __device__ __forceinline__ void join(Sums &a, const Sums &b) {
 }
 
 // Lists of 32 keys over a warp's lanes, largest first.
-__device__ __forceinline__ u64 sorted(u64 x, int lane) {          // x is bitonic
+__device__ __forceinline__ u64 exchanged(u64 x, int o, bool larger) {
+  const u64 y = __shfl_xor_sync(0xffffffffu, x, o);
+  return (x > y) == larger ? x : y;
+}
+__device__ __forceinline__ u64 sorted(u64 x, int lane) {
 #pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    const u64 y = __shfl_xor_sync(0xffffffffu, x, o);
-    x = (lane & o) == 0 ? (x > y ? x : y) : (x > y ? y : x);
-  }
+  for (int k = 2; k <= 32; k <<= 1)
+#pragma unroll
+    for (int o = k >> 1; o; o >>= 1) x = exchanged(x, o, ((lane & o) == 0) == ((lane & k) == 0));
   return x;
 }
 __device__ __forceinline__ u64 merged(u64 a, u64 b, int lane) {   // the best 32 of two lists
   b = __shfl_sync(0xffffffffu, b, 31 - lane);
-  return sorted(a > b ? a : b, lane);
+  u64 x = a > b ? a : b;                                          // bitonic
+#pragma unroll
+  for (int o = 16; o; o >>= 1) x = exchanged(x, o, (lane & o) == 0);
+  return x;
 }
 
 template <typename T>
@@ -104,51 +144,126 @@ __device__ __forceinline__ void unpack16<__nv_bfloat16>(const uint4 *raw, float 
     }
   }
 }
-__device__ __forceinline__ float one(const float *p) { return __ldg(p); }
-__device__ __forceinline__ float one(const __nv_bfloat16 *p) { return __bfloat162float(__ldg(p)); }
+__device__ __forceinline__ float one(const float *p) { return *p; }
+__device__ __forceinline__ float one(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
 
-// The best alternatives a warp has seen.
+// The CTA's candidates.
+template <int THREADS>
 struct Best {
-  u64 mine = 0;                                    // lane i: the i-th best, 0: none yet
-  float last = 0.f;                                // value of the n-th
-  bool full = false;                               // there are n
+  static constexpr int WARPS = THREADS / 32;
+  static constexpr int BUFFER = WATER + THREADS * E + 32;          // (in front of the first and behind the last whole 16 bytes there are 7 at most)
+  u64 *buffer;                                     // [BUFFER]
+  u64 *lists;                                      // [WARPS][32]
+  int *count;
+  uint32_t *bounds;                                // [WARPS]
+  float last;                                      // value of the n-th of those that were there when the buffer was last cut down
+  bool full;                                       // there were n
+  bool much;                                       // this thread has seen the buffer filled to WATER
+  bool over;                                       // something of this thread's did not get in
 
-  __device__ __forceinline__ void insert(u64 k, int lane) {
-    const int at = __popc(__ballot_sync(0xffffffffu, mine > k));
-    const u64 up = __shfl_up_sync(0xffffffffu, mine, 1);
-    mine = lane < at ? mine : lane == at ? k : up;
+  // The n-th largest of the lanes' numbers.
+  static __device__ __forceinline__ uint32_t nth(uint32_t s, int n, int lane) {
+#pragma unroll
+    for (int k = 2; k <= 32; k <<= 1)
+#pragma unroll
+      for (int o = k >> 1; o; o >>= 1) {
+        const uint32_t y = __shfl_xor_sync(0xffffffffu, s, o);
+        s = ((lane & o) == 0) == ((lane & k) == 0) ? max(s, y) : min(s, y);
+      }
+    return __shfl_sync(0xffffffffu, s, n - 1);
   }
-  // N logits of every lane: x[i] has id base + i % per + (i / per) * far, if bit i / per of there is set; top: the largest of them
-  // (NaN where there is one).
+  // All lanes' logits from bound on: x[i] has id base + i % per + (i / per) * far, if bit i / per of there is set.
+  template <int N>
+  __device__ __forceinline__ void push(const float *x, uint32_t bound, uint32_t base, int per, uint32_t far, uint32_t there, int lane) {
+    uint32_t take = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (image(x[i]) >= bound && (there >> (i / per) & 1)) take |= 1u << i;
+    const int mine = __popc(take);                 // places in the buffer: one request for the warp
+    int at = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int up = __shfl_up_sync(0xffffffffu, at, o);
+      if (lane >= o) at += up;
+    }
+    int first = 0;
+    if (lane == 31 && at > 0) first = atomicAdd(count, at);
+    at += __shfl_sync(0xffffffffu, first, 31) - mine;
+    much |= take != 0 && at + mine > WATER;
+    if (at + mine > BUFFER) over = true, take = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (take >> i & 1) buffer[at++] = (u64)image(x[i]) << 32 | (0xffffffffu - (base + i % per + (uint32_t)(i / per) * far));
+    __syncwarp();
+  }
+  // The same logits, those that may be among the best n; top: the largest of a lane (NaN where there is one).
   template <int N>
   __device__ __forceinline__ void offer(const float *x, float top, uint32_t base, int per, uint32_t far, uint32_t there, int n, int lane) {
-    const uint32_t some = __ballot_sync(0xffffffffu, there != 0 && (!full || !(top <= last)));
+    const bool have = there != 0 && (!full || !(top <= last));
+    const uint32_t some = __ballot_sync(0xffffffffu, have);
     if (some == 0) return;
-    uint32_t bound = full ? image(last) + 1 : 1;
-    if (__popc(some) >= CROWD) {
-      uint32_t s = there ? image(top) : 0;
+    if (full && __popc(some) < CROWD) {
+      if (have) {
 #pragma unroll
-      for (int k = 2; k <= 32; k <<= 1)
+        for (int g = 0; g < N; g += 4) {           // (four at a time: their maximum is there already)
+          float four = x[g];
 #pragma unroll
-        for (int o = k >> 1; o; o >>= 1) {
-          const uint32_t y = __shfl_xor_sync(0xffffffffu, s, o);
-          s = ((lane & o) == 0) == ((lane & k) == 0 || k == 32) ? max(s, y) : min(s, y);
+          for (int i = g + 1; i < g + 4 && i < N; ++i) four = max_nan(four, x[i]);
+          if (!(four <= last)) {
+#pragma unroll
+            for (int i = g; i < g + 4 && i < N; ++i)
+              if (!(x[i] <= last) && (there >> (i / per) & 1)) {
+                const int at = atomicAdd(count, 1);
+                much |= at >= WATER;
+                if (at < BUFFER) buffer[at] = (u64)image(x[i]) << 32 | (0xffffffffu - (base + i % per + (uint32_t)(i / per) * far));
+                else over = true;
+              }
+          }
         }
-      bound = max(bound, __shfl_sync(0xffffffffu, s, n - 1));
+      }
+      __syncwarp();
+    } else {                                       // (nothing is above NaN: then all are candidates, and lose)
+      push<N>(x, max(full ? image(last) + 1 : 1, nth(there ? image(top) : 0, n, lane)), base, per, far, there, lane);
+    }
+  }
+  // The first logits, all warps.
+  template <int N>
+  __device__ __forceinline__ void begin(const float *x, float top, uint32_t base, int per, uint32_t far, uint32_t there, int n, int warp, int lane) {
+    const uint32_t k_th = nth(there ? image(top) : 0, (n + WARPS - 1) / WARPS, lane);
+    if (lane == 0) bounds[warp] = k_th;
+    __syncthreads();
+    uint32_t b = bounds[0];
+#pragma unroll
+    for (int w = 1; w < WARPS; ++w) b = min(b, bounds[w]);
+    push<N>(x, max(b, 1u), base, per, far, there, lane);
+  }
+  // The best 32 to the buffer's beginning, in order.  All threads, behind a barrier.
+  __device__ __forceinline__ void cut(int n, int warp, int lane) {
+    const int c = min(*count, BUFFER), chunks = (c + 31) / 32;
+    u64 mine = 0;
+    for (int i = warp; i < chunks; i += WARPS) {
+      const u64 x = sorted(i * 32 + lane < c ? buffer[i * 32 + lane] : 0, lane);
+      mine = i == warp ? x : merged(mine, x, lane);
     }
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const uint32_t im = image(x[i]), id = base + i % per + (uint32_t)(i / per) * far;
-      uint32_t who = __ballot_sync(0xffffffffu, (there >> (i / per) & 1) && im >= bound);
-      while (who) {
-        const int src = __ffs(who) - 1;
-        who &= who - 1;
-        insert((u64)__shfl_sync(0xffffffffu, im, src) << 32 | (0xffffffffu - __shfl_sync(0xffffffffu, id, src)), lane);
-      }
+    for (int half = WARPS / 2; half; half >>= 1) {
+      if (chunks <= half) continue;                // (no list there; the same for all)
+      if (warp >= half && warp < 2 * half) lists[warp * 32 + lane] = mine;
+      __syncthreads();
+      if (warp < half) mine = merged(mine, lists[(warp + half) * 32 + lane], lane);
+      __syncthreads();
     }
-    const uint32_t nth = (uint32_t)(__shfl_sync(0xffffffffu, mine, n - 1) >> 32);
-    full = nth != 0;
-    last = full ? value_of(nth) : 0.f;
+    if (chunks <= 1) __syncthreads();              // (everybody knows the count)
+    if (warp == 0) {
+      buffer[lane] = mine;
+      if (lane == 0) *count = min(c, n);
+    }
+    __syncthreads();
+    const uint32_t im = (uint32_t)(buffer[n - 1] >> 32);
+    full = im != 0;                                // (what comes later has higher ids: equals are no candidates)
+    last = full ? value_of(im) : 0.f;
+    much = false;
+    __syncthreads();
   }
 };
 
@@ -172,27 +287,32 @@ __device__ __forceinline__ float peer_f32(uint32_t addr) {
   return v;
 }
 
-template <typename T, bool TOP>
-__global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const ScoreParams p) {
+template <typename T, bool TOP, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel(const ScoreParams p) {
+  constexpr int WARPS = THREADS / 32, BUFFER = Best<THREADS>::BUFFER;
   constexpr int VEC = 16 / sizeof(T), NV = E / VEC;               // logits of a load, loads at a time
-  __shared__ u64 s_list[WARPS][32];
+  __shared__ u64 s_list[TOP ? WARPS * 32 : 1], s_buffer[TOP ? BUFFER : 1];
   __shared__ Sums s_sums[WARPS];
+  __shared__ int s_count;
+  __shared__ uint32_t s_bounds[WARPS];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int row = blockIdx.x / p.ctas, rank = blockIdx.x - row * p.ctas;
   pdl_wait();
   pdl_trigger();
   const T *x0 = (const T *)p.logits + (int64_t)row * p.row_stride;
-  const int token = p.tokens && rank == 0 ? __ldg(p.tokens + row) : -1;
-  const float x_token = token >= 0 && token < p.vocab ? one(x0 + token) : -INFINITY;
+  const int token = p.tokens && rank == 0 ? p.tokens[row] : -1;
+  // Every load's address lies in the row; what was not to be read is masked afterwards.  (Guarding the load instead, with its value undefined
+  // otherwise, lets the compiler drop the guard.)
+  const bool known = token >= 0 && token < p.vocab;
+  const float x_token = known ? one(x0 + (known ? token : 0)) : -INFINITY;
   const int lead = min(p.vocab, (int)((16 - ((uintptr_t)x0 & 15)) & 15) / (int)sizeof(T));   // in front of the first whole 16 bytes
   const int vecs = (p.vocab - lead) / VEC, tail = p.vocab - lead - vecs * VEC;
   const int v_begin = (int)((int64_t)vecs * rank / p.ctas), v_end = (int)((int64_t)vecs * (rank + 1) / p.ctas);
   const uint4 *xv = (const uint4 *)(x0 + lead);
 
   Sums sum{-FLT_MAX, 0.f, 0.f};
-  Best best;
-  auto add = [&](const float *x, auto n_of, float top) {
-    constexpr int N = decltype(n_of)::value;
+  Best<THREADS> best{s_buffer, s_list, &s_count, s_bounds, 0.f, false, false, false};
+  auto grow = [&](float top) {                                     // the maximum covers top
     const float m = max_nan(sum.m, top);
     if (m != sum.m) {
       const float d = sum.m - m, f = ex2(d * LOG2E);
@@ -200,110 +320,167 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const ScorePara
       sum.z *= f;
       sum.m = m;
     }
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float d = x[i] - sum.m, e = ex2(d * LOG2E);
-      sum.z += e;
-      if (e > 0.f) sum.t = fmaf(d, e, sum.t);                      // (-inf: nothing)
-    }
   };
-  if (rank == 0 && warp == 0 && lead > 0) {                        // (at most 7)
-    const float x = lane < lead ? one(x0 + lane) : -INFINITY;
-    add(&x, std::integral_constant<int, 1>(), x);
-    if constexpr (TOP) best.offer<1>(&x, x, lane, 1, 0, lane < lead, p.n_top, lane);
-  }
-  uint4 raw[NV];
-  auto fetch = [&](int v0) {
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int v = v0 + j * THREADS + tid;
-      if (v < v_end) raw[j] = __ldg(xv + v);
-    }
+  auto add_one = [&](float x) {
+    grow(x);
+    const float d = x - sum.m, e = ex2(d * LOG2E);
+    sum.z += e;
+    if (e > 0.f) sum.t = fmaf(d, e, sum.t);                        // (-inf: nothing)
   };
-  fetch(v_begin);
-  for (int v0 = v_begin; v0 < v_end; v0 += NV * THREADS) {
-    float x[E];
-    unpack16<T>(raw, x);
-    uint32_t there = 0;
+  bool masked = false;                                             // this thread has met logits of -inf
+  auto add = [&](const float *x, float top) {
+    grow(top);
+    const u64 m2 = pair(-sum.m, -sum.m), l2 = pair(LOG2E, LOG2E);
+    u64 z2 = pair(sum.z, 0.f), t2 = pair(sum.t, 0.f);
+    if (!masked) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      if (v0 + j * THREADS + tid < v_end) {
-        there |= 1u << j;
-      } else {
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) x[j * VEC + i] = -INFINITY;
+      for (int i = 0; i < E; i += 2) {
+        const u64 d = add2(pair(x[i], x[i + 1]), m2);
+        float a, b;
+        unpair(mul2(d, l2), a, b);
+        const u64 e = pair(ex2(a), ex2(b));
+        z2 = add2(z2, e);
+        t2 = fma2(d, e, t2);
       }
     }
-    if (v0 + NV * THREADS < v_end) fetch(v0 + NV * THREADS);
-    float top = x[0];
+    float z0, z1, t0, t1;
+    unpair(t2, t0, t1);
+    if (masked || t0 + t1 != t0 + t1) {                            // -inf times 0 (or something that is no number, which Z shows)
+      masked = true;
+      z2 = pair(sum.z, 0.f);
+      t0 = sum.t;
+      t1 = 0.f;
 #pragma unroll
-    for (int i = 1; i < E; ++i) top = max_nan(top, x[i]);
-    add(x, std::integral_constant<int, E>(), top);
-    if constexpr (TOP) best.offer<E>(x, top, (uint32_t)lead + (uint32_t)(v0 + tid) * VEC, VEC, THREADS * VEC, there, p.n_top, lane);
-  }
-  if (rank == 0 && warp == 0 && tail > 0) {                        // (at most 7)
-    const int id = lead + vecs * VEC + lane;
-    const float x = lane < tail ? one(x0 + id) : -INFINITY;
-    add(&x, std::integral_constant<int, 1>(), x);
-    if constexpr (TOP) best.offer<1>(&x, x, id, 1, 0, lane < tail, p.n_top, lane);
+      for (int i = 0; i < E; i += 2) {
+        const u64 d = add2(pair(x[i], x[i + 1]), m2);
+        float a, b, d0, d1;
+        unpair(mul2(d, l2), a, b);
+        a = ex2(a);
+        b = ex2(b);
+        z2 = add2(z2, pair(a, b));
+        unpair(d, d0, d1);
+        if (a > 0.f) t0 = fmaf(d0, a, t0);
+        if (b > 0.f) t1 = fmaf(d1, b, t1);
+      }
+    }
+    unpair(z2, z0, z1);
+    sum.z = z0 + z1;
+    sum.t = t0 + t1;
+  };
+  for (int pass = 0; pass < 2; ++pass) {
+    const bool careful = pass > 0;                                 // the buffer is looked at after every batch
+    sum = Sums{-FLT_MAX, 0.f, 0.f};
+    if (TOP) {
+      best.full = best.much = best.over = false;
+      if (tid == 0) s_count = 0;
+      __syncthreads();
+    }
+    if (rank == 0 && warp == 0 && lead > 0) {                      // (at most 7)
+      const float x = lane < lead ? one(x0 + min(lane, lead - 1)) : -INFINITY;
+      add_one(x);
+      if constexpr (TOP) best.offer<1>(&x, x, lane, 1, 0, lane < lead, p.n_top, lane);
+    }
+    uint4 raw[NV];
+    auto fetch = [&](int v0) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        raw[j] = xv[min(v0 + j * THREADS + tid, v_end - 1)];
+      }
+    };
+    if (v_begin < v_end) fetch(v_begin);
+    int batch = 0, cut_at = 0;
+    for (int v0 = v_begin; v0 < v_end; v0 += NV * THREADS, ++batch) {
+      float x[E];
+      unpack16<T>(raw, x);
+      uint32_t there = (1u << NV) - 1;
+      if (v0 + NV * THREADS > v_end) {                             // the last batch
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+          if (v0 + j * THREADS + tid >= v_end) {
+            there &= ~(1u << j);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) x[j * VEC + i] = -INFINITY;
+          }
+      }
+      const bool more = v0 + NV * THREADS < v_end;
+      if (more) fetch(v0 + NV * THREADS);
+      float top = max_nan(max_nan(x[0], x[1]), x[2], x[3]);
+#pragma unroll
+      for (int i = 4; i < E; i += 4) top = max_nan(top, max_nan(x[i], x[i + 1]), max_nan(x[i + 2], x[i + 3]));
+      add(x, top);
+      if constexpr (TOP) {
+        const uint32_t id = (uint32_t)lead + (uint32_t)(v0 + tid) * VEC;
+        if (batch == 0) best.begin<E>(x, top, id, VEC, THREADS * VEC, there, p.n_top, warp, lane);
+        else best.offer<E>(x, top, id, VEC, THREADS * VEC, there, p.n_top, lane);
+        // (what is in the buffer then comes before what is offered later: ties go to the lower ids)
+        if (more) {
+          if (careful) {
+            if (__syncthreads_or(best.much || !best.full)) best.cut(p.n_top, warp, lane);
+          } else if (batch == cut_at) {
+            cut_at = GROWTH * cut_at + GROWTH - 1;
+            __syncthreads();
+            best.cut(p.n_top, warp, lane);
+          }
+        }
+      }
+    }
+    if (rank == 0 && warp == 0 && tail > 0) {                      // (at most 7)
+      const int id = lead + vecs * VEC + lane;
+      const float x = lane < tail ? one(x0 + min(id, p.vocab - 1)) : -INFINITY;
+      add_one(x);
+      if constexpr (TOP) best.offer<1>(&x, x, id, 1, 0, lane < tail, p.n_top, lane);
+    }
+    if (!TOP || careful) break;
+    if (!__syncthreads_or(best.over)) break;
   }
 
   // ---- the threads', the warps' and the CTAs' parts
+  auto reduce = [&](int lanes) {
 #pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    const Sums b{__shfl_xor_sync(0xffffffffu, sum.m, o), __shfl_xor_sync(0xffffffffu, sum.z, o), __shfl_xor_sync(0xffffffffu, sum.t, o)};
-    join(sum, b);
-  }
-  auto over_warps = [&](int many) {                                // afterwards in warp 0
-    if (lane == 0) s_sums[warp] = sum;
-    if (TOP) s_list[warp][lane] = best.mine;
-    __syncthreads();
-    if (warp == 0) {
-      sum = lane < many ? s_sums[lane] : Sums{-FLT_MAX, 0.f, 0.f};
-#pragma unroll
-      for (int o = WARPS / 2; o; o >>= 1) {
-        const Sums b{__shfl_xor_sync(0xffffffffu, sum.m, o), __shfl_xor_sync(0xffffffffu, sum.z, o), __shfl_xor_sync(0xffffffffu, sum.t, o)};
-        join(sum, b);
-      }
-      sum = Sums{__shfl_sync(0xffffffffu, sum.m, 0), __shfl_sync(0xffffffffu, sum.z, 0), __shfl_sync(0xffffffffu, sum.t, 0)};
-      if constexpr (TOP)
-        for (int w = 1; w < many; ++w) best.mine = merged(best.mine, s_list[w][lane], lane);
+    for (int o = 16; o; o >>= 1) {
+      if (o >= lanes) continue;
+      const Sums b{__shfl_xor_sync(0xffffffffu, sum.m, o), __shfl_xor_sync(0xffffffffu, sum.z, o), __shfl_xor_sync(0xffffffffu, sum.t, o)};
+      join(sum, b);
     }
   };
-  over_warps(WARPS);
+  reduce(32);
+  if (lane == 0) s_sums[warp] = sum;
+  __syncthreads();
+  if (TOP) best.cut(p.n_top, warp, lane);
+  u64 mine = TOP ? s_buffer[lane] : 0;
+  sum = s_sums[lane & (WARPS - 1)];
+  reduce(WARPS);                                                   // (every warp has the CTA's now)
   if (p.ctas > 1) {
     __syncthreads();
-    if (warp == 0) {
-      if (lane == 0) s_sums[0] = sum;
-      if (TOP) s_list[0][lane] = best.mine;
-    }
+    if (tid == 0) s_sums[0] = sum;
     cluster_barrier();
-    if (rank == 0) {
-      const bool on = warp < p.ctas;
-      if (on) {
-        const uint32_t a = of_rank(smem_u32(&s_sums[0]), warp), b = of_rank(smem_u32(&s_list[0][lane]), warp);
+    if (rank == 0 && warp == 0) {
+      sum = Sums{-FLT_MAX, 0.f, 0.f};
+      if (lane < p.ctas) {
+        const uint32_t a = of_rank(smem_u32(&s_sums[0]), lane);
         sum = Sums{peer_f32(a), peer_f32(a + 4), peer_f32(a + 8)};
-        if (TOP) best.mine = peer_u64(b);
       }
+      reduce(32);
+      if (TOP)
+        for (int i = 1; i < p.ctas; ++i) mine = merged(mine, peer_u64(of_rank(smem_u32(&s_buffer[lane]), i)), lane);
     }
     cluster_barrier();                                             // (everybody has been read)
     if (rank != 0) return;
-    over_warps(p.ctas);
   }
   if (warp != 0) return;
   const bool none = sum.z == 0.f;
   const float lnz = logf(sum.z);
   if (lane == 0) {
-    if (p.logprob) p.logprob[row] = none || x_token == -INFINITY ? (sum.z != sum.z && token >= 0 && token < p.vocab ? NAN : -INFINITY) : (x_token - sum.m) - lnz;
+    if (p.logprob) p.logprob[row] = none || x_token == -INFINITY ? (sum.z != sum.z && known ? NAN : -INFINITY) : (x_token - sum.m) - lnz;
     if (p.entropy) p.entropy[row] = none ? 0.f : lnz - sum.t / sum.z;
   }
   if (TOP && lane < p.n_top) {
-    p.top_ids[(int64_t)row * p.n_top + lane] = (int32_t)(0xffffffffu - (uint32_t)best.mine);
-    p.top_logprobs[(int64_t)row * p.n_top + lane] = none ? -INFINITY : (value_of((uint32_t)(best.mine >> 32)) - sum.m) - lnz;
+    p.top_ids[(int64_t)row * p.n_top + lane] = (int32_t)(0xffffffffu - (uint32_t)mine);
+    p.top_logprobs[(int64_t)row * p.n_top + lane] = none ? -INFINITY : (value_of((uint32_t)(mine >> 32)) - sum.m) - lnz;
   }
 }
 
-template <typename T>
+template <typename T, int THREADS>
 cudaError_t launch(const ScoreParams &p, int rows, cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)rows * p.ctas);
@@ -317,7 +494,7 @@ cudaError_t launch(const ScoreParams &p, int rows, cudaStream_t s) {
   at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = p.ctas > 1 ? 2 : 1;
-  return p.n_top > 0 ? cudaLaunchKernelEx(&cfg, token_logprobs_kernel<T, true>, p) : cudaLaunchKernelEx(&cfg, token_logprobs_kernel<T, false>, p);
+  return p.n_top > 0 ? cudaLaunchKernelEx(&cfg, token_logprobs_kernel<T, true, THREADS>, p) : cudaLaunchKernelEx(&cfg, token_logprobs_kernel<T, false, THREADS>, p);
 }
 
 }  // namespace
@@ -338,7 +515,13 @@ extern "C" int ouro_token_logprobs(const void *logits, int32_t dtype, int64_t ro
   if (!paged::device(&dev, &sms)) return paged::refuse(call, "no usable current device", OURO_ECUDA);
   ScoreParams p{logits, row_stride, tokens, logprob, entropy, top_ids, top_logprobs, vocab, n_top, 1};
   while (p.ctas < 8 && (int64_t)rows * p.ctas < 2 * sms && vocab / (2 * p.ctas) >= 2048) p.ctas *= 2;
-  const cudaError_t e = dtype == OURO_F32 ? launch<float>(p, rows, (cudaStream_t)stream) : launch<__nv_bfloat16>(p, rows, (cudaStream_t)stream);
+  // A row's fixed costs grow with its warps, its latency falls: 128 threads where there are rows enough for every SM, or where a row is one
+  // batch of 256.  (us with 256 / 128 threads, 20 alternatives: 512 rows of 32000 24.9 / 29.1, 700 35.9 / 40.9, 1000 42.7 / 41.7, 2048 of 64000
+  // 116.7 / 114.0; 5 alternatives: 2048 of 1024 25.3 / 13.4, 512 of 3000 8.8 / 7.8; one row of 130000 12.2 / 16.6.)
+  const bool few = rows < 6 * sms && vocab > 4096;
+  cudaError_t e;
+  if (dtype == OURO_F32) e = few ? launch<float, 256>(p, rows, (cudaStream_t)stream) : launch<float, 128>(p, rows, (cudaStream_t)stream);
+  else e = few ? launch<__nv_bfloat16, 256>(p, rows, (cudaStream_t)stream) : launch<__nv_bfloat16, 128>(p, rows, (cudaStream_t)stream);
   OURO_COUNT_LAUNCH();
   return e == cudaSuccess ? OURO_OK : paged::refuse(call, cudaGetErrorString(e), OURO_ECUDA);
 }

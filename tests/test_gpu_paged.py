@@ -514,6 +514,21 @@ def test_scores_equal_the_definition(rows, vocab, dtype, n, kind):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_scores_of_many_rows_that_go_on_rising(dtype):
+    """Whole rows in one CTA, whose every batch brings more candidates than the last; and rows of which all logits are equal."""
+    build.build()
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    x = torch.linspace(-20, 20, 100000, device=DEV).expand(300, 100000).clone()
+    x[1::3] = x[1::3].flip(1)
+    x[2::3] = 0.5
+    x = x.to(dt)
+    tokens = torch.arange(300, device=DEV, dtype=torch.int32) * 300
+    for n in (1, 32):
+        score_check(scores.token_logprobs(x, tokens, n), score_reference(x, tokens, n), n)
+
+
+@gpu
 def test_scores_where_there_is_no_distribution():
     build.build()
     x = torch.randn((4, 5000), device=DEV)
