@@ -27,8 +27,11 @@ using paged::MAX_CTAS;
 constexpr int WARPS = 4, THREADS = 32 * WARPS;
 constexpr int MAX_LIST = OURO_MAX_LIST;
 constexpr int ITEM_COST = 2;                        // what an item costs besides its units, in units
-constexpr int SNAP = 3;                             // units in front of or behind a cut for which it is not worth its join
-constexpr int MIN_RUN = 4;                          // units for which another CTA is
+// A unit takes a CTA about a microsecond alone (a chain of latencies), a join two and more.  us with runs from 1, 2, 4 units on, borders taken within
+// 0, 1, 3: one sequence of 700 keys (1.1B shape) 7.9, 9.4, 12.0; one of 1024 (70B shape) 9.4, 9.4, 13.2, of 4096 14.5, 13.3, 14.9; 60 ragged up to
+// 700 15.3, 14.2, 13.7; 16 of 512 15.1, 15.1, 13.7; one of 20000 with two kv heads 21.3, 21.2, 18.7; large calls the same.
+constexpr int SNAP = 1;                             // units in front of or behind a cut for which it is not worth its join
+constexpr int MIN_RUN = 2;                          // units for which another CTA is
 constexpr float GROWTH = 8.f;                       // (log2) a maximum may grow by this before sums are rescaled: they stay below 2^8 per key
 constexpr uint32_t SPIN_LIMIT = 1u << 22;
 
@@ -129,11 +132,12 @@ struct Cfg {
   static constexpr int HALF_STAGE = BF ? BOXES * BOX : KW * PITCH;
   static constexpr int STAGE = 2 * HALF_STAGE;
   static constexpr int STAGES = BF && D <= 64 ? 4 : 3;
-  static constexpr int CHUNK = 32;                  // pieces joined at a time
+  static constexpr int CHUNK = 512 / R;             // pieces joined at a time
   static constexpr int OFF_RING = 0;                                      // [warp][stage]
   static constexpr int OFF_Q = WARPS * STAGES * STAGE;                    // f32: [warp][R][D]
   static constexpr int OFF_ML = OFF_Q + (BF ? 0 : WARPS * R * D * 4);     // [warp][R][2]
   static constexpr int OFF_JOIN = OFF_ML + WARPS * R * 8;                // [CHUNK][R][2]
+  static_assert(CHUNK * R * 8 >= 5 * THREADS * 4, "the shares of a join fit there too");
   static constexpr int OFF_BAR = OFF_JOIN + CHUNK * R * 8;                // [warp][stage]
   static constexpr int OFF_MASK = OFF_BAR + WARPS * STAGES * 8;           // [warp][stage]
   static constexpr int OFF_LEN = OFF_MASK + WARPS * STAGES * 4;           // [n]
@@ -609,7 +613,7 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
       const int slot = first_tile == 0 ? 1 : 0;                    // pieces of a CTA: of an item it begins, of one it goes on with
       float *piece = p.pieces + ((int64_t)blockIdx.x * 2 + slot) * paged::ROW_TILE * D;
       float *mls = p.pieces + (int64_t)MAX_CTAS * 2 * paged::ROW_TILE * D;
-      constexpr int C4 = D / 4, EACH = (R * C4 + THREADS - 1) / THREADS;      // columns of four a row; of them a thread has at a time
+      constexpr int C4 = D / 4;
       auto finish = [&](int r, int col, float M, float L, const float *o) {       // four columns of a row to the output
         const int at = rt * R + r, tok = p.group_of.quot(at), head = kvh * p.group + at - tok * p.group;
         const int64_t row = ((int64_t)was.s * p.n_new + tok) * p.H + head;
@@ -657,49 +661,65 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
           __threadfence();
           float2 *s_join = (float2 *)(smem + C::OFF_JOIN);
           auto where = [&](int cta) { return ((int64_t)cta * 2 + (cta == c0 ? 1 : 0)) * paged::ROW_TILE; };
-          {
-            float M[EACH], L[EACH], o[EACH][4];
+          // Four columns of a row, EACH times a thread; where that leaves threads over, the pieces are dealt out to `shares` of them.
+          constexpr int EACH = (R * C4 + THREADS - 1) / THREADS;
+          const int E = rows * C4, shares = E < THREADS ? THREADS / E : 1, share = shares > 1 ? tid / E : 0;
+          int at[EACH];
+          float M[EACH], L[EACH], o[EACH][4];
+#pragma unroll
+          for (int k = 0; k < EACH; ++k) {
+            at[k] = min(k * THREADS + tid - share * E, E - 1);
+            M[k] = -INFINITY;
+            L[k] = o[k][0] = o[k][1] = o[k][2] = o[k][3] = 0.f;
+          }
+          for (int a0 = c0; a0 <= c1; a0 += C::CHUNK) {
+            const int many = min(C::CHUNK, c1 - a0 + 1);
+            for (int i = tid; i < many * R; i += THREADS)
+              if (i % R < rows) s_join[i] = __ldcg((const float2 *)(mls + (where(a0 + i / R) + i % R) * 2));
+            __syncthreads();
 #pragma unroll
             for (int k = 0; k < EACH; ++k) {
-              M[k] = -INFINITY;
-              L[k] = o[k][0] = o[k][1] = o[k][2] = o[k][3] = 0.f;
+              float mx = M[k];
+              for (int j = 0; j < many; ++j) mx = fmaxf(mx, s_join[j * R + at[k] / C4].x);
+              const float a = ex2(M[k] - base_of(mx));
+              M[k] = mx;
+              L[k] *= a;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) o[k][i] *= a;
             }
-            for (int a0 = c0; a0 <= c1; a0 += C::CHUNK) {
-              const int many = min(C::CHUNK, c1 - a0 + 1);
-              for (int i = tid; i < many * R; i += THREADS)
-                if (i % R < rows) s_join[i] = __ldcg((const float2 *)(mls + (where(a0 + i / R) + i % R) * 2));
-              __syncthreads();
+#pragma unroll(EACH > 2 ? 2 : 8 / EACH)
+            for (int j = share; j < many; j += shares) {
+              const float *piece_j = p.pieces + where(a0 + j) * D;
 #pragma unroll
               for (int k = 0; k < EACH; ++k) {
-                const int e = k * THREADS + tid, r = e / C4, col = (e - r * C4) * 4;
-                if (e >= rows * C4) break;
-                float mx = M[k];
-                for (int j = 0; j < many; ++j) mx = fmaxf(mx, s_join[j * R + r].x);
-                const float base = base_of(mx), a = ex2(M[k] - base);
-                M[k] = mx;
-                L[k] *= a;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) o[k][i] *= a;
-#pragma unroll 8
-                for (int j = 0; j < many; ++j) {
-                  const float4 y = __ldcg((const float4 *)(p.pieces + (where(a0 + j) + r) * D + col));
-                  const float2 ml = s_join[j * R + r];
-                  const float x = ex2(ml.x - base);
-                  L[k] = fmaf(x, ml.y, L[k]);
-                  o[k][0] = fmaf(x, y.x, o[k][0]);
-                  o[k][1] = fmaf(x, y.y, o[k][1]);
-                  o[k][2] = fmaf(x, y.z, o[k][2]);
-                  o[k][3] = fmaf(x, y.w, o[k][3]);
-                }
+                const float4 y = __ldcg((const float4 *)(piece_j + at[k] * 4));
+                const float2 ml = s_join[j * R + at[k] / C4];
+                const float x = ex2(ml.x - base_of(M[k]));
+                L[k] = fmaf(x, ml.y, L[k]);
+                o[k][0] = fmaf(x, y.x, o[k][0]);
+                o[k][1] = fmaf(x, y.y, o[k][1]);
+                o[k][2] = fmaf(x, y.z, o[k][2]);
+                o[k][3] = fmaf(x, y.w, o[k][3]);
               }
-              __syncthreads();
             }
-#pragma unroll
-            for (int k = 0; k < EACH; ++k) {
-              const int e = k * THREADS + tid, r = e / C4;
-              if (e < rows * C4) finish(r, (e - r * C4) * 4, M[k], L[k], o[k]);
-            }
+            __syncthreads();
           }
+          if (shares > 1) {                                        // (EACH is 1 or has one element, and all have the same M)
+            float *s_part = (float *)s_join;
+            s_part[tid] = L[0];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s_part[(i + 1) * THREADS + tid] = o[0][i];
+            __syncthreads();
+            if (share == 0)
+              for (int w = 1; w < shares; ++w) {
+                L[0] += s_part[w * E + tid];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[0][i] += s_part[(i + 1) * THREADS + w * E + tid];
+              }
+          }
+#pragma unroll
+          for (int k = 0; k < EACH; ++k)
+            if (share == 0 && k * THREADS + tid < E) finish(at[k] / C4, at[k] % C4 * 4, M[k], L[k], o[k]);
         }
       }
       if (run_ends) break;
