@@ -11,6 +11,8 @@ namespace paged {
 
 constexpr int MAX_CTAS = 444;        // of the attention kernel: three per SM at most
 constexpr int ROW_TILE = 16;         // query rows a CTA works on at a time at most
+constexpr int TC_CTAS = 160;         // the same for many query rows to a kv head: one per SM
+constexpr int TC_ROWS = 128;
 constexpr int TEXT_DIM = 128;        // largest head dim
 
 // Workspace: counters that are zero between calls, then what a call needs while it runs.
@@ -22,8 +24,9 @@ inline Layout layout(const ouro_paged_cache &c) {
   Layout l{};
   l.counters = 0;
   l.pieces = up256(MAX_CTAS * sizeof(int));
-  // attention: two pieces a CTA, each ROW_TILE rows of (maximum, sum, head_dim values)
-  const size_t pieces = (size_t)MAX_CTAS * 2 * ROW_TILE * (c.head_dim + 2) * sizeof(float);
+  // attention: two pieces a CTA, each a tile's rows of (maximum, sum, head_dim values)
+  const size_t rows_few = (size_t)MAX_CTAS * ROW_TILE, rows_many = (size_t)TC_CTAS * TC_ROWS;
+  const size_t pieces = 2 * (rows_few > rows_many ? rows_few : rows_many) * (c.head_dim + 2) * sizeof(float);
   // page calls: entries of the rows a fork rewrites; pairs of pages to copy and the pages' new ids
   l.staged = l.pieces;
   const size_t rows = c.max_seqs < OURO_MAX_LIST ? c.max_seqs : OURO_MAX_LIST;

@@ -6,7 +6,7 @@
 // few dozen operations a byte.  So the whole design is about reading every key and value once, without a pause, on all SMs:
 //  - The query rows that share a kv head (new tokens x query heads of its group) are row tiles of 8 or 16, a sequence's kv
 //    head and row tile an item, TILE keys of an item a unit.  All units of a call, in order, are dealt out to the CTAs in runs of the same
-//    cost whatever the lengths are (see Place).  An item that lies in one CTA is finished there; of an item cut between CTAs each leaves
+//    cost whatever the lengths are (paged_runs.cuh).  An item that lies in one CTA is finished there; of an item cut between CTAs each leaves
 //    a piece (maximum, sum, unnormalised output, in 32 bits), and the CTA that is last to do so joins the pieces in ascending order
 //    (so the result does not depend on who that is).
 //  - A warp fetches KW keys of every unit into its part of a ring in shared memory, STAGES - 1 units ahead, across the borders of items;
@@ -18,11 +18,13 @@
 // Keys that are not there (beyond the length, on no page) have probability 0, and zeros take their values' place.
 #include <cuda.h>
 
-#include "paged.h"
+#include "paged_runs.cuh"
 
 namespace {
 
+using paged::AttnParams;
 using paged::MAX_CTAS;
+using paged::Walk;
 
 constexpr int WARPS = 4, THREADS = 32 * WARPS;
 constexpr int MAX_LIST = OURO_MAX_LIST;
@@ -32,37 +34,13 @@ constexpr int ITEM_COST = 2;                        // what an item costs beside
 // 700 15.3, 14.2, 13.7; 16 of 512 15.1, 15.1, 13.7; one of 20000 with two kv heads 21.3, 21.2, 18.7; large calls the same.
 constexpr int SNAP = 1;                             // units in front of or behind a cut for which it is not worth its join
 constexpr int MIN_RUN = 2;                          // units for which another CTA is
+#ifndef MROWS
+#define MROWS 16
+#endif
+constexpr int MMA_ROWS = MROWS;                     // query rows of a kv head from which on they go to the other kernel
 constexpr float GROWTH = 8.f;                       // (log2) a maximum may grow by this before sums are rescaled: they stay below 2^8 per key
 constexpr uint32_t SPIN_LIMIT = 1u << 22;
 
-// Division of 0 .. 2^31 - 1 by a number that a call does not change: three instructions instead of some thirty, and it is done for every unit.
-struct Div {
-  uint32_t d, mul, shift;
-  void set(uint32_t x) {
-    d = x;
-    uint32_t bits = 0;
-    while (bits < 31 && (1u << bits) < x) ++bits;
-    // ceil(2^(31 + bits) / x) < 2^32, and its excess over the quotient is below 2^-31 of it
-    mul = x == 1 ? 0 : (uint32_t)((((uint64_t)1 << (31 + bits)) + x - 1) / x);
-    shift = bits ? bits - 1 : 0;
-  }
-  __device__ __forceinline__ int quot(int n) const { return mul ? (int)(__umulhi((uint32_t)n, mul) >> shift) : n; }
-};
-
-struct AttnParams {
-  const uint8_t *k, *v;                             // of the layer
-  const int32_t *table, *lens, *seqs;
-  const void *q;
-  void *out;
-  float *lse;
-  int *counters, *status;
-  float *pieces;                                    // [CTA][2][ROW_TILE][D], then [CTA][2][ROW_TILE][2]
-  int64_t page_bytes, slot_bytes, head_bytes, q_stride;
-  int n, n_new, H, Hkv, group, rows, row_tiles;     // rows = n_new * group
-  int n_pages, max_pages, max_seqs, cap, layer;
-  Div page, group_of;
-  float scale_log2;
-};
 // The pools as five dimensions (dim, head, row, page, layer); boxes of 64 dims x 16 rows.
 struct Maps {
   CUtensorMap k, v;
@@ -147,12 +125,6 @@ struct Cfg {
   static_assert(R * D * 4 <= STAGE && R <= paged::ROW_TILE, "a warp's output fits its stage");
 };
 
-// A place in the list of units: sequence, head, row tile, unit of the item; and what is known of the sequence.
-struct Walk {
-  int s, head, rt, tile, tiles, len;
-  const int32_t *row;
-};
-
 // TMA: the copy engine fetches (bf16, pages of a multiple of 16 rows).
 template <typename T, int D, int R, bool TMA>
 __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnParams p, const __grid_constant__ Maps maps) {
@@ -174,80 +146,11 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
   pdl_wait();
   pdl_trigger();
 
-  // ---- what the sequences cost, and this CTA's run
-  {
-    const int per = (p.n + THREADS - 1) / THREADS;
-    int sum = 0;
-    for (int i = tid * per; i < min(p.n, (tid + 1) * per); ++i) {
-      const int sid = p.seqs ? p.seqs[i] : i;
-      const bool known = sid >= 0 && sid < p.max_seqs;              // (here and below: addresses are valid whether or not the value is wanted)
-      const int len = known ? min(max(p.lens[known ? sid : 0], 0), p.cap) : 0;
-      s_len[i] = len;
-      sum += max(1, (len + C::TILE - 1) / C::TILE) + ITEM_COST;
-    }
-    int inc = sum;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int up = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += up;
-    }
-    if (lane == 31) s_misc[warp] = inc;
-    __syncthreads();
-    int at = inc - sum;
-    for (int w = 0; w < warp; ++w) at += s_misc[w];
-    for (int i = tid * per; i < min(p.n, (tid + 1) * per); ++i) {
-      s_cum[i] = at;
-      at += max(1, (s_len[i] + C::TILE - 1) / C::TILE) + ITEM_COST;
-    }
-    if (tid == THREADS - 1) s_cum[p.n] = at;
-    __syncthreads();
-  }
-  const int F = p.Hkv * p.row_tiles;                               // items of a sequence
-  const int64_t cost = (int64_t)s_cum[p.n] * F;
-  const int64_t G = min((int64_t)gridDim.x, max((int64_t)1, cost / MIN_RUN));
-  if (blockIdx.x >= G) return;
-  auto enter = [&](Walk &w) {
-    w.len = s_len[w.s];
-    w.tiles = s_cum[w.s + 1] - s_cum[w.s] - ITEM_COST;
-    const int sid = p.seqs ? p.seqs[w.s] : w.s;
-    w.row = p.table + (int64_t)(w.len > 0 ? sid : 0) * p.max_pages;
-  };
-  auto next = [&](Walk &w) {
-    if (++w.tile < w.tiles) return;
-    w.tile = 0;
-    if (++w.rt < p.row_tiles) return;
-    w.rt = 0;
-    if (++w.head < p.Hkv) return;
-    w.head = 0;
-    if (++w.s < p.n) enter(w);
-  };
-  // Where the c-th run begins: at equal cost; within SNAP units of an item's border at that border.
-  auto place = [&](int64_t c) {
-    const int64_t at = cost * c / G;
-    Walk w{p.n, 0, 0, 0, 0, 0, nullptr};
-    if (at >= cost) return w;
-    int lo = 0, hi = p.n - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) / 2;
-      if ((int64_t)s_cum[mid] * F <= at) lo = mid; else hi = mid - 1;
-    }
-    w.s = lo;
-    enter(w);
-    const int in = (int)(at - (int64_t)s_cum[lo] * F), each = w.tiles + ITEM_COST;   // fits: a sequence's cost is checked on the host
-    const int hr = in / each, tile = in - hr * each - ITEM_COST;
-    w.head = hr / p.row_tiles;
-    w.rt = hr - w.head * p.row_tiles;
-    w.tile = tile <= SNAP ? 0 : tile;
-    if (w.tile > 0 && w.tiles - tile <= SNAP) {
-      w.tile = w.tiles - 1;
-      next(w);
-    }
-    return w;
-  };
-  Walk c = place(blockIdx.x);                                      // the unit being worked on
-  const Walk end = place(blockIdx.x + 1);
-  auto at_end = [&](const Walk &w) { return w.tile == end.tile && w.rt == end.rt && w.head == end.head && w.s == end.s; };
-  if (at_end(c)) return;
+  const paged::Runs<C::TILE, ITEM_COST, SNAP, MIN_RUN> runs(p, gridDim.x, s_len, s_cum, s_misc, THREADS);
+  if (blockIdx.x >= runs.G) return;
+  Walk c = runs.place(blockIdx.x);                                 // the unit being worked on
+  const Walk end = runs.place(blockIdx.x + 1);
+  if (paged::same(c, end)) return;
 
   // ---- the warp's ring
   uint8_t *ring_p = smem + C::OFF_RING + warp * C::STAGES * C::STAGE;
@@ -321,8 +224,8 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
           }
         }
       }
-      next(f);
-      f_on = !at_end(f);
+      runs.next(f);
+      f_on = !paged::same(f, end);
       read_ids();
     }
     if constexpr (!TMA) asm volatile("cp.async.commit_group;" ::: "memory");
@@ -574,8 +477,8 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
     // ---- the item's or the run's end: the warps' parts are added up
     const Walk was = c;
     const bool item_ends = c.tile == c.tiles - 1;
-    next(c);
-    const bool run_ends = at_end(c);
+    runs.next(c);
+    const bool run_ends = paged::same(c, end);
     if (!item_ends && !run_ends) continue;
     {
       // The warp's part goes to the stage just read: [row][column], the columns of a row exchanged so that eight rows' stores hit different banks.
@@ -648,10 +551,8 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
         }
       }
       if (!whole) {
-        // The cuts inside the item, which are those that place() leaves there; c0 has its beginning, c1 its end.
-        const int64_t item0 = (int64_t)s_cum[was.s] * F + (int64_t)(was.head * p.row_tiles + was.rt) * (was.tiles + ITEM_COST) + ITEM_COST;
-        const int64_t lo = item0 + SNAP + 1, hi = item0 + was.tiles - SNAP - 1;
-        const int c0 = (int)((lo * G + cost - 1) / cost) - 1, c1 = (int)(((hi + 1) * G + cost - 1) / cost) - 1;
+        int c0, c1;
+        runs.owners(was, c0, c1);
         __threadfence();
         __syncthreads();
         if (tid == 0) s_misc[4] = atomicAdd(p.counters + c0, 1) == c1 - c0;
@@ -737,7 +638,9 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
 
 const char *CALL = "ouro_paged_attention";
 
-bool make_map(CUtensorMap *m, const ouro_paged_cache *c, const void *base) {
+}  // namespace
+
+bool paged::make_map(CUtensorMap *m, const ouro_paged_cache *c, const void *base, int box_rows) {
   typedef CUresult (*encode_fn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
                                 const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
   static encode_fn encode = nullptr;
@@ -752,10 +655,12 @@ bool make_map(CUtensorMap *m, const ouro_paged_cache *c, const void *base) {
   const int64_t st[4] = {c->head_stride, c->slot_stride, c->page_stride, c->layer_stride};
   cuuint64_t strides[4];
   for (int i = 0; i < 4; ++i) strides[i] = dims[i + 1] == 1 && st[i] == 0 ? (cuuint64_t)c->head_dim * 2 : (cuuint64_t)st[i] * 2;
-  const cuuint32_t box[5] = {64, 1, 16, 1, 1}, one[5] = {1, 1, 1, 1, 1};
+  const cuuint32_t box[5] = {64, 1, (cuuint32_t)box_rows, 1, 1}, one[5] = {1, 1, 1, 1, 1};
   return encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void *>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+
+namespace {
 
 template <typename T, int D, int R, bool TMA>
 int launch(const AttnParams &p, const Maps &maps, int64_t most_cost, cudaStream_t s) {
@@ -806,7 +711,7 @@ extern "C" int ouro_paged_attention(const ouro_paged_cache *c, int32_t layer, co
   const int tile = (c->dtype == OURO_F32 ? 8 : 16) * WARPS, rows_of = c->dtype == OURO_F32 || p.rows <= 8 ? 8 : 16;
   p.row_tiles = (p.rows + rows_of - 1) / rows_of;
   p.cap = c->max_pages * c->page_size;
-  const int64_t cost = ((int64_t)(p.cap + tile - 1) / tile + ITEM_COST) * c->n_kv_heads * p.row_tiles;
+  const int64_t cost = ((int64_t)(p.cap + tile - 1) / tile + 8) * c->n_kv_heads * p.row_tiles;   // (8: no kernel's item costs more)
   if (cost > INT32_MAX || cost / (c->n_kv_heads * p.row_tiles) * n > INT32_MAX) return paged::refuse(CALL, "the sequences' work is above 2^31 units");
   const paged::Layout l = paged::layout(*c);
   p.k = (const uint8_t *)c->k + (int64_t)layer * c->layer_stride * esize;
@@ -820,9 +725,11 @@ extern "C" int ouro_paged_attention(const ouro_paged_cache *c, int32_t layer, co
   p.page.set(c->page_size); p.group_of.set(p.group);
   p.n_pages = c->n_pages; p.max_pages = c->max_pages; p.max_seqs = c->max_seqs;
   p.scale_log2 = scale * 1.4426950408889634f;
+  int status = OURO_OK;
+  if (p.rows > MMA_ROWS && paged::attention_tc(c, p, (cudaStream_t)stream, &status)) return status;
   // The copy engine fetches 16 rows of a head at a time: where pages are multiples of that.
   Maps maps{};
-  const bool tma = c->dtype == OURO_BF16 && c->page_size % 16 == 0 && make_map(&maps.k, c, c->k) && make_map(&maps.v, c, c->v);
+  const bool tma = c->dtype == OURO_BF16 && c->page_size % 16 == 0 && paged::make_map(&maps.k, c, c->k, 16) && paged::make_map(&maps.v, c, c->v, 16);
   switch (c->head_dim) {
     case 32: return by_kind<32>(c, p, tma, maps, cost * n, (cudaStream_t)stream);
     case 64: return by_kind<64>(c, p, tma, maps, cost * n, (cudaStream_t)stream);

@@ -332,19 +332,57 @@ def test_one_token_and_three_dimensions():
 
 
 @gpu
-@pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_later_tokens_do_not_reach_earlier_ones(dtype):
+@pytest.mark.parametrize("layout,page,h,hkv,d,new,lens", [
+    ("rows", 16, 24, 1, 128, 1, [0, 1, 63, 64, 65, 1000]), ("heads", 48, 40, 8, 128, 5, [0, 1, 4, 5, 6, 64, 65, 700, 63, 129]), ("rows", 64, 64, 8, 128, 16, [3, 16, 17, 300, 2000]),
+    ("both", 32, 32, 4, 64, 8, [8, 7, 63, 64, 65, 500, 1, 0]), ("padded", 16, 71, 1, 64, 16, [15, 16, 200]), ("rows", 128, 32, 1, 128, 4, [5000]), ("rows", 16, 8, 1, 64, 9, [1, 9, 300, 10000]),
+    ("rows", 80, 18, 1, 128, 1, [4000, 1, 1, 64]), ("heads", 256, 56, 8, 128, 16, [777, 20])])
+def test_attention_of_many_query_rows(layout, page, h, hkv, d, new, lens):
+    """More than 16 query rows to a kv head: up to 128, with rows of several row tiles, and several boxes a page."""
+    build.build()
+    cache, table = filled(layout, page, hkv, d, torch.bfloat16, lens)
+    g = torch.Generator(device=DEV).manual_seed(2)
+    q = (2 * torch.randn((len(lens), new, h, d), device=DEV, generator=g)).to(torch.bfloat16)
+    for layer in (0, 1):
+        out, lse = cache.attend(layer, q, want_lse=True)
+        want, want_lse = reference(cache.k[layer], cache.v[layer], table, lens, range(len(lens)), q, d ** -0.5)
+        close(out, want, 5.5, torch.bfloat16)
+        some = torch.isfinite(want_lse)
+        assert torch.equal(some, torch.isfinite(lse)) and bool(((lse - want_lse)[some].abs() <= 1e-4).all())
+    assert torch.equal(cache.attend(1, q), out)
+    # scores that grow along the text, so that maxima do: every key's score larger than the last one's
+    n = max(lens)
+    ramp = torch.linspace(0, 40, n, device=DEV)
+    for s, x in enumerate(lens):
+        for j in range(0, x, max(1, x // 50)):
+            cache.k[0, int(table[s, j // page]), j % page] = (ramp[j] * torch.ones((hkv, d), device=DEV) / d ** 0.5).to(torch.bfloat16)
+    q = torch.ones_like(q)
+    want, _ = reference(cache.k[0], cache.v[0], table, lens, range(len(lens)), q, d ** -0.5)
+    close(cache.attend(0, q), want, 5.5, torch.bfloat16)
+    cache.check()
+
+
+@gpu
+@pytest.mark.parametrize("dtype,heads,d", [("f32", 8, 64), ("bf16", 8, 64), ("bf16", 20, 64), ("bf16", 64, 128)])
+def test_later_tokens_do_not_reach_earlier_ones(dtype, heads, d):
     """Keys and values of a later token that are not numbers are masked places for the earlier ones."""
     build.build()
     dt = torch.float32 if dtype == "f32" else torch.bfloat16
-    lens, new = [37, 64, 3, 66], 4
-    cache, table = filled("rows", 16, 2, 64, dt, lens)
-    q = torch.randn((4, new, 8, 64), device=DEV).to(dt)
+    lens, new = [37, 64, 3, 66, 400], 4
+    cache, table = filled("rows", 16, 2, d, dt, lens)
+    q = torch.randn((len(lens), new, heads, d), device=DEV).to(dt)
     want = cache.attend(0, q)
-    for s, x in enumerate(lens):
-        j = x - 1
-        cache.k[0, int(table[s, j // 16]), j % 16] = float("nan")
-        cache.v[0, int(table[s, j // 16]), j % 16] = float("inf")
+    at = [(int(table[s, (x - 1) // 16]), (x - 1) % 16) for s, x in enumerate(lens)]
+    keep = cache.v[0].clone()
+    for p, r in at:                                        # a single value: its column alone, for the last token alone
+        cache.v[0, p, r, :, 5] = float("inf")
+    got = cache.attend(0, q)
+    assert bool((got[:, -1, :, 5] == float("inf")).all())
+    got[:, -1, :, 5] = want[:, -1, :, 5]
+    assert torch.isfinite(got).all() and bool(((got - want).abs() <= 2 ** -7 * want.abs() + 2 ** -12).all())
+    cache.v[0].copy_(keep)
+    for p, r in at:
+        cache.k[0, p, r] = float("nan")
+        cache.v[0, p, r] = float("inf")
     got = cache.attend(0, q)
     assert torch.equal(got[:, :-1], want[:, :-1]) if dtype == "f32" else bool(((got - want)[:, :-1].abs() <= 2 ** -7 * want[:, :-1].abs() + 2 ** -12).all())
     assert not torch.isfinite(got[:, -1]).any()
