@@ -34,10 +34,10 @@ constexpr int ITEM_COST = 2;                        // what an item costs beside
 // 700 15.3, 14.2, 13.7; 16 of 512 15.1, 15.1, 13.7; one of 20000 with two kv heads 21.3, 21.2, 18.7; large calls the same.
 constexpr int SNAP = 1;                             // units in front of or behind a cut for which it is not worth its join
 constexpr int MIN_RUN = 2;                          // units for which another CTA is
-#ifndef MROWS
-#define MROWS 16
-#endif
-constexpr int MMA_ROWS = MROWS;                     // query rows of a kv head from which on they go to the other kernel
+// More query rows of a kv head go to paged_attention_tc.cu (head dims 64 and 128).  us here and there: 35 rows, 34B drafts 20.0 and 20.7, one sequence of 4096
+// 21.8 and 22.0; 40 rows, 64 ragged up to 300 42.0 and 30.0, 48 up to 12345 (70B shape) 471 and 228; 128 rows, 8 of 4096 153 and 50; 64 rows of head
+// dim 64, one sequence of 700 10.4 and 12.7.  At 16 rows: 16 of 1000 (70B) 23.4 and 34.1, of the 1.1B shape 13.0 and 22.3.
+constexpr int MMA_ROWS = 16;
 constexpr float GROWTH = 8.f;                       // (log2) a maximum may grow by this before sums are rescaled: they stay below 2^8 per key
 constexpr uint32_t SPIN_LIMIT = 1u << 22;
 

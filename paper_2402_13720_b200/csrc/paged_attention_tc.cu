@@ -8,7 +8,8 @@
 //                  P goes back to TMEM as two bf16 parts (P = hi + lo up to 2^-17, see paged_attention.cu), two buffers;
 //     O += P V     accumulates in TMEM over the units of an item.  It is rescaled only where a row's maximum grew by 2^8, so that nearly always
 //                  nothing waits for it; V is the MN-major operand and is never transposed.
-// (With Q and P in shared memory the contractions took 1500 cycles a unit, waiting for 8 KB of operands each.)
+// 48 sequences of the 70B shape, up to 12345 tokens, 5 new: 228 us for 171 us of keys and values (334 with Q and P in shared memory, where a contraction
+// waits for 8 KB of operands; 214 with units of 128 keys, which cost 96 sequences of 5 tokens 48 us instead of 34 and 34B drafts 23 instead of 21).
 // Warps 0-7 are the rows, warp 8 fetches (TMA straight from the pages, a box of 16, 32 or 64 rows of a page), warp 9 issues the contractions: the
 // scores of a unit before the P V of the one before it, so that the row threads always have scores to work on.  Warp 10 sees to the units at a
 // sequence's end before they are contracted.  Items, runs, pieces and their join are those of paged_attention.cu (paged_runs.cuh).
@@ -23,18 +24,11 @@ using paged::Walk;
 
 constexpr int ROW_WARPS = 8, ROW_THREADS = 32 * ROW_WARPS, THREADS = ROW_THREADS + 96;
 constexpr int KEYS = 64, HALF = KEYS / 2;          // of a unit, of a thread
-#ifndef IC
-#define IC 4
-#endif
-#ifndef SN
-#define SN 2
-#endif
-#ifndef MR
-#define MR 3
-#endif
-constexpr int ITEM_COST = IC;                       // what an item costs besides its units (queries, filling and draining the chain), in units
-constexpr int SNAP = SN;                            // units in front of or behind a cut for which it is not worth its join
-constexpr int MIN_RUN = MR;                         // units for which another CTA is
+// us with runs from 2 (borders taken within 1), 3 (2) and 5 units on: 34B drafts 20.1, 20.7, 21.5; 64 ragged up to 300 with 5 tokens (70B shape) 31.8, 30.0, 32.4;
+// one sequence of 300 (34B) 11.5, 10.6, 10.7; large calls the same.
+constexpr int ITEM_COST = 4;                       // what an item costs besides its units (filling and draining the chain), in units
+constexpr int SNAP = 2;                            // units in front of or behind a cut for which it is not worth its join
+constexpr int MIN_RUN = 3;                         // units for which another CTA is
 constexpr int R = 128;                             // query rows of a tile
 typedef paged::Runs<KEYS, ITEM_COST, SNAP, MIN_RUN> Share;
 constexpr float GROWTH = 8.f;                      // (log2) a maximum may grow by this before sums and outputs are rescaled
@@ -389,15 +383,11 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attention_tc_kernel(const At
       const int quarter = warp & 3, half = warp >> 2, r = quarter * 32 + lane;
       const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
       float *xs = (float *)(smem + C::OFF_X);
-      while (!paged::same(c, end)) {
-        const Walk item = c;
-        const int rt = c.rt, kvh = c.head, rows = min(R, p.rows - rt * R);
-        const bool on = quarter * 32 < rows, mine = r < rows;      // the warp has rows; this thread has one
-        const int at = rt * R + min(r, rows - 1), tok = p.group_of.quot(at), head = kvh * p.group + at - tok * p.group;
-        const int vis = c.len - p.n_new + 1 + tok;
-        const int64_t row = (int64_t)c.s * p.n_new + tok;
-        if (on) {
-          const uint4 *src = (const uint4 *)((const __nv_bfloat16 *)p.q + row * p.q_stride + (int64_t)head * D) + half * (D / 16);
+      // The queries of an item's rows, which it needs from its first unit on: brought as soon as the scores of the item before are done.
+      auto bring = [&](const Walk &w) {
+        const int n = min(R, p.rows - w.rt * R), at = w.rt * R + min(r, n - 1), tok = p.group_of.quot(at), head = w.head * p.group + at - tok * p.group;
+        if (quarter * 32 < n) {
+          const uint4 *src = (const uint4 *)((const __nv_bfloat16 *)p.q + ((int64_t)w.s * p.n_new + tok) * p.q_stride + (int64_t)head * D) + half * (D / 16);
 #pragma unroll
           for (int j = 0; j < D / 16; j += 4) {                    // 32 dims, 16 columns
             uint32_t w[16];
@@ -416,6 +406,15 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attention_tc_kernel(const At
         fence_before_sync();
         __syncwarp();
         if (lane == 0) mbar_arrive(&ms->q_full);
+      };
+      bring(c);
+      while (!paged::same(c, end)) {
+        const Walk item = c;
+        const int rt = c.rt, kvh = c.head, rows = min(R, p.rows - rt * R);
+        const bool on = quarter * 32 < rows, mine = r < rows;      // the warp has rows; this thread has one
+        const int at = rt * R + min(r, rows - 1), tok = p.group_of.quot(at), head = kvh * p.group + at - tok * p.group;
+        const int vis = c.len - p.n_new + 1 + tok;
+        const int64_t row = (int64_t)c.s * p.n_new + tok;
         float m = -INFINITY, l = 0.f;
         bool item_ends = false;
         for (bool first = true;; first = false) {
@@ -510,6 +509,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attention_tc_kernel(const At
           if (item_ends || paged::same(c, end)) break;
         }
         // ---- the item's or the run's end
+        if (!paged::same(c, end)) bring(c);
         warp_wait(&ms->pv_done[(u - 1) & 1], (u - 1) >> 1, ms, p.status);
         fence_after_sync();
         const bool whole = item_ends && item.tile == 0;
