@@ -109,7 +109,9 @@ struct Cfg {
   static constexpr int PITCH = D * 4 + 16;
   static constexpr int HALF_STAGE = BF ? BOXES * BOX : KW * PITCH;
   static constexpr int STAGE = 2 * HALF_STAGE;
-  static constexpr int STAGES = BF && D <= 64 ? 4 : 3;
+  // (f32: two CTAs on an SM with two stages, one with three: four sequences of 1024, 7B shape, 40 and 61 us)
+  static constexpr int STAGES = BF ? (D <= 64 ? 4 : 3) : 2;
+  static constexpr int KEY_LANES = D == 96 ? 1 : 128 / D;   // f32: keys whose values the lanes of a warp work on at a time
   static constexpr int CHUNK = 512 / R;             // pieces joined at a time
   static constexpr int OFF_RING = 0;                                      // [warp][stage]
   static constexpr int OFF_Q = WARPS * STAGES * STAGE;                    // f32: [warp][R][D]
@@ -456,18 +458,19 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
           s[r] = ex2(x - base_of(m[r]));
           l[r] += part == 0 ? s[r] : 0.f;
         }
-        const int col = min(lane, D / 4 - 1) * 4;                  // (lanes beyond the columns take part in the exchange below)
-        for (int j = 0; j < C::KW; ++j) {
+        const int kl = C::KEY_LANES > 1 ? lane / (D / 4) : 0, col = min(lane - kl * (D / 4), D / 4 - 1) * 4;   // (96: lanes beyond the columns take part in the exchange)
+        for (int j = kl; j < C::KW; j += C::KEY_LANES) {
           const float4 vv = *(const float4 *)(vp + j * C::PITCH + col * 4);
 #pragma unroll
           for (int r = 0; r < R; ++r) {
             if (r >= rows) break;
             const float pr = __shfl_sync(0xffffffffu, s[r], j * 4);
-            if (!((mask >> j & 1) && key0 + j < vis[r])) continue;   // (uniform: 0 times what is stored there would not be 0 for all values)
-            acc[4 * r] = fmaf(pr, vv.x, acc[4 * r]);
-            acc[4 * r + 1] = fmaf(pr, vv.y, acc[4 * r + 1]);
-            acc[4 * r + 2] = fmaf(pr, vv.z, acc[4 * r + 2]);
-            acc[4 * r + 3] = fmaf(pr, vv.w, acc[4 * r + 3]);
+            if ((mask >> j & 1) && key0 + j < vis[r]) {            // (0 times what is stored there would not be 0 for all values)
+              acc[4 * r] = fmaf(pr, vv.x, acc[4 * r]);
+              acc[4 * r + 1] = fmaf(pr, vv.y, acc[4 * r + 1]);
+              acc[4 * r + 2] = fmaf(pr, vv.z, acc[4 * r + 2]);
+              acc[4 * r + 3] = fmaf(pr, vv.w, acc[4 * r + 3]);
+            }
           }
         }
       }
@@ -507,6 +510,10 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
           x += __shfl_xor_sync(0xffffffffu, x, 4);
           x += __shfl_xor_sync(0xffffffffu, x, 8);
           x += __shfl_xor_sync(0xffffffffu, x, 16);
+#pragma unroll
+          for (int o = 16; o >= D / 4 && C::KEY_LANES > 1; o >>= 1)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[4 * r + i] += __shfl_xor_sync(0xffffffffu, acc[4 * r + i], o);
           if (lane < D / 4) *(float4 *)(part + r * D + ((lane * 4) ^ ((r & 3) * 8))) = make_float4(acc[4 * r], acc[4 * r + 1], acc[4 * r + 2], acc[4 * r + 3]);
           if (lane == 0) *(float2 *)(s_ml + (warp * R + r) * 2) = make_float2(m[r], x);
         }
