@@ -3,17 +3,19 @@
 //     m = max x,  Z = sum e^(x - m),  T = sum (x - m) e^(x - m)
 //     log p(t) = (x_t - m) - ln Z,    H = ln Z - T / Z
 //
-// Bound by HBM without alternatives (2048 rows of 64000 f32: 81 us, 6.5 TB/s); with them by what the warps have to issue (20: 114 us, of 67 %
-// of the issue slots; bf16, 5: 88 us for 40.6).  A row is a CTA's or, where rows are few, a cluster's, whose CTAs join through shared
+// Bound by HBM without alternatives (2048 rows of 64000 f32: 81 us, 6.5 TB/s); with them by what the warps have to issue (20: 103 us; bf16,
+// 5: 81 us for 40.6).  A row is a CTA's or, where rows are few, a cluster's, whose CTAs join through shared
 // memory: one launch, no workspace.
 //  - A thread keeps (m, Z, T) of what it has seen, in 32 bits, relative to its own maximum, sixteen logits at a time, two in an instruction.
 //  - Candidates for the best alternatives go to a buffer of the CTA as 64-bit keys (value in an order-preserving integer image, then the
-//    complement of the id: no two are equal, and the lowest id is first among equals).  After 1, 2, 4, .. batches of THREADS * E logits the
-//    buffer is cut down to the best n; in between only what is larger than the n-th gets in, n for every doubling on average, which
-//    the maximum of a thread's sixteen logits, needed for the sum anyway, mostly rules out for all of them.  In the first batch, k of each
-//    warp make n, so the smallest of the warps' k-th largest maxima bounds the n-th best of all from below; and where many lanes of a warp have
-//    something to offer later (in rows that ascend), so does the n-th largest of the lanes' maxima.  Rows that fill the buffer all the same are done
-//    again with a look at it after every batch.
+//    complement of the id: no two are equal, and the lowest id is first among equals).  After 1, 4, 16, .. batches of THREADS * E logits the
+//    buffer is cut down to the best n; in between only what is larger than the n-th counts, some 3 n for every cut on average, which the maximum
+//    of a thread's sixteen logits, needed for the sum anyway, mostly rules out for all of them.  Where it does not, the thread only notes where
+//    it is, so that the loop stays one comparison and no warp waits for its lane: the notes are followed before the next cut, by as many threads
+//    at once, from L2 (looked at in the loop: 114 us for 103).  In the first batch, k of each warp make n, so the smallest of the warps' k-th
+//    largest maxima bounds the n-th best of all from below.  Rows that fill the buffer or the notes all the same (they ascend) are done again
+//    for the alternatives alone, with a look at the buffer after every batch; there, where many lanes of a warp have something to offer, the
+//    n-th largest of the lanes' maxima bounds it too.
 #include "paged.h"
 #include "row_ops.cuh"
 
@@ -23,8 +25,9 @@ namespace {
 
 constexpr int E = 16;                              // logits of a thread at a time
 constexpr int CROWD = 8;                           // lanes with something to offer from which on the maxima are sorted first
-constexpr int GROWTH = 4;                          // the buffer is cut down after this many times as many batches as before
-constexpr int WATER = 256;                         // candidates at which the buffer is cut down where that is looked at; a batch adds THREADS * E at most
+constexpr int GROWTH = 4;                          // the buffer is cut down after this many times as many batches as before (2: 107 us for 103)
+constexpr int NOTES = 512;                         // threads' batches with something larger than the n-th, since the buffer was last cut down
+constexpr int WATER = 256;                         // candidates at which a row done again cuts the buffer down; a batch adds THREADS * E at most
 constexpr float LOG2E = 1.4426950408889634f;
 
 struct ScoreParams {
@@ -155,6 +158,7 @@ struct Best {
   u64 *buffer;                                     // [BUFFER]
   u64 *lists;                                      // [WARPS][32]
   int *count;
+  int *notes, *noted;                              // [NOTES] and their number
   uint32_t *bounds;                                // [WARPS]
   float last;                                      // value of the n-th of those that were there when the buffer was last cut down
   bool full;                                       // there were n
@@ -226,6 +230,35 @@ struct Best {
       push<N>(x, max(full ? image(last) + 1 : 1, nth(there ? image(top) : 0, n, lane)), base, per, far, there, lane);
     }
   }
+  // Between two cuts only where there is something is put down (the thread's first vector); the sixteen logits are looked at when it comes to the
+  // cut, by as many threads at once.
+  __device__ __forceinline__ void note(float top, int vector) {
+    if (!(top <= last)) {
+      const int at = atomicAdd(noted, 1);
+      if (at < NOTES) notes[at] = vector;
+      else over = true;
+    }
+  }
+  // The logits noted, behind a barrier and in front of one.
+  template <typename T>
+  __device__ __forceinline__ void look(const uint4 *xv, int v_end, int lead) {
+    constexpr int VEC = 16 / sizeof(T), NV = E / VEC;
+    for (int i = threadIdx.x; i < min(*noted, NOTES); i += THREADS) {
+      const int v = notes[i];
+      uint4 raw[NV];
+#pragma unroll
+      for (int j = 0; j < NV; ++j) raw[j] = xv[min(v + j * THREADS, v_end - 1)];
+      float x[E];
+      unpack16<T>(raw, x);
+#pragma unroll
+      for (int k = 0; k < E; ++k)
+        if (!(x[k] <= last) && v + k / VEC * THREADS < v_end) {
+          const int at = atomicAdd(count, 1);
+          if (at < BUFFER) buffer[at] = (u64)image(x[k]) << 32 | (0xffffffffu - (uint32_t)(lead + (v + k / VEC * THREADS) * VEC + k % VEC));
+          else over = true;
+        }
+    }
+  }
   // The first logits, all warps.
   template <int N>
   __device__ __forceinline__ void begin(const float *x, float top, uint32_t base, int per, uint32_t far, uint32_t there, int n, int warp, int lane) {
@@ -287,13 +320,15 @@ __device__ __forceinline__ float peer_f32(uint32_t addr) {
   return v;
 }
 
+// (128 threads: 7 CTAs of 72 registers on an SM, for 8 of 64 that spill in the loop: 103 us for 114.  256: 4, for 3 that leave 512 rows in two
+// rounds: 25 us for 31.)
 template <typename T, bool TOP, int THREADS>
-__global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel(const ScoreParams p) {
+__global__ void __launch_bounds__(THREADS, THREADS == 128 ? 7 : 4) token_logprobs_kernel(const ScoreParams p) {
   constexpr int WARPS = THREADS / 32, BUFFER = Best<THREADS>::BUFFER;
   constexpr int VEC = 16 / sizeof(T), NV = E / VEC;               // logits of a load, loads at a time
   __shared__ u64 s_list[TOP ? WARPS * 32 : 1], s_buffer[TOP ? BUFFER : 1];
   __shared__ Sums s_sums[WARPS];
-  __shared__ int s_count;
+  __shared__ int s_count, s_noted, s_notes[TOP ? NOTES : 1];
   __shared__ uint32_t s_bounds[WARPS];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int row = blockIdx.x / p.ctas, rank = blockIdx.x - row * p.ctas;
@@ -311,7 +346,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
   const uint4 *xv = (const uint4 *)(x0 + lead);
 
   Sums sum{-FLT_MAX, 0.f, 0.f};
-  Best<THREADS> best{s_buffer, s_list, &s_count, s_bounds, 0.f, false, false, false};
+  Best<THREADS> best{s_buffer, s_list, &s_count, s_notes, &s_noted, s_bounds, 0.f, false, false, false};
   auto grow = [&](float top) {                                     // the maximum covers top
     const float m = max_nan(sum.m, top);
     if (m != sum.m) {
@@ -367,71 +402,96 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
     sum.z = z0 + z1;
     sum.t = t0 + t1;
   };
-  for (int pass = 0; pass < 2; ++pass) {
-    const bool careful = pass > 0;                                 // the buffer is looked at after every batch
-    sum = Sums{-FLT_MAX, 0.f, 0.f};
-    if (TOP) {
-      best.full = best.much = best.over = false;
-      if (tid == 0) s_count = 0;
-      __syncthreads();
+  uint4 raw[NV];
+  auto fetch = [&](int v0) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) raw[j] = xv[min(v0 + j * THREADS + tid, v_end - 1)];
+  };
+  // The batch that has been fetched (-inf where the row ends), its largest and which of its vectors there are; the next one is asked for.
+  constexpr int STEP = NV * THREADS;
+  auto take = [&](int v0, float *x, float &top, uint32_t &there) {
+    unpack16<T>(raw, x);
+    there = (1u << NV) - 1;
+    if (v0 + STEP > v_end) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+        if (v0 + j * THREADS + tid >= v_end) {
+          there &= ~(1u << j);
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) x[j * VEC + i] = -INFINITY;
+        }
     }
-    if (rank == 0 && warp == 0 && lead > 0) {                      // (at most 7)
-      const float x = lane < lead ? one(x0 + min(lane, lead - 1)) : -INFINITY;
-      add_one(x);
-      if constexpr (TOP) best.offer<1>(&x, x, lane, 1, 0, lane < lead, p.n_top, lane);
+    if (v0 + STEP < v_end) fetch(v0 + STEP);
+    top = max_nan(max_nan(x[0], x[1]), x[2], x[3]);
+#pragma unroll
+    for (int i = 4; i < E; i += 4) top = max_nan(top, max_nan(x[i], x[i + 1]), max_nan(x[i + 2], x[i + 3]));
+  };
+  auto id_of = [&](int v0) { return (uint32_t)lead + (uint32_t)(v0 + tid) * VEC; };
+  // What is in front of the first and behind the last whole 16 bytes (at most 7 each).
+  auto ends = [&](bool front, bool sums) {
+    if (rank != 0 || warp != 0) return;
+    const int many = front ? lead : tail, id = front ? lane : lead + vecs * VEC + lane;
+    if (many == 0) return;
+    const float x = lane < many ? one(x0 + min(id, p.vocab - 1)) : -INFINITY;
+    if (sums) add_one(x);
+    if constexpr (TOP) best.template offer<1>(&x, x, id, 1, 0, lane < many, p.n_top, lane);
+  };
+  auto begin = [&]() {
+    best.full = best.much = best.over = false;
+    if (tid == 0) s_count = s_noted = 0;
+    __syncthreads();
+  };
+
+  if (TOP) begin();
+  ends(true, true);
+  if (v_begin < v_end) {
+    fetch(v_begin);
+    float x[E], top;
+    uint32_t there;
+    int v0 = v_begin, cut_at = v_begin + (GROWTH - 1) * STEP;      // the first logit of the batch behind which the next cut is
+    if constexpr (TOP) {
+      take(v0, x, top, there);
+      add(x, top);
+      best.template begin<E>(x, top, id_of(v0), VEC, THREADS * VEC, there, p.n_top, warp, lane);
+      v0 += STEP;
+      if (v0 < v_end) {
+        __syncthreads();
+        best.cut(p.n_top, warp, lane);
+      }
     }
-    uint4 raw[NV];
-    auto fetch = [&](int v0) {
-#pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        raw[j] = xv[min(v0 + j * THREADS + tid, v_end - 1)];
-      }
-    };
-    if (v_begin < v_end) fetch(v_begin);
-    int batch = 0, cut_at = 0;
-    for (int v0 = v_begin; v0 < v_end; v0 += NV * THREADS, ++batch) {
-      float x[E];
-      unpack16<T>(raw, x);
-      uint32_t there = (1u << NV) - 1;
-      if (v0 + NV * THREADS > v_end) {                             // the last batch
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-          if (v0 + j * THREADS + tid >= v_end) {
-            there &= ~(1u << j);
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) x[j * VEC + i] = -INFINITY;
-          }
-      }
-      const bool more = v0 + NV * THREADS < v_end;
-      if (more) fetch(v0 + NV * THREADS);
-      float top = max_nan(max_nan(x[0], x[1]), x[2], x[3]);
-#pragma unroll
-      for (int i = 4; i < E; i += 4) top = max_nan(top, max_nan(x[i], x[i + 1]), max_nan(x[i + 2], x[i + 3]));
+    for (; v0 < v_end; v0 += STEP) {
+      take(v0, x, top, there);
       add(x, top);
       if constexpr (TOP) {
-        const uint32_t id = (uint32_t)lead + (uint32_t)(v0 + tid) * VEC;
-        if (batch == 0) best.begin<E>(x, top, id, VEC, THREADS * VEC, there, p.n_top, warp, lane);
-        else best.offer<E>(x, top, id, VEC, THREADS * VEC, there, p.n_top, lane);
-        // (what is in the buffer then comes before what is offered later: ties go to the lower ids)
-        if (more) {
-          if (careful) {
-            if (__syncthreads_or(best.much || !best.full)) best.cut(p.n_top, warp, lane);
-          } else if (batch == cut_at) {
-            cut_at = GROWTH * cut_at + GROWTH - 1;
-            __syncthreads();
-            best.cut(p.n_top, warp, lane);
-          }
+        if (there) best.note(top, v0 + tid);
+        if (v0 == cut_at && v0 + STEP < v_end) {                   // (what is in the buffer then has lower ids than what is noted later: ties go to them)
+          cut_at = v_begin + GROWTH * (cut_at - v_begin) + (GROWTH - 1) * STEP;
+          __syncthreads();
+          best.template look<T>(xv, v_end, lead);
+          __syncthreads();
+          if (tid == 0) s_noted = 0;
+          best.cut(p.n_top, warp, lane);
         }
       }
     }
-    if (rank == 0 && warp == 0 && tail > 0) {                      // (at most 7)
-      const int id = lead + vecs * VEC + lane;
-      const float x = lane < tail ? one(x0 + min(id, p.vocab - 1)) : -INFINITY;
-      add_one(x);
-      if constexpr (TOP) best.offer<1>(&x, x, id, 1, 0, lane < tail, p.n_top, lane);
+  }
+  ends(false, true);
+  if constexpr (TOP) {
+    __syncthreads();
+    best.template look<T>(xv, v_end, lead);
+    if (__syncthreads_or(best.over)) {                             // the alternatives again, with a look at the buffer after every batch
+      begin();
+      ends(true, false);
+      if (v_begin < v_end) fetch(v_begin);
+      for (int v0 = v_begin; v0 < v_end; v0 += STEP) {
+        float x[E], top;
+        uint32_t there;
+        take(v0, x, top, there);
+        best.template offer<E>(x, top, id_of(v0), VEC, THREADS * VEC, there, p.n_top, lane);
+        if (__syncthreads_or(best.much || !best.full) && v0 + STEP < v_end) best.cut(p.n_top, warp, lane);
+      }
+      ends(false, false);
     }
-    if (!TOP || careful) break;
-    if (!__syncthreads_or(best.over)) break;
   }
 
   // ---- the threads', the warps' and the CTAs' parts
@@ -515,10 +575,10 @@ extern "C" int ouro_token_logprobs(const void *logits, int32_t dtype, int64_t ro
   if (!paged::device(&dev, &sms)) return paged::refuse(call, "no usable current device", OURO_ECUDA);
   ScoreParams p{logits, row_stride, tokens, logprob, entropy, top_ids, top_logprobs, vocab, n_top, 1};
   while (p.ctas < 8 && (int64_t)rows * p.ctas < 2 * sms && vocab / (2 * p.ctas) >= 2048) p.ctas *= 2;
-  // A row's fixed costs grow with its warps, its latency falls: 128 threads where there are rows enough for every SM, or where a row is one
-  // batch of 256.  (us with 256 / 128 threads, 20 alternatives: 512 rows of 32000 24.9 / 29.1, 700 35.9 / 40.9, 1000 42.7 / 41.7, 2048 of 64000
-  // 116.7 / 114.0; 5 alternatives: 2048 of 1024 25.3 / 13.4, 512 of 3000 8.8 / 7.8; one row of 130000 12.2 / 16.6.)
-  const bool few = rows < 6 * sms && vocab > 4096;
+  // A row's fixed costs grow with its warps, its latency falls: 128 threads where there are more rows than SMs hold of 256 threads' at once, or
+  // where a row is one batch of 256.  (us with 256 / 128 threads, 20 alternatives: 512 rows of 32000 25.1 / 24.9, as bf16 with 95 % masked 21.7 /
+  // 20.8, 700 38.8 / 29.9, 512 rows that ascend 172 / 209; 5 alternatives: 2048 rows of 1024 25.3 / 13.4; one row of 130000 12.2 / 16.6.)
+  const bool few = rows <= 4 * sms && vocab > 4096;
   cudaError_t e;
   if (dtype == OURO_F32) e = few ? launch<float, 256>(p, rows, (cudaStream_t)stream) : launch<float, 128>(p, rows, (cudaStream_t)stream);
   else e = few ? launch<__nv_bfloat16, 256>(p, rows, (cudaStream_t)stream) : launch<__nv_bfloat16, 128>(p, rows, (cudaStream_t)stream);
