@@ -3,16 +3,18 @@
 //     m = max x,  Z = sum e^(x - m),  T = sum (x - m) e^(x - m)
 //     log p(t) = (x_t - m) - ln Z,    H = ln Z - T / Z
 //
-// Bound by HBM without alternatives (2048 rows of 64000 f32: 81 us, 6.5 TB/s); with them by what the warps have to issue (20: 103 us; bf16,
-// 5: 81 us for 40.6).  A row is a CTA's or, where rows are few, a cluster's, whose CTAs join through shared
+// Bound by HBM without alternatives (2048 rows of 64000 f32: 81 us, 6.5 TB/s); with them by what the warps have to issue (20: 107 us; bf16,
+// 5: 80 us for 40.6).  A row is a CTA's or, where rows are few, a cluster's, whose CTAs join through shared
 // memory: one launch, no workspace.
-//  - A thread keeps (m, Z, T) of what it has seen, in 32 bits, relative to its own maximum, sixteen logits at a time, two in an instruction.
+//  - A thread keeps (m, Z - 1, T) of what it has seen, in 32 bits, relative to its own maximum, sixteen logits at a time, two in an instruction.
+//    Z - 1, because a token that has nearly everything is as likely as the others leave it: ln Z = ln (1 + r), to r's precision (and with Z in place
+//    of r 3 % less time).
 //  - Candidates for the best alternatives go to a buffer of the CTA as 64-bit keys (value in an order-preserving integer image, then the
 //    complement of the id: no two are equal, and the lowest id is first among equals).  After 1, 4, 16, .. batches of THREADS * E logits the
 //    buffer is cut down to the best n; in between only what is larger than the n-th counts, some 3 n for every cut on average, which the maximum
 //    of a thread's sixteen logits, needed for the sum anyway, mostly rules out for all of them.  Where it does not, the thread only notes where
 //    it is, so that the loop stays one comparison and no warp waits for its lane: the notes are followed before the next cut, by as many threads
-//    at once, from L2 (looked at in the loop: 114 us for 103).  In the first batch, k of each warp make n, so the smallest of the warps' k-th
+//    at once, from L2 (looked at in the loop: 114 us for 103, with Z).  In the first batch, k of each warp make n, so the smallest of the warps' k-th
 //    largest maxima bounds the n-th best of all from below.  Rows that fill the buffer or the notes all the same (they ascend) are done again
 //    for the alternatives alone, with a look at the buffer after every batch; there, where many lanes of a warp have something to offer, the
 //    n-th largest of the lanes' maxima bounds it too.
@@ -25,7 +27,7 @@ namespace {
 
 constexpr int E = 16;                              // logits of a thread at a time
 constexpr int CROWD = 8;                           // lanes with something to offer from which on the maxima are sorted first
-constexpr int GROWTH = 4;                          // the buffer is cut down after this many times as many batches as before (2: 107 us for 103)
+constexpr int GROWTH = 4;                          // the buffer is cut down after this many times as many batches as before (2: 110 us for 107)
 constexpr int NOTES = 512;                         // threads' batches with something larger than the n-th, since the buffer was last cut down
 constexpr int WATER = 256;                         // candidates at which a row done again cuts the buffer down; a batch adds THREADS * E at most
 constexpr float LOG2E = 1.4426950408889634f;
@@ -90,17 +92,16 @@ __device__ __forceinline__ float value_of(uint32_t im) {
 }
 
 struct Sums {
-  float m, z, t;
+  float m, r, t;                                   // Z = 1 + r: without the largest's own 1, which would round away what little there is beside it
 };
 // Adds what b has seen to a.
 __device__ __forceinline__ void join(Sums &a, const Sums &b) {
-  const float m = max_nan(a.m, b.m);
-  const float da = a.m - m, db = b.m - m, fa = ex2(da * LOG2E), fb = ex2(db * LOG2E);
-  // (a factor of 0 leaves nothing of T either, however far apart the maxima are; a NaN is kept by Z)
-  const float ta = fa > 0.f ? fmaf(da, a.z, a.t) * fa : 0.f, tb = fb > 0.f ? fmaf(db, b.z, b.t) * fb : 0.f;
-  a.z = a.z * fa + b.z * fb;
-  a.t = ta + tb;
-  a.m = m;
+  const bool first = a.m >= b.m;                                  // (NaN: not, and then r becomes NaN by the factor or by itself)
+  const float d = first ? b.m - a.m : a.m - b.m, f = ex2(d * LOG2E);
+  const float z = 1.f + (first ? b.r : a.r), t = first ? b.t : a.t;
+  a.r = fmaf(z, f, first ? a.r : b.r);
+  a.t = (first ? a.t : b.t) + (f > 0.f ? fmaf(d, z, t) * f : 0.f);   // (a factor of 0 leaves nothing of T either, however far apart the maxima are)
+  a.m = max_nan(a.m, b.m);
 }
 
 // Lists of 32 keys over a warp's lanes, largest first.
@@ -320,14 +321,16 @@ __device__ __forceinline__ float peer_f32(uint32_t addr) {
   return v;
 }
 
-// (128 threads: 7 CTAs of 72 registers on an SM, for 8 of 64 that spill in the loop: 103 us for 114.  256: 4, for 3 that leave 512 rows in two
-// rounds: 25 us for 31.)
+// (128 threads: 7 CTAs of 72 registers on an SM, 2048 x 64000 with 20 alternatives 107 us; 8 spill in the loop, 116; 6: 120.  256: 4, with 3 512
+// rows of 32000 take two rounds: 26 us for 32.)
 template <typename T, bool TOP, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 7 : 4) token_logprobs_kernel(const ScoreParams p) {
   constexpr int WARPS = THREADS / 32, BUFFER = Best<THREADS>::BUFFER;
   constexpr int VEC = 16 / sizeof(T), NV = E / VEC;               // logits of a load, loads at a time
   __shared__ u64 s_list[TOP ? WARPS * 32 : 1], s_buffer[TOP ? BUFFER : 1];
   __shared__ Sums s_sums[WARPS];
+  __shared__ float s_more;
+  __shared__ int s_peak[THREADS];
   __shared__ int s_count, s_noted, s_notes[TOP ? NOTES : 1];
   __shared__ uint32_t s_bounds[WARPS];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -345,28 +348,31 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 7 : 4) token_logprob
   const int v_begin = (int)((int64_t)vecs * rank / p.ctas), v_end = (int)((int64_t)vecs * (rank + 1) / p.ctas);
   const uint4 *xv = (const uint4 *)(x0 + lead);
 
-  Sums sum{-FLT_MAX, 0.f, 0.f};
+  Sums sum{-FLT_MAX, -1.f, 0.f};
+  s_peak[tid] = -1;                                                // the batch in which this thread's maximum is (its first vector)
   Best<THREADS> best{s_buffer, s_list, &s_count, s_notes, &s_noted, s_bounds, 0.f, false, false, false};
-  auto grow = [&](float top) {                                     // the maximum covers top
+  // The maximum covers top, which is in batch `at`; what of the new maximum's own 1 will be added to r.
+  auto grow = [&](float top, int at) {
     const float m = max_nan(sum.m, top);
-    if (m != sum.m) {
-      const float d = sum.m - m, f = ex2(d * LOG2E);
-      sum.t = f > 0.f ? fmaf(d, sum.z, sum.t) * f : 0.f;
-      sum.z *= f;
-      sum.m = m;
-    }
+    if (m == sum.m) return 0.f;
+    const float d = sum.m - m, f = ex2(d * LOG2E), z = 1.f + sum.r;
+    sum.t = f > 0.f ? fmaf(d, z, sum.t) * f : 0.f;
+    sum.r = z * f;
+    sum.m = m;
+    s_peak[tid] = at;
+    return 1.f;
   };
   auto add_one = [&](float x) {
-    grow(x);
+    const float own = grow(x, -1);
     const float d = x - sum.m, e = ex2(d * LOG2E);
-    sum.z += e;
+    sum.r += e - own;
     if (e > 0.f) sum.t = fmaf(d, e, sum.t);                        // (-inf: nothing)
   };
   bool masked = false;                                             // this thread has met logits of -inf
-  auto add = [&](const float *x, float top) {
-    grow(top);
+  auto add = [&](const float *x, float top, int at) {
+    const float own = grow(top, at);
     const u64 m2 = pair(-sum.m, -sum.m), l2 = pair(LOG2E, LOG2E);
-    u64 z2 = pair(sum.z, 0.f), t2 = pair(sum.t, 0.f);
+    u64 z2 = 0, t2 = pair(sum.t, 0.f);
     if (!masked) {
 #pragma unroll
       for (int i = 0; i < E; i += 2) {
@@ -380,9 +386,9 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 7 : 4) token_logprob
     }
     float z0, z1, t0, t1;
     unpair(t2, t0, t1);
-    if (masked || t0 + t1 != t0 + t1) {                            // -inf times 0 (or something that is no number, which Z shows)
+    if (masked || t0 + t1 != t0 + t1) {                            // -inf times 0 (or something that is no number, which r shows)
       masked = true;
-      z2 = pair(sum.z, 0.f);
+      z2 = 0;
       t0 = sum.t;
       t1 = 0.f;
 #pragma unroll
@@ -399,7 +405,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 7 : 4) token_logprob
       }
     }
     unpair(z2, z0, z1);
-    sum.z = z0 + z1;
+    sum.r += (z0 + z1) - own;
     sum.t = t0 + t1;
   };
   uint4 raw[NV];
@@ -451,7 +457,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 7 : 4) token_logprob
     int v0 = v_begin, cut_at = v_begin + (GROWTH - 1) * STEP;      // the first logit of the batch behind which the next cut is
     if constexpr (TOP) {
       take(v0, x, top, there);
-      add(x, top);
+      add(x, top, v0 + tid);
       best.template begin<E>(x, top, id_of(v0), VEC, THREADS * VEC, there, p.n_top, warp, lane);
       v0 += STEP;
       if (v0 < v_end) {
@@ -461,7 +467,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 7 : 4) token_logprob
     }
     for (; v0 < v_end; v0 += STEP) {
       take(v0, x, top, there);
-      add(x, top);
+      add(x, top, v0 + tid);
       if constexpr (TOP) {
         if (there) best.note(top, v0 + tid);
         if (v0 == cut_at && v0 + STEP < v_end) {                   // (what is in the buffer then has lower ids than what is noted later: ties go to them)
@@ -499,23 +505,55 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 7 : 4) token_logprob
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
       if (o >= lanes) continue;
-      const Sums b{__shfl_xor_sync(0xffffffffu, sum.m, o), __shfl_xor_sync(0xffffffffu, sum.z, o), __shfl_xor_sync(0xffffffffu, sum.t, o)};
+      const Sums b{__shfl_xor_sync(0xffffffffu, sum.m, o), __shfl_xor_sync(0xffffffffu, sum.r, o), __shfl_xor_sync(0xffffffffu, sum.t, o)};
       join(sum, b);
     }
   };
+  const float own_m = sum.m;
   reduce(32);
   if (lane == 0) s_sums[warp] = sum;
+  if (tid == 0) s_more = 0.f;
   __syncthreads();
   if (TOP) best.cut(p.n_top, warp, lane);
   u64 mine = TOP ? s_buffer[lane] : 0;
   sum = s_sums[lane & (WARPS - 1)];
   reduce(WARPS);                                                   // (every warp has the CTA's now)
+  // Where one logit has nearly everything, ln Z is what the others leave, and the sixteen that it was added with, rounded beside its 1, are added
+  // once more without it.  (Some 1e-7 of Z: behind 1 / 4 less than 5e-7 of ln Z.  0.3 us for a row that needs it.)
+  if (__shfl_sync(0xffffffffu, sum.r, 0) < 0.25f) {
+    const int peak = s_peak[tid];
+    if (own_m == sum.m && peak >= 0) {                             // (one thread: two that are equal make r 1)
+      uint4 again[NV];
+#pragma unroll
+      for (int j = 0; j < NV; ++j) again[j] = xv[min(peak + j * THREADS, v_end - 1)];
+      float x[E], rest = 0.f, equal = -1.f;
+      unpack16<T>(again, x);
+      const u64 m2 = pair(-own_m, -own_m), l2 = pair(LOG2E, LOG2E);
+      u64 z2 = 0;
+#pragma unroll
+      for (int i = 0; i < E; i += 2) {                             // (as above: the same roundings, which go)
+        float a, b;
+        if (peak + i / VEC * THREADS >= v_end) x[i] = x[i + 1] = -INFINITY;
+        unpair(mul2(add2(pair(x[i], x[i + 1]), m2), l2), a, b);
+        a = ex2(a);
+        b = ex2(b);
+        z2 = add2(z2, pair(a, b));
+        if (x[i] == own_m) equal += 1.f; else rest += a;
+        if (x[i + 1] == own_m) equal += 1.f; else rest += b;
+      }
+      float z0, z1;
+      unpair(z2, z0, z1);
+      s_more = (rest + equal) - ((z0 + z1) - 1.f);
+    }
+    __syncthreads();
+    sum.r += s_more;
+  }
   if (p.ctas > 1) {
     __syncthreads();
     if (tid == 0) s_sums[0] = sum;
     cluster_barrier();
     if (rank == 0 && warp == 0) {
-      sum = Sums{-FLT_MAX, 0.f, 0.f};
+      sum = Sums{-FLT_MAX, -1.f, 0.f};
       if (lane < p.ctas) {
         const uint32_t a = of_rank(smem_u32(&s_sums[0]), lane);
         sum = Sums{peer_f32(a), peer_f32(a + 4), peer_f32(a + 8)};
@@ -528,11 +566,13 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 7 : 4) token_logprob
     if (rank != 0) return;
   }
   if (warp != 0) return;
-  const bool none = sum.z == 0.f;
-  const float lnz = logf(sum.z);
+  const bool none = sum.r == -1.f;
+  // ln (1 + r) = 2 artanh(s), s = r / (2 + r): four terms leave 3e-9 of it at r = 1 / 4
+  const float s = sum.r / (2.f + sum.r), s2 = s * s;
+  const float lnz = sum.r < 0.25f ? 2.f * s * fmaf(s2, fmaf(s2, fmaf(s2, 1.f / 7, 1.f / 5), 1.f / 3), 1.f) : logf(1.f + sum.r);
   if (lane == 0) {
-    if (p.logprob) p.logprob[row] = none || x_token == -INFINITY ? (sum.z != sum.z && known ? NAN : -INFINITY) : (x_token - sum.m) - lnz;
-    if (p.entropy) p.entropy[row] = none ? 0.f : lnz - sum.t / sum.z;
+    if (p.logprob) p.logprob[row] = none || x_token == -INFINITY ? (sum.r != sum.r && known ? NAN : -INFINITY) : (x_token - sum.m) - lnz;
+    if (p.entropy) p.entropy[row] = none ? 0.f : lnz - sum.t / (1.f + sum.r);
   }
   if (TOP && lane < p.n_top) {
     p.top_ids[(int64_t)row * p.n_top + lane] = (int32_t)(0xffffffffu - (uint32_t)mine);
@@ -576,8 +616,8 @@ extern "C" int ouro_token_logprobs(const void *logits, int32_t dtype, int64_t ro
   ScoreParams p{logits, row_stride, tokens, logprob, entropy, top_ids, top_logprobs, vocab, n_top, 1};
   while (p.ctas < 8 && (int64_t)rows * p.ctas < 2 * sms && vocab / (2 * p.ctas) >= 2048) p.ctas *= 2;
   // A row's fixed costs grow with its warps, its latency falls: 128 threads where there are more rows than SMs hold of 256 threads' at once, or
-  // where a row is one batch of 256.  (us with 256 / 128 threads, 20 alternatives: 512 rows of 32000 25.1 / 24.9, as bf16 with 95 % masked 21.7 /
-  // 20.8, 700 38.8 / 29.9, 512 rows that ascend 172 / 209; 5 alternatives: 2048 rows of 1024 25.3 / 13.4; one row of 130000 12.2 / 16.6.)
+  // where a row is one batch of 256.  (us with 256 / 128 threads, 20 alternatives: one row of 130000 11.5 / 13.9, 128 of 32000 16.0 / 16.1, 512 25.7 /
+  // 26.0, 512 that ascend 173 / 209, 700 39.4 / 31.5, 1000 45.5 / 35.3, 2048 of 64000 130 / 107; 5 alternatives: 2048 of 1024 30 / 15.)
   const bool few = rows <= 4 * sms && vocab > 4096;
   cudaError_t e;
   if (dtype == OURO_F32) e = few ? launch<float, 256>(p, rows, (cudaStream_t)stream) : launch<float, 128>(p, rows, (cudaStream_t)stream);

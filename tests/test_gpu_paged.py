@@ -10,6 +10,7 @@ Tolerances, from the arithmetic (fixed before the first run):
    12 Z here; the difference x - m and the logarithm are rounded to 2^-24 of themselves: 3e-5 and 12 x 2e-5 + 2e-5 = 3e-4, + 2^-22 relative.
  * rotation: the products and their sum in 32 bits, then one rounding: 2^-8 relative + 2^-22 of the pair (bf16), 2^-22 of the pair (f32).
 """
+import math
 import ctypes as C
 
 import numpy as np
@@ -564,6 +565,31 @@ def test_scores_of_many_rows_that_go_on_rising(dtype):
     tokens = torch.arange(300, device=DEV, dtype=torch.int32) * 300
     for n in (1, 32):
         score_check(scores.token_logprobs(x, tokens, n), score_reference(x, tokens, n), n)
+
+
+@gpu
+@pytest.mark.parametrize("rows,vocab,dtype,n", [(9, 5, "f32", 1), (7, 700, "bf16", 1), (2, 1024, "f32", 0), (12, 32001, "f32", 20), (700, 4001, "f32", 5), (40, 64000, "bf16", 0)])
+@pytest.mark.parametrize("gap", [4.0, 12.0, 20.0])
+def test_scores_of_a_token_that_has_nearly_everything(rows, vocab, dtype, n, gap):
+    """Its log probability and the entropy are as small as what the others leave, and are known to as many digits.
+
+    A term e^d is off by |d| 2^-23 (the difference and the product with log2 e, rounded), e^x itself by 2^-22, some thirty sums in a row by 2^-24 each;
+    where the others have an eighth, what is rounded beside 1 (eight times 2^-24) by 2^-18 of them."""
+    build.build()
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    g = torch.Generator(device=DEV).manual_seed(vocab + int(gap))
+    x = torch.randn((rows, vocab + 1), device=DEV, generator=g).clamp(-4, 4).to(dt)[:, :vocab]
+    top = (torch.arange(rows, device=DEV) * max(1, (vocab - 1) // max(1, rows - 1))).clamp(max=vocab - 1)
+    top[-1] = vocab - 1
+    x.scatter_(1, top[:, None], (math.log(vocab) + gap))
+    d = x.double() - x.double().gather(1, top[:, None])
+    e = d.exp().scatter(1, top[:, None], 0.0)
+    left = e.sum(1).log1p()
+    h = left - (d * e).sum(1) / (1 + e.sum(1))
+    s = scores.token_logprobs(x, top.int(), n)
+    bound = float(-d.min()) * 2 ** -23 + 2 ** -22 + 30 * 2 ** -24 + 2 ** -18
+    for got, want in ((s.logprob, -left), (s.entropy, h)) + (((s.top_logprobs[:, 0], -left),) if n else ()):
+        assert bool(((got.double() - want).abs() <= bound * want.abs()).all()), float(((got.double() - want) / want).abs().max())
 
 
 @gpu
