@@ -347,7 +347,10 @@ struct CopyParams {
   int32_t *slots, *positions;
 };
 constexpr int COPY_THREADS = 256, UNROLL = 8;
-constexpr int CHUNK = 32 * UNROLL * 4;             // 16-byte pieces a warp takes at a time: 16 KB
+constexpr int CHUNK = 32 * UNROLL;                 // 16-byte pieces a warp takes at a time: 4 KB (beam step of 12 sequences 12.9 us, 16 KB: 13.4)
+// CTAs of an SM, 4 at a time: who is done early takes another, so that the last bytes are not left to a few.  us with 4, 16, 32, 64: 70 pages of
+// 32 layers (587 MB) 211, 201, 200, 199, 20 pages 73, 69, 69, 71, none 11.0, 12.5, 15.0, 19.9; extending 64 sequences of the 70B shape 59, 55, 55, 56.
+constexpr int COPY_CTAS = 16;
 
 // WHOLE: heads and rows of a page lie side by side (its rows are one piece of memory); COMPACT: whole pages, and the table follows.
 template <bool WHOLE, bool COMPACT>
@@ -391,27 +394,27 @@ __global__ void __launch_bounds__(COPY_THREADS) copy_kernel(const CacheDev c, co
     const int lk = (int)(rem % (2 * p.layers)), mv = (int)(rem / (2 * p.layers));
     const int src = p.lists.src[mv], dst = p.lists.dst[mv];
     const int pieces = (COMPACT ? c.page : p.lists.aux[mv]) * per_row;
+    if (chunk * CHUNK >= pieces) continue;
     uint8_t *base = (lk & 1 ? p.v : p.k) + (int64_t)(lk >> 1) * p.layer_bytes;
     const uint8_t *from = base + (int64_t)src * p.page_bytes;
     uint8_t *to = base + (int64_t)dst * p.page_bytes;
-    for (int e0 = chunk * CHUNK; e0 < min(pieces, (chunk + 1) * CHUNK); e0 += 32 * UNROLL) {
-      uint4 x[UNROLL];
-      int64_t off[UNROLL];
+    const int e0 = chunk * CHUNK + lane;
+    uint4 x[UNROLL];
+    int64_t off[UNROLL];
 #pragma unroll
-      for (int j = 0; j < UNROLL; ++j) {
-        const int e = min(e0 + j * 32 + lane, pieces - 1);         // (always a valid address; stored only where it is meant)
-        if (WHOLE) {
-          off[j] = (int64_t)e * 16;
-        } else {
-          const int row = e / per_row, in = e - row * per_row, head = in / p.row_pieces;
-          off[j] = row * p.slot_bytes + head * p.head_bytes + (int64_t)(in - head * p.row_pieces) * 16;
-        }
-        x[j] = __ldcs((const uint4 *)(from + off[j]));
+    for (int j = 0; j < UNROLL; ++j) {
+      const int e = min(e0 + j * 32, pieces - 1);                  // (always a valid address; stored only where it is meant)
+      if (WHOLE) {
+        off[j] = (int64_t)e * 16;
+      } else {
+        const int row = e / per_row, in = e - row * per_row, head = in / p.row_pieces;
+        off[j] = row * p.slot_bytes + head * p.head_bytes + (int64_t)(in - head * p.row_pieces) * 16;
       }
-#pragma unroll
-      for (int j = 0; j < UNROLL; ++j)
-        if (e0 + j * 32 + lane < pieces) __stcs((uint4 *)(to + off[j]), x[j]);
+      x[j] = __ldcs((const uint4 *)(from + off[j]));
     }
+#pragma unroll
+    for (int j = 0; j < UNROLL; ++j)
+      if (e0 + j * 32 < pieces) __stcs((uint4 *)(to + off[j]), x[j]);
   }
 }
 
@@ -425,7 +428,7 @@ int launch_copy(const char *call, const ouro_paged_cache *c, CopyParams p, bool 
   p.layers = c->n_layers; p.Hkv = c->n_kv_heads; p.row_pieces = c->head_dim * e / 16;
   const bool whole = c->head_stride == c->head_dim && c->slot_stride == (int64_t)c->n_kv_heads * c->head_dim;
   const int64_t ctas = (most_tasks + COPY_THREADS / 32 - 1) / (COPY_THREADS / 32);
-  const dim3 grid((unsigned)(ctas < 1 ? 1 : ctas < 4 * sms ? ctas : 4 * sms));
+  const dim3 grid((unsigned)(ctas < 1 ? 1 : ctas < COPY_CTAS * sms ? ctas : COPY_CTAS * sms));
   cudaError_t r;
   if (compact) r = launch_pdl(whole ? copy_kernel<true, true> : copy_kernel<false, true>, grid, dim3(COPY_THREADS), 0, s, dev_of(c), p);
   else r = launch_pdl(whole ? copy_kernel<true, false> : copy_kernel<false, false>, grid, dim3(COPY_THREADS), 0, s, dev_of(c), p);
