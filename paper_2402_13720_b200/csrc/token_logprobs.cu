@@ -3,8 +3,8 @@
 //     m = max x,  Z = sum e^(x - m),  T = sum (x - m) e^(x - m)
 //     log p(t) = (x_t - m) - ln Z,    H = ln Z - T / Z
 //
-// Bound by HBM without alternatives (2048 rows of 64000 f32: 81 us, 6.5 TB/s); with them by what the warps have to issue (20: 107 us; bf16,
-// 5: 80 us for 40.6).  A row is a CTA's or, where rows are few, a cluster's, whose CTAs join through shared
+// Bound by HBM without alternatives (2048 rows of 64000 f32: 81 us, 6.5 TB/s); with them by what the warps have to issue (20: 96 us; bf16,
+// 5: 82 us for 40.6).  A row is a CTA's or, where rows are few, a cluster's, whose CTAs join through shared
 // memory: one launch, no workspace.
 //  - A thread keeps (m, Z - 1, T) of what it has seen, in 32 bits, relative to its own maximum, sixteen logits at a time, two in an instruction.
 //    Z - 1, because a token that has nearly everything is as likely as the others leave it: ln Z = ln (1 + r), to r's precision (and with Z in place
@@ -14,7 +14,7 @@
 //    buffer is cut down to the best n; in between only what is larger than the n-th counts, some 3 n for every cut on average, which the maximum
 //    of a thread's sixteen logits, needed for the sum anyway, mostly rules out for all of them.  Where it does not, the thread only notes where
 //    it is, so that the loop stays one comparison and no warp waits for its lane: the notes are followed before the next cut, by as many threads
-//    at once, from L2 (looked at in the loop: 114 us for 103, with Z).  In the first batch, k of each warp make n, so the smallest of the warps' k-th
+//    at once, from L2 (looked at in the loop: 114 us for 103, both with Z and loads through registers).  In the first batch, k of each warp make n, so the smallest of the warps' k-th
 //    largest maxima bounds the n-th best of all from below.  Rows that fill the buffer or the notes all the same (they ascend) are done again
 //    for the alternatives alone, with a look at the buffer after every batch; there, where many lanes of a warp have something to offer, the
 //    n-th largest of the lanes' maxima bounds it too.
@@ -27,8 +27,9 @@ namespace {
 
 constexpr int E = 16;                              // logits of a thread at a time
 constexpr int CROWD = 8;                           // lanes with something to offer from which on the maxima are sorted first
-constexpr int GROWTH = 4;                          // the buffer is cut down after this many times as many batches as before (2: 110 us for 107)
-constexpr int NOTES = 512;                         // threads' batches with something larger than the n-th, since the buffer was last cut down
+constexpr int GROWTH = 4;                          // the buffer is cut down after this many times as many batches as before (2: 4 % more time)
+constexpr int SMALL = 512;                         // candidates of a CTA of 128 threads while the ring is in use
+constexpr int NOTES = 256;                         // threads' batches with something larger than the n-th, since the buffer was last cut down
 constexpr int WATER = 256;                         // candidates at which a row done again cuts the buffer down; a batch adds THREADS * E at most
 constexpr float LOG2E = 1.4426950408889634f;
 
@@ -156,7 +157,8 @@ template <int THREADS>
 struct Best {
   static constexpr int WARPS = THREADS / 32;
   static constexpr int BUFFER = WATER + THREADS * E + 32;          // (in front of the first and behind the last whole 16 bytes there are 7 at most)
-  u64 *buffer;                                     // [BUFFER]
+  u64 *buffer;                                     // [room], at last [BUFFER]
+  int room;
   u64 *lists;                                      // [WARPS][32]
   int *count;
   int *notes, *noted;                              // [NOTES] and their number
@@ -179,11 +181,11 @@ struct Best {
   }
   // All lanes' logits from bound on: x[i] has id base + i % per + (i / per) * far, if bit i / per of there is set.
   template <int N>
-  __device__ __forceinline__ void push(const float *x, uint32_t bound, uint32_t base, int per, uint32_t far, uint32_t there, int lane) {
+  __device__ __forceinline__ void push(const float *x, uint32_t bound, uint32_t base, int per, uint32_t far, uint32_t there, int lane, uint32_t all = 0) {
     uint32_t take = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      if (image(x[i]) >= bound && (there >> (i / per) & 1)) take |= 1u << i;
+      if ((image(x[i]) >= bound || (all >> i & 1)) && (there >> (i / per) & 1)) take |= 1u << i;
     const int mine = __popc(take);                 // places in the buffer: one request for the warp
     int at = mine;
 #pragma unroll
@@ -195,7 +197,7 @@ struct Best {
     if (lane == 31 && at > 0) first = atomicAdd(count, at);
     at += __shfl_sync(0xffffffffu, first, 31) - mine;
     much |= take != 0 && at + mine > WATER;
-    if (at + mine > BUFFER) over = true, take = 0;
+    if (at + mine > room) over = true, take = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i)
       if (take >> i & 1) buffer[at++] = (u64)image(x[i]) << 32 | (0xffffffffu - (base + i % per + (uint32_t)(i / per) * far));
@@ -220,7 +222,7 @@ struct Best {
               if (!(x[i] <= last) && (there >> (i / per) & 1)) {
                 const int at = atomicAdd(count, 1);
                 much |= at >= WATER;
-                if (at < BUFFER) buffer[at] = (u64)image(x[i]) << 32 | (0xffffffffu - (base + i % per + (uint32_t)(i / per) * far));
+                if (at < room) buffer[at] = (u64)image(x[i]) << 32 | (0xffffffffu - (base + i % per + (uint32_t)(i / per) * far));
                 else over = true;
               }
           }
@@ -255,7 +257,7 @@ struct Best {
       for (int k = 0; k < E; ++k)
         if (!(x[k] <= last) && v + k / VEC * THREADS < v_end) {
           const int at = atomicAdd(count, 1);
-          if (at < BUFFER) buffer[at] = (u64)image(x[k]) << 32 | (0xffffffffu - (uint32_t)(lead + (v + k / VEC * THREADS) * VEC + k % VEC));
+          if (at < room) buffer[at] = (u64)image(x[k]) << 32 | (0xffffffffu - (uint32_t)(lead + (v + k / VEC * THREADS) * VEC + k % VEC));
           else over = true;
         }
     }
@@ -269,11 +271,13 @@ struct Best {
     uint32_t b = bounds[0];
 #pragma unroll
     for (int w = 1; w < WARPS; ++w) b = min(b, bounds[w]);
-    push<N>(x, max(b, 1u), base, per, far, there, lane);
+    // Where so much is masked that the bound is -inf: of that only the first of the batch, which are the ones with the lowest ids.
+    const bool low = b <= image(-INFINITY);
+    push<N>(x, low ? image(-INFINITY) + 1 : b, base, per, far, there, lane, low && warp == 0 ? (1u << per) - 1 : 0);
   }
   // The best 32 to the buffer's beginning, in order.  All threads, behind a barrier.
   __device__ __forceinline__ void cut(int n, int warp, int lane) {
-    const int c = min(*count, BUFFER), chunks = (c + 31) / 32;
+    const int c = min(*count, room), chunks = (c + 31) / 32;
     u64 mine = 0;
     for (int i = warp; i < chunks; i += WARPS) {
       const u64 x = sorted(i * 32 + lane < c ? buffer[i * 32 + lane] : 0, lane);
@@ -321,13 +325,20 @@ __device__ __forceinline__ float peer_f32(uint32_t addr) {
   return v;
 }
 
-// (128 threads: 7 CTAs of 72 registers on an SM, 2048 x 64000 with 20 alternatives 107 us; 8 spill in the loop, 116; 6: 120.  256: 4, with 3 512
-// rows of 32000 take two rounds: 26 us for 32.)
+// (128 threads: 7 CTAs of 72 registers on an SM, 2048 x 64000 with 20 alternatives 96 us; 8 spill in the loop, 104; 6: 106.  256: 4, with 3 512
+// rows of 32000 take two rounds: 23 us for 32.)
 template <typename T, bool TOP, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 7 : 4) token_logprobs_kernel(const ScoreParams p) {
   constexpr int WARPS = THREADS / 32, BUFFER = Best<THREADS>::BUFFER;
   constexpr int VEC = 16 / sizeof(T), NV = E / VEC;               // logits of a load, loads at a time
-  __shared__ u64 s_list[TOP ? WARPS * 32 : 1], s_buffer[TOP ? BUFFER : 1];
+  // Batches on their way: each thread copies its own vectors and waits for its own, so that no barrier stands between, and a cut keeps no load
+  // waiting.  (us with 1, 2, 3 of 128 threads: 2048 x 64000 f32, 20 alternatives 102, 96, 101, without 82, 80, 85; through registers 107 and 81.  With
+  // 1, 2 of 256 threads: one row of 130000 11.2, 11.3, 512 of 32000 22.9, 23.8.)
+  constexpr int STAGES = THREADS == 128 ? 2 : 1, RING = STAGES * NV * THREADS * 16;
+  // The ring, and behind it the candidates; a row that is done again has all of it for its candidates.
+  constexpr int POOL = !TOP ? RING : RING + SMALL * 8 > BUFFER * 8 ? RING + SMALL * 8 : BUFFER * 8;
+  __shared__ __align__(16) uint8_t s_pool[POOL];
+  __shared__ u64 s_list[TOP ? WARPS * 32 : 1];
   __shared__ Sums s_sums[WARPS];
   __shared__ float s_more;
   __shared__ int s_peak[THREADS];
@@ -350,7 +361,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 7 : 4) token_logprob
 
   Sums sum{-FLT_MAX, -1.f, 0.f};
   s_peak[tid] = -1;                                                // the batch in which this thread's maximum is (its first vector)
-  Best<THREADS> best{s_buffer, s_list, &s_count, s_notes, &s_noted, s_bounds, 0.f, false, false, false};
+  Best<THREADS> best{(u64 *)(s_pool + RING), (POOL - RING) / 8, s_list, &s_count, s_notes, &s_noted, s_bounds, 0.f, false, false, false};
   // The maximum covers top, which is in batch `at`; what of the new maximum's own 1 will be added to r.
   auto grow = [&](float top, int at) {
     const float m = max_nan(sum.m, top);
@@ -408,14 +419,19 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 7 : 4) token_logprob
     sum.r += (z0 + z1) - own;
     sum.t = t0 + t1;
   };
-  uint4 raw[NV];
-  auto fetch = [&](int v0) {
-#pragma unroll
-    for (int j = 0; j < NV; ++j) raw[j] = xv[min(v0 + j * THREADS + tid, v_end - 1)];
-  };
-  // The batch that has been fetched (-inf where the row ends), its largest and which of its vectors there are; the next one is asked for.
   constexpr int STEP = NV * THREADS;
-  auto take = [&](int v0, float *x, float &top, uint32_t &there) {
+  const uint32_t ring = smem_u32(s_pool) + tid * 16;
+  int stage = 0;
+  auto fetch = [&](int v0, int st) {
+    if (v0 < v_end) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring + (st * NV + j) * THREADS * 16), "l"(xv + min(v0 + j * THREADS + tid, v_end - 1)) : "memory");
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  // The logits in raw (-inf where the row ends), their largest and which of the vectors there are.
+  auto have = [&](const uint4 *raw, int v0, float *x, float &top, uint32_t &there) {
     unpack16<T>(raw, x);
     there = (1u << NV) - 1;
     if (v0 + STEP > v_end) {
@@ -427,10 +443,22 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 7 : 4) token_logprob
           for (int i = 0; i < VEC; ++i) x[j * VEC + i] = -INFINITY;
         }
     }
-    if (v0 + STEP < v_end) fetch(v0 + STEP);
     top = max_nan(max_nan(x[0], x[1]), x[2], x[3]);
 #pragma unroll
     for (int i = 4; i < E; i += 4) top = max_nan(top, max_nan(x[i], x[i + 1]), max_nan(x[i + 2], x[i + 3]));
+  };
+  auto take = [&](int v0, float *x, float &top, uint32_t &there) {  // the next batch of the ring; another is asked for in its place
+    asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
+    uint4 raw[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(raw[j].x), "=r"(raw[j].y), "=r"(raw[j].z), "=r"(raw[j].w)
+                   : "r"(ring + (stage * NV + j) * THREADS * 16)
+                   : "memory");
+    have(raw, v0, x, top, there);
+    fetch(v0 + STAGES * STEP, stage);
+    stage = stage == STAGES - 1 ? 0 : stage + 1;
   };
   auto id_of = [&](int v0) { return (uint32_t)lead + (uint32_t)(v0 + tid) * VEC; };
   // What is in front of the first and behind the last whole 16 bytes (at most 7 each).
@@ -451,7 +479,8 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 7 : 4) token_logprob
   if (TOP) begin();
   ends(true, true);
   if (v_begin < v_end) {
-    fetch(v_begin);
+#pragma unroll
+    for (int i = 0; i < STAGES; ++i) fetch(v_begin + i * STEP, i);
     float x[E], top;
     uint32_t there;
     int v0 = v_begin, cut_at = v_begin + (GROWTH - 1) * STEP;      // the first logit of the batch behind which the next cut is
@@ -486,13 +515,17 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 7 : 4) token_logprob
     __syncthreads();
     best.template look<T>(xv, v_end, lead);
     if (__syncthreads_or(best.over)) {                             // the alternatives again, with a look at the buffer after every batch
+      best.buffer = (u64 *)s_pool;
+      best.room = BUFFER;
       begin();
       ends(true, false);
-      if (v_begin < v_end) fetch(v_begin);
       for (int v0 = v_begin; v0 < v_end; v0 += STEP) {
         float x[E], top;
         uint32_t there;
-        take(v0, x, top, there);
+        uint4 raw[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) raw[j] = xv[min(v0 + j * THREADS + tid, v_end - 1)];
+        have(raw, v0, x, top, there);
         best.template offer<E>(x, top, id_of(v0), VEC, THREADS * VEC, there, p.n_top, lane);
         if (__syncthreads_or(best.much || !best.full) && v0 + STEP < v_end) best.cut(p.n_top, warp, lane);
       }
@@ -515,7 +548,8 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 7 : 4) token_logprob
   if (tid == 0) s_more = 0.f;
   __syncthreads();
   if (TOP) best.cut(p.n_top, warp, lane);
-  u64 mine = TOP ? s_buffer[lane] : 0;
+  u64 mine = TOP ? best.buffer[lane] : 0;
+  if (TOP && p.ctas > 1 && warp == 0) s_list[lane] = mine;
   sum = s_sums[lane & (WARPS - 1)];
   reduce(WARPS);                                                   // (every warp has the CTA's now)
   // Where one logit has nearly everything, ln Z is what the others leave, and the sixteen that it was added with, rounded beside its 1, are added
@@ -560,7 +594,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 7 : 4) token_logprob
       }
       reduce(32);
       if (TOP)
-        for (int i = 1; i < p.ctas; ++i) mine = merged(mine, peer_u64(of_rank(smem_u32(&s_buffer[lane]), i)), lane);
+        for (int i = 1; i < p.ctas; ++i) mine = merged(mine, peer_u64(of_rank(smem_u32(&s_list[lane]), i)), lane);
     }
     cluster_barrier();                                             // (everybody has been read)
     if (rank != 0) return;
@@ -616,8 +650,8 @@ extern "C" int ouro_token_logprobs(const void *logits, int32_t dtype, int64_t ro
   ScoreParams p{logits, row_stride, tokens, logprob, entropy, top_ids, top_logprobs, vocab, n_top, 1};
   while (p.ctas < 8 && (int64_t)rows * p.ctas < 2 * sms && vocab / (2 * p.ctas) >= 2048) p.ctas *= 2;
   // A row's fixed costs grow with its warps, its latency falls: 128 threads where there are more rows than SMs hold of 256 threads' at once, or
-  // where a row is one batch of 256.  (us with 256 / 128 threads, 20 alternatives: one row of 130000 11.5 / 13.9, 128 of 32000 16.0 / 16.1, 512 25.7 /
-  // 26.0, 512 that ascend 173 / 209, 700 39.4 / 31.5, 1000 45.5 / 35.3, 2048 of 64000 130 / 107; 5 alternatives: 2048 of 1024 30 / 15.)
+  // where a row is one batch of 256.  (us with 256 / 128 threads, 20 alternatives: one row of 130000 11.2 / 14.1, 128 of 32000 14.3 / 15.4, 512 23.2 /
+  // 22.6, 512 that ascend 158 / 188, 700 35 / 29, 1000 41 / 31, 2048 of 64000 117 / 96; 5 alternatives: 2048 of 1024 28 / 15.)
   const bool few = rows <= 4 * sms && vocab > 4096;
   cudaError_t e;
   if (dtype == OURO_F32) e = few ? launch<float, 256>(p, rows, (cudaStream_t)stream) : launch<float, 128>(p, rows, (cudaStream_t)stream);

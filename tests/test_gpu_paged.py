@@ -553,6 +553,23 @@ def test_scores_equal_the_definition(rows, vocab, dtype, n, kind):
 
 
 @gpu
+@pytest.mark.parametrize("rows,vocab,dtype,n", [(1, 32000, "f32", 20), (5, 32001, "bf16", 32), (600, 16000, "f32", 20), (700, 9001, "bf16", 5), (3, 3000, "f32", 32)])
+@pytest.mark.parametrize("left", [0.003, 0.02, 0.0005])
+def test_scores_of_rows_where_little_is_left(rows, vocab, dtype, n, left):
+    """Constrained decoding: nearly everything is masked; the masked tokens with the lowest ids stand behind what is left, where that is less than n."""
+    build.build()
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    g = torch.Generator(device=DEV).manual_seed(vocab + n)
+    x = 3 * torch.randn((rows, vocab), device=DEV, generator=g)
+    x[torch.rand((rows, vocab), device=DEV, generator=g) >= left] = -float("inf")
+    x[:, vocab // 2] = 0.25                                # (something is)
+    x[-1, :200] = 1.0                                      # ties in the first warp's share
+    x = x.to(dt)
+    tokens = torch.full((rows,), vocab // 2, device=DEV, dtype=torch.int32)
+    score_check(scores.token_logprobs(x, tokens, n), score_reference(x, tokens, n), n)
+
+
+@gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_scores_of_many_rows_that_go_on_rising(dtype):
     """Whole rows in one CTA, whose every batch brings more candidates than the last; and rows of which all logits are equal."""
