@@ -14,7 +14,10 @@
 //  - bf16: S = Q K^T and O += P V as mma.sync m16n8k16 with Q, P and O in registers (the tensor cores idle most of the time
 //    anyway).  P goes in as two bf16 parts, P = hi + lo up to 2^-17: one part alone would add an error as large as the output's own
 //    rounding.  Up to 8 query rows the parts are the two halves of one 16-row operand, beyond that two contractions.
-//    f32: multiply-adds in 32 bits.
+//    f32: multiply-adds in 32 bits, two in an instruction, bound by what comes from shared memory: a lane has two keys and an eighth of the dims for all R
+//    rows, so that the queries are read once for two keys; the eight lanes' sums end up one row to a lane, which alone sees to its maximum
+//    and exponentials.  (us for floors of 21, 10.7, 8.3: 70B shape, 4 x 4096 34, 32 ragged up to 473 26, 34B shape, 59 up to 146 with 5 new tokens
+//    67; with a key to four lanes 41, 31, 83; with a branch for each row that is there 110, 89, 268.)
 // Keys that are not there (beyond the length, on no page) have probability 0, and zeros take their values' place.
 #include <cuda.h>
 
@@ -97,7 +100,20 @@ __device__ __forceinline__ uint32_t rest(float a, float b, uint32_t hi) {
 }
 __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
 
-// T: the cache's type.  R: query rows of a tile (8, or 16 in bf16).
+// Two 32-bit numbers at a time.
+__device__ __forceinline__ u64 pair(float a, float b) {
+  u64 y;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"(a), "f"(b));
+  return y;
+}
+__device__ __forceinline__ void unpair(u64 x, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x)); }
+__device__ __forceinline__ u64 fma2(u64 a, u64 b, u64 c) {
+  u64 y;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(y) : "l"(a), "l"(b), "l"(c));
+  return y;
+}
+
+// T: the cache's type.  R: query rows of a tile (8 or 16; f32: 1, 4 or 8).
 template <typename T, int D, int R>
 struct Cfg {
   static constexpr bool BF = sizeof(T) == 2;
@@ -109,13 +125,14 @@ struct Cfg {
   static constexpr int PITCH = D * 4 + 16;
   static constexpr int HALF_STAGE = BF ? BOXES * BOX : KW * PITCH;
   static constexpr int STAGE = 2 * HALF_STAGE;
-  // (f32: two CTAs on an SM with two stages, one with three: four sequences of 1024, 7B shape, 40 and 61 us)
-  static constexpr int STAGES = BF ? (D <= 64 ? 4 : 3) : 2;
+  // (f32, 128: two CTAs on an SM with two stages, one with three: four sequences of 1024, 7B shape, 29 and 32 us, of 4096, 70B shape, 34 and 44)
+  static constexpr int STAGES = BF ? (D <= 64 ? 4 : 3) : D == 128 ? 2 : D == 96 ? 3 : 4;
   static constexpr int KEY_LANES = D == 96 ? 1 : 128 / D;   // f32: keys whose values the lanes of a warp work on at a time
   static constexpr int CHUNK = 512 / R;             // pieces joined at a time
   static constexpr int OFF_RING = 0;                                      // [warp][stage]
   static constexpr int OFF_Q = WARPS * STAGES * STAGE;                    // f32: [warp][R][D]
-  static constexpr int OFF_ML = OFF_Q + (BF ? 0 : WARPS * R * D * 4);     // [warp][R][2]
+  static constexpr int OFF_P = OFF_Q + (BF ? 0 : WARPS * R * D * 4);      // f32: [warp][key][R]
+  static constexpr int OFF_ML = OFF_P + (BF ? 0 : WARPS * KW * R * 4);    // [warp][R][2]
   static constexpr int OFF_JOIN = OFF_ML + WARPS * R * 8;                // [CHUNK][R][2]
   static_assert(CHUNK * R * 8 >= 5 * THREADS * 4, "the shares of a join fit there too");
   static constexpr int OFF_BAR = OFF_JOIN + CHUNK * R * 8;                // [warp][stage]
@@ -257,12 +274,14 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
 
   // ---- state of the item.  bf16: mma fragments, rows lane / 4 (and + 8; up to 8 rows that half holds the probabilities' second parts);
   // f32: four columns a lane.
-  constexpr int NACC = C::BF ? D / 2 : R * 4, NST = C::BF ? R / 8 : R;
+  constexpr int NACC = C::BF ? D / 2 : R * 4, NST = C::BF ? R / 8 : 1;
   float acc[NACC], m[NST], l[NST];
   uint32_t qf[C::BF ? D / 16 * 2 * NST : 1];                       // [step][row half][k half]
   int vis[NST];
   float *s_q = (float *)(smem + C::OFF_Q) + (C::BF ? 0 : warp * R * D);
+  float *s_p = (float *)(smem + C::OFF_P) + (C::BF ? 0 : warp * C::KW * R);
   float *s_ml = (float *)(smem + C::OFF_ML);
+  auto slot_of = [](int r, int i) { return R == 1 ? i : ((r >> 1) * 4 + i) * 2 + (r & 1); };   // f32: of row r, column i in acc: two rows side by side
   bool fresh = true;
   int first_tile = 0;                                              // of the item's part that this CTA has
 
@@ -276,20 +295,27 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
       for (int i = 0; i < NACC; ++i) acc[i] = 0.f;
 #pragma unroll
       for (int i = 0; i < NST; ++i) {
-        const int r = C::BF ? (lane >> 2) + 8 * i : i, at = rt * R + min(r, rows - 1), tok = p.group_of.quot(at);
+        const int r = C::BF ? (lane >> 2) + 8 * i : lane & (R - 1), at = rt * R + min(r, rows - 1), tok = p.group_of.quot(at);
         m[i] = -INFINITY;
         l[i] = 0.f;
         vis[i] = r < rows ? c.len - p.n_new + 1 + tok : 0;
-        const int64_t q_at = ((int64_t)c.s * p.n_new + tok) * p.q_stride + (int64_t)(kvh * p.group + at - tok * p.group) * D;
         if constexpr (C::BF) {
+          const int64_t q_at = ((int64_t)c.s * p.n_new + tok) * p.q_stride + (int64_t)(kvh * p.group + at - tok * p.group) * D;
           const uint32_t *src = (const uint32_t *)((const __nv_bfloat16 *)p.q + q_at) + (lane & 3);
 #pragma unroll
           for (int j = 0; j < D / 16; ++j) {
             qf[(j * NST + i) * 2] = r < rows ? src[j * 8] : 0u;
             qf[(j * NST + i) * 2 + 1] = r < rows ? src[j * 8 + 4] : 0u;
           }
-        } else {
-          for (int d = lane; d < D; d += 32) s_q[r * D + d] = r < rows ? ((const float *)p.q)[q_at + d] : 0.f;
+        }
+      }
+      if constexpr (!C::BF) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          const int at = rt * R + min(r, rows - 1), tok = p.group_of.quot(at);
+          const int64_t q_at = ((int64_t)c.s * p.n_new + tok) * p.q_stride + (int64_t)(kvh * p.group + at - tok * p.group) * D;
+          const float4 x = *(const float4 *)((const float *)p.q + q_at + min(lane, D / 4 - 1) * 4);
+          if (lane < D / 4) *(float4 *)(s_q + r * D + lane * 4) = r < rows ? x : make_float4(0.f, 0.f, 0.f, 0.f);
         }
       }
       if (!C::BF) __syncwarp();
@@ -420,57 +446,135 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
           }
         }
       } else {
-        // scores: a key has four lanes, each a quarter of the dims (every fourth piece of four)
-        const int key = lane >> 2, part = lane & 3;
-        const float *kr = (const float *)(kp + key * C::PITCH);
-        float s[R];
+        // Scores: two keys have eight lanes, each an eighth of the dims (every eighth piece of four).  All R rows, whether there or not: a branch for
+        // each would put their chains one after another.
+        const int part = lane & 7, pair_of = lane >> 3;
+        const float *kr = (const float *)(kp + pair_of * 2 * C::PITCH);
+        float x[2][R];
+        {
+          u64 s2[2][R];
 #pragma unroll
-        for (int r = 0; r < R; ++r) s[r] = 0.f;
-        for (int j = 0; j < D / 16; ++j) {
-          const int d = (4 * j + part) * 4;
-          const float4 kk = *(const float4 *)(kr + d);
+          for (int r = 0; r < R; ++r) s2[0][r] = s2[1][r] = 0;
 #pragma unroll
-          for (int r = 0; r < R; ++r) {
-            if (r >= rows) break;
-            const float4 qq = *(const float4 *)(s_q + r * D + d);
-            s[r] = fmaf(kk.x, qq.x, fmaf(kk.y, qq.y, fmaf(kk.z, qq.z, fmaf(kk.w, qq.w, s[r]))));
-          }
-        }
-        const bool there = mask >> key & 1;
+          for (int j = 0; j < D / 32; ++j) {
+            const int d = (8 * j + part) * 4;
+            const ulonglong2 k0 = *(const ulonglong2 *)(kr + d), k1 = *(const ulonglong2 *)(kr + C::PITCH / 4 + d);
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-          if (r >= rows) break;
-          float x = s[r];
-          x += __shfl_xor_sync(0xffffffffu, x, 1);
-          x += __shfl_xor_sync(0xffffffffu, x, 2);
-          x = there && key0 + key < vis[r] ? x * p.scale_log2 : -INFINITY;
-          float mx = x;
-          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
-          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
-          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-          if (mx > m[r] + GROWTH) {
-            const float a = ex2(m[r] - mx);
-            m[r] = mx;
-            l[r] *= a;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[4 * r + i] *= a;
-          }
-          s[r] = ex2(x - base_of(m[r]));
-          l[r] += part == 0 ? s[r] : 0.f;
-        }
-        const int kl = C::KEY_LANES > 1 ? lane / (D / 4) : 0, col = min(lane - kl * (D / 4), D / 4 - 1) * 4;   // (96: lanes beyond the columns take part in the exchange)
-        for (int j = kl; j < C::KW; j += C::KEY_LANES) {
-          const float4 vv = *(const float4 *)(vp + j * C::PITCH + col * 4);
-#pragma unroll
-          for (int r = 0; r < R; ++r) {
-            if (r >= rows) break;
-            const float pr = __shfl_sync(0xffffffffu, s[r], j * 4);
-            if ((mask >> j & 1) && key0 + j < vis[r]) {            // (0 times what is stored there would not be 0 for all values)
-              acc[4 * r] = fmaf(pr, vv.x, acc[4 * r]);
-              acc[4 * r + 1] = fmaf(pr, vv.y, acc[4 * r + 1]);
-              acc[4 * r + 2] = fmaf(pr, vv.z, acc[4 * r + 2]);
-              acc[4 * r + 3] = fmaf(pr, vv.w, acc[4 * r + 3]);
+            for (int r = 0; r < R; ++r) {
+              const ulonglong2 qq = *(const ulonglong2 *)(s_q + r * D + d);
+              s2[0][r] = fma2(k0.y, qq.y, fma2(k0.x, qq.x, s2[0][r]));
+              s2[1][r] = fma2(k1.y, qq.y, fma2(k1.x, qq.x, s2[1][r]));
             }
+          }
+#pragma unroll
+          for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+              float a, b;
+              unpair(s2[k][r], a, b);
+              x[k][r] = a + b;
+            }
+        }
+        // The eight lanes' sums: of each two numbers a lane keeps one and hands the other over, until it has its own row's (8 rows: of both keys; fewer:
+        // of one key, the second in lanes 4 to 7).
+        constexpr int NX = R == 8 ? 2 : 1;
+        auto halve = [&](float a, float b, int o) {                // a to the lanes without bit o, b to those with it
+          const bool up = lane & o;
+          return (up ? b : a) + __shfl_xor_sync(0xffffffffu, up ? a : b, o);
+        };
+        float sc[NX];
+        if constexpr (R == 8) {
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[k][r] = halve(x[k][r], x[k][r + 4], 4);
+#pragma unroll
+            for (int r = 0; r < 2; ++r) x[k][r] = halve(x[k][r], x[k][r + 2], 2);
+            sc[k] = halve(x[k][0], x[k][1], 1);
+          }
+        } else {
+#pragma unroll
+          for (int r = 0; r < R; ++r) x[0][r] = halve(x[0][r], x[1][r], 4);
+          if constexpr (R == 4) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) x[0][r] = halve(x[0][r], x[0][r + 2], 2);
+            sc[0] = halve(x[0][0], x[0][1], 1);
+          } else {
+            sc[0] = x[0][0];
+            sc[0] += __shfl_xor_sync(0xffffffffu, sc[0], 2);
+            sc[0] += __shfl_xor_sync(0xffffffffu, sc[0], 1);
+          }
+        }
+        constexpr int KEYS_FROM = R == 8 ? 8 : 4;                  // from this bit on lanes differ in the key
+        const int row = lane & (R - 1), key = pair_of * 2 + (R == 8 ? 0 : lane >> 2 & 1);
+        const bool all = mask == (1u << C::KW) - 1 && key0 + C::KW <= c.len - p.n_new + 1;   // (uniform) every row sees every key
+        float mx = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < NX; ++i) {
+          sc[i] = all || ((mask >> (key + i) & 1) && key0 + key + i < vis[0]) ? sc[i] * p.scale_log2 : -INFINITY;
+          mx = fmaxf(mx, sc[i]);
+        }
+        if (__any_sync(0xffffffffu, mx > m[0] + GROWTH)) {
+#pragma unroll
+          for (int o = KEYS_FROM; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+          const float a = mx > m[0] + GROWTH ? ex2(m[0] - mx) : 1.f;
+          if (mx > m[0] + GROWTH) m[0] = mx;
+          l[0] *= a;
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            const float ar = __shfl_sync(0xffffffffu, a, r);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[slot_of(r, i)] *= ar;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < NX; ++i) {
+          const float e = ex2(sc[i] - base_of(m[0]));
+          l[0] += e;
+          s_p[(key + i) * R + row] = e;                            // (one row: four lanes the same)
+        }
+        __syncwarp();
+        const int kl = C::KEY_LANES > 1 ? lane / (D / 4) : 0, col = min(lane - kl * (D / 4), D / 4 - 1) * 4;
+        if (p.n_new == 1 || all) {                                 // (the values of keys that are not there are zeros)
+#pragma unroll
+          for (int j0 = 0; j0 < C::KW; j0 += C::KEY_LANES) {
+            const int j = j0 + kl;
+            const float4 vv = *(const float4 *)(vp + j * C::PITCH + col * 4);
+            if constexpr (R == 1) {
+              const float pr = s_p[j];
+              acc[0] = fmaf(pr, vv.x, acc[0]);
+              acc[1] = fmaf(pr, vv.y, acc[1]);
+              acc[2] = fmaf(pr, vv.z, acc[2]);
+              acc[3] = fmaf(pr, vv.w, acc[3]);
+            } else {
+              const u64 v2[4] = {pair(vv.x, vv.x), pair(vv.y, vv.y), pair(vv.z, vv.z), pair(vv.w, vv.w)};
+#pragma unroll
+              for (int r = 0; r < R; r += 4) {
+                const ulonglong2 pr = *(const ulonglong2 *)(s_p + j * R + r);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  float *a = acc + slot_of(r, i), *b = acc + slot_of(r + 2, i);
+                  unpair(fma2(pr.x, v2[i], pair(a[0], a[1])), a[0], a[1]);
+                  unpair(fma2(pr.y, v2[i], pair(b[0], b[1])), b[0], b[1]);
+                }
+              }
+            }
+          }
+        } else {                                                   // (0 times what is stored there would not be 0 for all values)
+          int seen[R];
+#pragma unroll
+          for (int r = 0; r < R; ++r) seen[r] = __shfl_sync(0xffffffffu, vis[0], r);
+          for (int j = kl; j < C::KW; j += C::KEY_LANES) {
+            const float4 vv = *(const float4 *)(vp + j * C::PITCH + col * 4);
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+              if ((mask >> j & 1) && key0 + j < seen[r]) {
+                const float pr = s_p[j * R + r];
+                acc[slot_of(r, 0)] = fmaf(pr, vv.x, acc[slot_of(r, 0)]);
+                acc[slot_of(r, 1)] = fmaf(pr, vv.y, acc[slot_of(r, 1)]);
+                acc[slot_of(r, 2)] = fmaf(pr, vv.z, acc[slot_of(r, 2)]);
+                acc[slot_of(r, 3)] = fmaf(pr, vv.w, acc[slot_of(r, 3)]);
+              }
           }
         }
       }
@@ -504,18 +608,16 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
         }
       } else {
 #pragma unroll
+        for (int o = R == 8 ? 8 : 4; o < 32; o <<= 1) l[0] += __shfl_xor_sync(0xffffffffu, l[0], o);
+        if (lane < min(R, rows)) *(float2 *)(s_ml + (warp * R + lane) * 2) = make_float2(m[0], l[0]);
+#pragma unroll
         for (int r = 0; r < R; ++r) {
-          if (r >= rows) break;
-          float x = l[r];
-          x += __shfl_xor_sync(0xffffffffu, x, 4);
-          x += __shfl_xor_sync(0xffffffffu, x, 8);
-          x += __shfl_xor_sync(0xffffffffu, x, 16);
 #pragma unroll
           for (int o = 16; o >= D / 4 && C::KEY_LANES > 1; o >>= 1)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) acc[4 * r + i] += __shfl_xor_sync(0xffffffffu, acc[4 * r + i], o);
-          if (lane < D / 4) *(float4 *)(part + r * D + ((lane * 4) ^ ((r & 3) * 8))) = make_float4(acc[4 * r], acc[4 * r + 1], acc[4 * r + 2], acc[4 * r + 3]);
-          if (lane == 0) *(float2 *)(s_ml + (warp * R + r) * 2) = make_float2(m[r], x);
+            for (int i = 0; i < 4; ++i) acc[slot_of(r, i)] += __shfl_xor_sync(0xffffffffu, acc[slot_of(r, i)], o);
+          if (lane < D / 4 && r < rows)
+            *(float4 *)(part + r * D + ((lane * 4) ^ ((r & 3) * 8))) = make_float4(acc[slot_of(r, 0)], acc[slot_of(r, 1)], acc[slot_of(r, 2)], acc[slot_of(r, 3)]);
         }
       }
       __syncthreads();
@@ -691,7 +793,9 @@ int launch(const AttnParams &p, const Maps &maps, int64_t most_cost, cudaStream_
 
 template <int D>
 int by_kind(const ouro_paged_cache *c, AttnParams p, bool tma, const Maps &maps, int64_t cost, cudaStream_t s) {
-  if (c->dtype == OURO_F32) return launch<float, D, 8, false>(p, maps, cost, s);
+  // (us with tiles of 1, 4, 8 rows: one row, 7B shape, 4 x 1024 28.7, 29.4, 33.7, 76 x 1528 of `tiny` 33.8, 46, 54; two, 7B shape: -, 29.6, 34.1)
+  if (c->dtype == OURO_F32)
+    return p.rows == 1 ? launch<float, D, 1, false>(p, maps, cost, s) : p.rows <= 4 ? launch<float, D, 4, false>(p, maps, cost, s) : launch<float, D, 8, false>(p, maps, cost, s);
   if (p.rows <= 8) return tma ? launch<__nv_bfloat16, D, 8, true>(p, maps, cost, s) : launch<__nv_bfloat16, D, 8, false>(p, maps, cost, s);
   return tma ? launch<__nv_bfloat16, D, 16, true>(p, maps, cost, s) : launch<__nv_bfloat16, D, 16, false>(p, maps, cost, s);
 }
@@ -715,7 +819,7 @@ extern "C" int ouro_paged_attention(const ouro_paged_cache *c, int32_t layer, co
   AttnParams p{};
   p.group = n_heads / c->n_kv_heads;
   p.rows = n_new * p.group;
-  const int tile = (c->dtype == OURO_F32 ? 8 : 16) * WARPS, rows_of = c->dtype == OURO_F32 || p.rows <= 8 ? 8 : 16;
+  const int tile = (c->dtype == OURO_F32 ? 8 : 16) * WARPS, rows_of = c->dtype == OURO_F32 ? (p.rows == 1 ? 1 : p.rows <= 4 ? 4 : 8) : p.rows <= 8 ? 8 : 16;
   p.row_tiles = (p.rows + rows_of - 1) / rows_of;
   p.cap = c->max_pages * c->page_size;
   const int64_t cost = ((int64_t)(p.cap + tile - 1) / tile + 8) * c->n_kv_heads * p.row_tiles;   // (8: no kernel's item costs more)
