@@ -128,14 +128,12 @@ struct Cfg {
   // (f32, 128: two CTAs on an SM with two stages, one with three: four sequences of 1024, 7B shape, 29 and 32 us, of 4096, 70B shape, 34 and 44)
   static constexpr int STAGES = BF ? (D <= 64 ? 4 : 3) : D == 128 ? 2 : D == 96 ? 3 : 4;
   static constexpr int KEY_LANES = D == 96 ? 1 : 128 / D;   // f32: keys whose values the lanes of a warp work on at a time
-  static constexpr int CHUNK = 512 / R;             // pieces joined at a time
   static constexpr int OFF_RING = 0;                                      // [warp][stage]
   static constexpr int OFF_Q = WARPS * STAGES * STAGE;                    // f32: [warp][R][D]
   static constexpr int OFF_P = OFF_Q + (BF ? 0 : WARPS * R * D * 4);      // f32: [warp][key][R]
   static constexpr int OFF_ML = OFF_P + (BF ? 0 : WARPS * KW * R * 4);    // [warp][R][2]
-  static constexpr int OFF_JOIN = OFF_ML + WARPS * R * 8;                // [CHUNK][R][2]
-  static_assert(CHUNK * R * 8 >= 5 * THREADS * 4, "the shares of a join fit there too");
-  static constexpr int OFF_BAR = OFF_JOIN + CHUNK * R * 8;                // [warp][stage]
+  static constexpr int OFF_JOIN = OFF_ML + WARPS * R * 8;                // [6][THREADS]: shares of a join
+  static constexpr int OFF_BAR = OFF_JOIN + 6 * THREADS * 4;                // [warp][stage]
   static constexpr int OFF_MASK = OFF_BAR + WARPS * STAGES * 8;           // [warp][stage]
   static constexpr int OFF_LEN = OFF_MASK + WARPS * STAGES * 4;           // [n]
   static constexpr int OFF_CUM = OFF_LEN + MAX_LIST * 4;                  // [n + 1] cost of a head and row tile
@@ -669,10 +667,10 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
         if (s_misc[4]) {
           if (tid == 0) p.counters[c0] = 0;
           __threadfence();
-          float2 *s_join = (float2 *)(smem + C::OFF_JOIN);
           auto where = [&](int cta) { return ((int64_t)cta * 2 + (cta == c0 ? 1 : 0)) * paged::ROW_TILE; };
-          // Four columns of a row, EACH times a thread; where that leaves threads over, the pieces are dealt out to `shares` of them.
-          constexpr int EACH = (R * C4 + THREADS - 1) / THREADS;
+          // Four columns of a row, EACH times a thread; where that leaves threads over, the pieces are dealt out to `shares` of them.  Sums and outputs
+          // of BATCH pieces are asked for at once, so that few pieces take one round trip.
+          constexpr int EACH = (R * C4 + THREADS - 1) / THREADS, BATCH = EACH > 2 ? 2 : 8 / EACH;
           const int E = rows * C4, shares = E < THREADS ? THREADS / E : 1, share = shares > 1 ? tid / E : 0;
           int at[EACH];
           float M[EACH], L[EACH], o[EACH][4];
@@ -682,50 +680,62 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
             M[k] = -INFINITY;
             L[k] = o[k][0] = o[k][1] = o[k][2] = o[k][3] = 0.f;
           }
-          for (int a0 = c0; a0 <= c1; a0 += C::CHUNK) {
-            const int many = min(C::CHUNK, c1 - a0 + 1);
-            for (int i = tid; i < many * R; i += THREADS)
-              if (i % R < rows) s_join[i] = __ldcg((const float2 *)(mls + (where(a0 + i / R) + i % R) * 2));
-            __syncthreads();
+          for (int a0 = c0 + share; a0 <= c1; a0 += BATCH * shares) {
+            float2 ml[EACH][BATCH];
+            float4 y[EACH][BATCH];
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b) {
+              const int64_t from = where(min(a0 + b * shares, c1));
+#pragma unroll
+              for (int k = 0; k < EACH; ++k) {
+                ml[k][b] = __ldcg((const float2 *)(mls + (from + at[k] / C4) * 2));
+                y[k][b] = __ldcg((const float4 *)(p.pieces + from * D + at[k] * 4));
+              }
+            }
 #pragma unroll
             for (int k = 0; k < EACH; ++k) {
               float mx = M[k];
-              for (int j = 0; j < many; ++j) mx = fmaxf(mx, s_join[j * R + at[k] / C4].x);
+#pragma unroll
+              for (int b = 0; b < BATCH; ++b) mx = fmaxf(mx, ml[k][b].x);    // (a piece twice changes no maximum)
               const float a = ex2(M[k] - base_of(mx));
               M[k] = mx;
               L[k] *= a;
 #pragma unroll
               for (int i = 0; i < 4; ++i) o[k][i] *= a;
-            }
-#pragma unroll(EACH > 2 ? 2 : 8 / EACH)
-            for (int j = share; j < many; j += shares) {
-              const float *piece_j = p.pieces + where(a0 + j) * D;
 #pragma unroll
-              for (int k = 0; k < EACH; ++k) {
-                const float4 y = __ldcg((const float4 *)(piece_j + at[k] * 4));
-                const float2 ml = s_join[j * R + at[k] / C4];
-                const float x = ex2(ml.x - base_of(M[k]));
-                L[k] = fmaf(x, ml.y, L[k]);
-                o[k][0] = fmaf(x, y.x, o[k][0]);
-                o[k][1] = fmaf(x, y.y, o[k][1]);
-                o[k][2] = fmaf(x, y.z, o[k][2]);
-                o[k][3] = fmaf(x, y.w, o[k][3]);
+              for (int b = 0; b < BATCH; ++b) {
+                if (a0 + b * shares > c1) continue;
+                const float x = ex2(ml[k][b].x - base_of(mx));
+                L[k] = fmaf(x, ml[k][b].y, L[k]);
+                o[k][0] = fmaf(x, y[k][b].x, o[k][0]);
+                o[k][1] = fmaf(x, y[k][b].y, o[k][1]);
+                o[k][2] = fmaf(x, y[k][b].z, o[k][2]);
+                o[k][3] = fmaf(x, y[k][b].w, o[k][3]);
               }
             }
-            __syncthreads();
           }
-          if (shares > 1) {                                        // (EACH is 1 or has one element, and all have the same M)
-            float *s_part = (float *)s_join;
+          if (shares > 1) {                                        // (EACH is 1 or has one element)
+            float *s_part = (float *)(smem + C::OFF_JOIN);
             s_part[tid] = L[0];
 #pragma unroll
             for (int i = 0; i < 4; ++i) s_part[(i + 1) * THREADS + tid] = o[0][i];
+            s_part[5 * THREADS + tid] = M[0];
             __syncthreads();
-            if (share == 0)
-              for (int w = 1; w < shares; ++w) {
-                L[0] += s_part[w * E + tid];
+            if (share == 0) {
+              float mx = M[0];
+              for (int w = 1; w < shares; ++w) mx = fmaxf(mx, s_part[5 * THREADS + w * E + tid]);
+              const float a = ex2(M[0] - base_of(mx));
+              M[0] = mx;
+              L[0] *= a;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o[0][i] += s_part[(i + 1) * THREADS + w * E + tid];
+              for (int i = 0; i < 4; ++i) o[0][i] *= a;
+              for (int w = 1; w < shares; ++w) {
+                const float x = ex2(s_part[5 * THREADS + w * E + tid] - base_of(mx));
+                L[0] = fmaf(x, s_part[w * E + tid], L[0]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[0][i] = fmaf(x, s_part[(i + 1) * THREADS + w * E + tid], o[0][i]);
               }
+            }
           }
 #pragma unroll
           for (int k = 0; k < EACH; ++k)
