@@ -127,7 +127,7 @@ struct Cfg {
   static constexpr int STAGE = 2 * HALF_STAGE;
   // (f32, 128: two CTAs on an SM with two stages, one with three: four sequences of 1024, 7B shape, 29 and 32 us, of 4096, 70B shape, 34 and 44)
   static constexpr int STAGES = BF ? (D <= 64 ? 4 : 3) : D == 128 ? 2 : D == 96 ? 3 : 4;
-  static constexpr int KEY_LANES = D == 96 ? 1 : 128 / D;   // f32: keys whose values the lanes of a warp work on at a time
+  [[maybe_unused]] static constexpr int KEY_LANES = D == 96 ? 1 : 128 / D;   // f32: keys whose values the lanes of a warp work on at a time
   static constexpr int OFF_RING = 0;                                      // [warp][stage]
   static constexpr int OFF_Q = WARPS * STAGES * STAGE;                    // f32: [warp][R][D]
   static constexpr int OFF_P = OFF_Q + (BF ? 0 : WARPS * R * D * 4);      // f32: [warp][key][R]

@@ -24,7 +24,7 @@ using paged::Walk;
 
 constexpr int ROW_WARPS = 8, ROW_THREADS = 32 * ROW_WARPS, THREADS = ROW_THREADS + 96;
 constexpr int KEYS = 64, HALF = KEYS / 2;          // of a unit, of a thread
-// us with runs from 2 (borders taken within 1), 3 (2) and 5 units on: 34B drafts 20.1, 20.7, 21.5; 64 ragged up to 300 with 5 tokens (70B shape) 31.8, 30.0, 32.4;
+// us with runs from 2 (borders taken within 1), 3 (2) and 5 units on: 34B drafts (with an earlier join) 20.1, 20.7, 21.5; 64 ragged up to 300 with 5 tokens (70B shape) 31.8, 30.0, 32.4;
 // one sequence of 300 (34B) 11.5, 10.6, 10.7; large calls the same.
 constexpr int ITEM_COST = 4;                       // what an item costs besides its units (filling and draining the chain), in units
 constexpr int SNAP = 2;                            // units in front of or behind a cut for which it is not worth its join
@@ -582,10 +582,13 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attention_tc_kernel(const At
 // on all SMs and behind the end of the kernel in front; by the CTA that was last to leave a piece it took 10 us and more (35 rows of D = 128 in 13
 // pieces).  The rows of an item are shared by gridDim.y CTAs.
 constexpr int JOIN_THREADS = 256, JOIN_SLICES = 8;
+// Pieces whose sums and outputs are asked for at once.  us with 2, 3, 4, 8 (all maxima first: 20.9, 31.3, 30.0): 34B drafts 19.0, 19.0, 19.1, 21.3; one of 11993 (70B
+// shape) 28.8, 27.4, 28.1, 28.1; 64 ragged up to 300 29.9, 30.6, 30.5, 33.0.
+constexpr int BATCH = 3;
 template <int D>
 __global__ void __launch_bounds__(JOIN_THREADS) paged_join_kernel(const AttnParams p, const int grid) {
   __shared__ int s_len[OURO_MAX_LIST], s_cum[OURO_MAX_LIST + 1], s_sums[JOIN_THREADS / 32];
-  __shared__ float s_part[5][JOIN_THREADS];
+  __shared__ float s_part[6][JOIN_THREADS];
   const int tid = threadIdx.x;
   pdl_trigger();
   // (the lengths were there before the kernel in front began)
@@ -611,31 +614,54 @@ __global__ void __launch_bounds__(JOIN_THREADS) paged_join_kernel(const AttnPara
   for (int e0 = 0; e0 < E; e0 += JOIN_THREADS) {
     const int e = min(e0 + tid - share * E, E - 1), r = r0 + e / C4, col = e % C4 * 4;
     float M = -INFINITY, L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int j = c0; j <= c1; ++j) M = fmaxf(M, __ldcg(mls + (where(j) + r) * 2));
-    const float base = M == -INFINITY ? 0.f : M;
-#pragma unroll 8
-    for (int j = c0 + share; j <= c1; j += shares) {
-      const float2 ml = __ldcg((const float2 *)(mls + (where(j) + r) * 2));
-      const float4 y = __ldcg((const float4 *)(p.pieces + (where(j) + r) * D + col));
-      const float x = ex2(ml.x - base);
-      L = fmaf(x, ml.y, L);
-      o[0] = fmaf(x, y.x, o[0]);
-      o[1] = fmaf(x, y.y, o[1]);
-      o[2] = fmaf(x, y.z, o[2]);
-      o[3] = fmaf(x, y.w, o[3]);
+    auto rescale = [&](float mx) {
+      const float a = ex2(M - base_of(mx));
+      M = mx;
+      L *= a;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] *= a;
+    };
+    for (int j0 = c0 + share; j0 <= c1; j0 += BATCH * shares) {    // sums and outputs of BATCH pieces are asked for at once
+      float2 ml[BATCH];
+      float4 y[BATCH];
+#pragma unroll
+      for (int b = 0; b < BATCH; ++b) {
+        const int64_t at = where(min(j0 + b * shares, c1)) + r;
+        ml[b] = __ldcg((const float2 *)(mls + at * 2));
+        y[b] = __ldcg((const float4 *)(p.pieces + at * D + col));
+      }
+      float mx = M;
+#pragma unroll
+      for (int b = 0; b < BATCH; ++b) mx = fmaxf(mx, ml[b].x);     // (a piece twice changes no maximum)
+      rescale(mx);
+#pragma unroll
+      for (int b = 0; b < BATCH; ++b) {
+        if (j0 + b * shares > c1) continue;
+        const float x = ex2(ml[b].x - base_of(mx));
+        L = fmaf(x, ml[b].y, L);
+        o[0] = fmaf(x, y[b].x, o[0]);
+        o[1] = fmaf(x, y[b].y, o[1]);
+        o[2] = fmaf(x, y[b].z, o[2]);
+        o[3] = fmaf(x, y[b].w, o[3]);
+      }
     }
     if (shares > 1) {
       s_part[0][tid] = L;
 #pragma unroll
       for (int i = 0; i < 4; ++i) s_part[i + 1][tid] = o[i];
+      s_part[5][tid] = M;
       __syncthreads();
-      if (share == 0)
+      if (share == 0) {
+        float mx = M;
+        for (int k = 1; k < shares; ++k) mx = fmaxf(mx, s_part[5][k * E + tid]);
+        rescale(mx);
         for (int k = 1; k < shares; ++k) {
-          L += s_part[0][k * E + tid];
+          const float x = ex2(s_part[5][k * E + tid] - base_of(mx));
+          L = fmaf(x, s_part[0][k * E + tid], L);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) o[i] += s_part[i + 1][k * E + tid];
+          for (int i = 0; i < 4; ++i) o[i] = fmaf(x, s_part[i + 1][k * E + tid], o[i]);
         }
+      }
     }
     if (share == 0 && e0 + tid < E) {
       const int at = w.rt * R + r, tok = p.group_of.quot(at);
