@@ -32,14 +32,14 @@ using paged::Walk;
 constexpr int WARPS = 4, THREADS = 32 * WARPS;
 constexpr int MAX_LIST = OURO_MAX_LIST;
 constexpr int ITEM_COST = 2;                        // what an item costs besides its units, in units
-// A unit takes a CTA about a microsecond alone (a chain of latencies), a join two and more.  us with runs from 1, 2, 4 units on, borders taken within
+// A unit takes a CTA about a microsecond alone (a chain of latencies), a join two and more.  us (with joins a microsecond longer) with runs from 1, 2, 4 units on, borders taken within
 // 0, 1, 3: one sequence of 700 keys (1.1B shape) 7.9, 9.4, 12.0; one of 1024 (70B shape) 9.4, 9.4, 13.2, of 4096 14.5, 13.3, 14.9; 60 ragged up to
 // 700 15.3, 14.2, 13.7; 16 of 512 15.1, 15.1, 13.7; one of 20000 with two kv heads 21.3, 21.2, 18.7; large calls the same.
 constexpr int SNAP = 1;                             // units in front of or behind a cut for which it is not worth its join
 constexpr int MIN_RUN = 2;                          // units for which another CTA is
-// More query rows of a kv head go to paged_attention_tc.cu (head dims 64 and 128).  us here and there: 35 rows, 34B drafts 20.0 and 20.7, one sequence of 4096
-// 21.8 and 22.0; 40 rows, 64 ragged up to 300 42.0 and 30.0, 48 up to 12345 (70B shape) 471 and 228; 128 rows, 8 of 4096 153 and 50; 64 rows of head
-// dim 64, one sequence of 700 10.4 and 12.7.  At 16 rows: 16 of 1000 (70B) 23.4 and 34.1, of the 1.1B shape 13.0 and 22.3.
+// More query rows of a kv head go to paged_attention_tc.cu (head dims 64 and 128).  us here and there: 35 rows, 34B drafts 17.4 and 19.0, 27 ragged up to 393
+// 27.8 and 25.4; 40 rows (70B shape), 64 ragged up to 300 40.8 and 30.6, one of 11993 33.8 and 27.4; 56 rows, two up to 4998 33.9 and 25.7; 128 rows, 8 of
+// 4096 154 and 51; 64 rows of head dim 64, one of 700 9.8 and 11.6.  At 16 rows: 16 of 1000 (70B) 22.3 and 30.6, of the 1.1B shape 12.4 and 22.6.
 constexpr int MMA_ROWS = 16;
 constexpr float GROWTH = 8.f;                       // (log2) a maximum may grow by this before sums are rescaled: they stay below 2^8 per key
 constexpr uint32_t SPIN_LIMIT = 1u << 22;
