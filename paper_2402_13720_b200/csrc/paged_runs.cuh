@@ -86,7 +86,7 @@ struct Runs {
     __syncthreads();
     cost = (int64_t)s_cum[p.n] * (p.Hkv * p.row_tiles);
     G = min((int64_t)grid, max((int64_t)1, cost / MIN_RUN));
-    each_run = cost / G;
+    each_run = cost <= INT32_MAX ? (int64_t)((uint32_t)cost / (uint32_t)G) : cost / G;
     rest = cost - each_run * G;
   }
   __device__ __forceinline__ void enter(Walk &w) const {
@@ -104,16 +104,15 @@ struct Runs {
     w.head = 0;
     if (++w.s < p.n) enter(w);
   }
-  // Where the c-th run begins.
+  // Where the c-th run begins.  A warp looks for the sequence together: one step for 32 sequences, two for all there can be.
   __device__ __forceinline__ Walk place(int64_t c) const {
     const int64_t at = each_run * c + (uint32_t)(rest * c) / (uint32_t)G, F = p.Hkv * p.row_tiles;   // cost * c / G
     Walk w{p.n, 0, 0, 0, 0, 0, nullptr};
     if (at >= cost) return w;
-    int lo = 0, hi = p.n - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) / 2;
-      if (s_cum[mid] * F <= at) lo = mid; else hi = mid - 1;
-    }
+    const int lane = threadIdx.x & 31;
+    int lo = 0;
+    if (p.n > 32) lo = 32 * (__popc(__ballot_sync(0xffffffffu, 32 * lane < p.n && s_cum[min(32 * lane, p.n)] * F <= at)) - 1);
+    if (p.n > 1) lo += __popc(__ballot_sync(0xffffffffu, lo + lane < p.n && s_cum[min(lo + lane, p.n)] * F <= at)) - 1;
     w.s = lo;
     enter(w);
     const int in = (int)(at - s_cum[lo] * F), each = w.tiles + ITEM_COST;   // fits: a sequence's cost is checked on the host
