@@ -660,13 +660,15 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
       if (!whole) {
         int c0, c1;
         runs.owners(was, c0, c1);
-        __threadfence();
         __syncthreads();
-        if (tid == 0) s_misc[4] = atomicAdd(p.counters + c0, 1) == c1 - c0;
+        if (tid == 0) {                                            // (releases what the CTA has written, acquires what the others have)
+          int before;
+          asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(p.counters + c0) : "memory");
+          s_misc[4] = before == c1 - c0;
+        }
         __syncthreads();
         if (s_misc[4]) {
           if (tid == 0) p.counters[c0] = 0;
-          __threadfence();
           auto where = [&](int cta) { return ((int64_t)cta * 2 + (cta == c0 ? 1 : 0)) * paged::ROW_TILE; };
           // Four columns of a row, EACH times a thread; where that leaves threads over, the pieces are dealt out to `shares` of them.  Sums and outputs
           // of BATCH pieces are asked for at once, so that few pieces take one round trip.
