@@ -1,7 +1,7 @@
 // Attention of several newest tokens over a paged cache (more than 16 query rows to a kv head): tcgen05 with TMEM accumulators.
 //
 // mma.sync tiles of 16 rows read every key from L2 and shared memory once per 16 rows, and a step of 16 keys takes a warp two thousand cycles
-// whatever it does (128 rows behind 8 x 4096 keys of the 70B shape: 150 us for 21 us of keys and values).  Here a tile has up to 128 query rows
+// whatever it does (128 rows behind 8 x 4096 keys of the 70B shape: 153 us for 21 us of keys and values, here 49).  Here a tile has up to 128 query rows
 // (new tokens x query heads of a group), one TMEM lane each:
 //     S = Q K^T    128 x 64 keys, two buffers in TMEM; Q lies in TMEM as well;
 //     P            two threads per row, half of the keys each: S comes into their registers, and all that they exchange is whether a maximum grew;
@@ -581,9 +581,12 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attention_tc_kernel(const At
 // The items that are cut, by the border of the first two runs that share one: its pieces are added up in ascending order.  One launch more, but
 // on all SMs and behind the end of the kernel in front; by the CTA that was last to leave a piece it took 10 us and more (35 rows of D = 128 in 13
 // pieces).  The rows of an item are shared by gridDim.y CTAs.
-constexpr int JOIN_THREADS = 256, JOIN_SLICES = 8;
-// Pieces whose sums and outputs are asked for at once.  us with 2, 3, 4, 8 (all maxima first: 20.9, 31.3, 30.0): 34B drafts 19.0, 19.0, 19.1, 21.3; one of 11993 (70B
-// shape) 28.8, 27.4, 28.1, 28.1; 64 ragged up to 300 29.9, 30.6, 30.5, 33.0.
+// (Every warp works out the runs and the item's CTAs, which is most of what few pieces cost.  us with 8 slices of 256 threads, 4 of 256, 8 of 128, 4 of 128,
+// 16 of 64: 34B drafts 18.1, 16.3, 16.6, 17.7, 16.6; 64 ragged up to 300, 70B shape, 29.7, 28.0, 27.2, 26.7, 27.6; 8 of 4096 with 16 new tokens 47.2, 45.8,
+// 44.6, 47.8, 45.2.)
+constexpr int JOIN_THREADS = 128, JOIN_SLICES = 8;
+// Pieces whose sums and outputs are asked for at once.  us with 2, 3, 4: 34B drafts 17.0, 16.5, 16.7; one of 30000 (70B shape) 41.3, 39.4, 40.5; 64 ragged up
+// to 300 27.2 each.  (All maxima first, then the outputs: some 2 us more.)
 constexpr int BATCH = 3;
 template <int D>
 __global__ void __launch_bounds__(JOIN_THREADS) paged_join_kernel(const AttnParams p, const int grid) {
