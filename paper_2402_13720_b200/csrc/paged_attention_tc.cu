@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attention_tc_kernel(const At
   if (tid == 0) {
     for (int i = 0; i < MAX_STAGES; ++i) {
       mbar_init(&ms->full[i], 1);
-      mbar_init(&ms->empty[i], 1);
+      mbar_init(&ms->empty[i], 2);                 // the contractions' commit, and warp 10: nobody may be a ring behind
       mbar_init(&ms->fixed[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -340,7 +340,9 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attention_tc_kernel(const At
       Walk c = begin;
       int stage = 0, round = 0, item = 0;
       for (; !paged::same(c, end); runs.next(c)) {
-        warp_wait(&ms->full[stage], round, ms, p.status);          // (of every unit: a phase's parity tells no more than two apart)
+        // (Of every unit, and each is given back here too: a phase's parity tells no more than two apart, so this warp may be neither ahead of
+        // `full` nor lapped by it.)
+        warp_wait(&ms->full[stage], round, ms, p.status);
         if (at_tail(c)) {
           const int rest = c.len - c.tile * KEYS;                  // keys of the sequence from here on
           uint8_t *vp = smem + C::OFF_RING + stage * C::STAGE + C::BOXES * C::KV_BOX;
@@ -372,6 +374,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attention_tc_kernel(const At
           __syncwarp();
           if (lane == 0) mbar_arrive(&ms->fixed[stage]);
         }
+        if (lane == 0) mbar_arrive(&ms->empty[stage]);
         item += c.tile == c.tiles - 1;
         if (++stage == C::STAGES) stage = 0, ++round;
       }
