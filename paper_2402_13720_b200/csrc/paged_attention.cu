@@ -208,8 +208,8 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
       const uint32_t dst = ring + stage * C::STAGE;
       if constexpr (TMA) {
         const int key = f.tile * C::TILE + warp * C::KW, id = __shfl_sync(0xffffffffu, ids, f.tile - ids_base);
-        if (key < f.len && !*s_abort) {                            // (else the warp has no keys in the unit)
-          if (elect_one()) {
+        if (key < f.len) {                                         // (else the warp has no keys in the unit)
+          if (elect_one() && !*s_abort) {                          // (who gave up is asked by the one thread: the warp stays together)
             const bool there = id >= 0 && id < p.n_pages;
             s_mask[stage] = there ? 0xffffu : 0u;
             const uint32_t bar = bars + stage * 8;
@@ -252,15 +252,18 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
   auto wait = [&](int stage) {
     if constexpr (TMA) {
       const uint32_t parity = phases >> stage & 1;
-      for (uint32_t i = 0; i < SPIN_LIMIT; ++i) {
-        if (mbar_test(bars + stage * 8, parity)) {
-          phases ^= 1u << stage;
-          return;
-        }
-        if ((i & 63) == 63 && *s_abort) return;
+      bool done = false;
+      for (uint32_t i = 0; i < SPIN_LIMIT && !done; ++i) {
+        done = mbar_test(bars + stage * 8, parity);
+        if (!done && (i & 63) == 63 && *s_abort) break;
+      }
+      // (each lane polls for itself; ldmatrix and the contractions behind this want the warp together)
+      if (__all_sync(0xffffffffu, done)) {
+        phases ^= 1u << stage;
+        return;
       }
       *s_abort = 1;
-      atomicCAS(p.status, OURO_OK, OURO_ETIMEOUT);
+      if (lane == 0) atomicCAS(p.status, OURO_OK, OURO_ETIMEOUT);
     } else {
       asm volatile("cp.async.wait_group %0;" ::"n"(C::STAGES - 2) : "memory");
       __syncwarp();

@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attention_tc_kernel(const At
         const int id0 = on ? mine : p.n_pages;                     // beyond the pool: zeros, nothing is read
         if (elect_one()) ms->there[stage] = there;
         __syncwarp();
-        if (!*dead) {
+        if (!__any_sync(0xffffffffu, *dead)) {                     // (the same for the warp: it shuffles and elects in there)
           const int step = box_rows / 16;                          // blocks in a box, all on one page
           const int boxes = blocks <= 0 ? 0 : (blocks + step - 1) / step;
           if (elect_one()) mbar_expect(&ms->full[stage], boxes * step * 16 * 128 * 2 * C::BOXES);

@@ -322,6 +322,23 @@ def test_attention_equals_the_definition(layout, page, h, hkv, d, dtype, new, le
 
 
 @gpu
+@pytest.mark.parametrize("page,h,hkv,d", [(16, 4, 4, 128), (32, 32, 4, 64), (64, 16, 1, 128), (128, 12, 1, 64), (16, 6, 3, 96)])
+def test_whole_units_to_the_last(page, h, hkv, d):
+    """Lengths of whole units with one new token: nothing at a sequence's end is looked at apart, the contractions come right behind the wait."""
+    build.build()
+    for lens in ([64], [128, 64, 192], [64 * k for k in range(1, 30)], [64 * 200, 64], [4096] * 9):
+        lens = [-(-x // page) * page for x in lens]
+        cache, table = filled("rows", page, hkv, d, torch.bfloat16, lens)
+        q = torch.randn((len(lens), 1, h, d), device=DEV).to(torch.bfloat16)
+        want, _ = reference(cache.k[0], cache.v[0], table, lens, range(len(lens)), q, d ** -0.5)
+        first = cache.attend(0, q)
+        close(first, want, 5.5, torch.bfloat16)
+        for _ in range(20):
+            assert torch.equal(cache.attend(0, q), first)
+        cache.check()
+
+
+@gpu
 def test_one_token_and_three_dimensions():
     build.build()
     cache, table = filled("rows", 16, 2, 128, torch.bfloat16, [33, 5])
