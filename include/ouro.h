@@ -346,6 +346,12 @@ int ouro_paged_append(const ouro_paged_cache *cache, int32_t layer, const void *
 int ouro_paged_attention(const ouro_paged_cache *cache, int32_t layer, const int32_t *seqs_dev, int32_t n, int32_t n_new, const void *q_dev,
                          int64_t q_stride, int32_t n_heads, float scale, void *out_dev, float *lse_dev, void *cuda_stream);
 
+/* Test aid: how often the attention kernels' bounded waits for their own copies and contractions poll, in calls made from now on in this process (default
+ * 1 << 22; negative restores it).  0 makes a wait for what is not there yet give up at once: the kernels return normally with wrong outputs, ouro_paged_status returns
+ * OURO_ETIMEOUT, and the next call with the default is right again.  (Caches in f32 and with a page_size that is no multiple of 16 wait without a limit of
+ * their own: for copies that each thread has issued itself.) */
+int ouro_paged_debug_set_wait_limit(int64_t polls);
+
 /* What a row of logits says about a token: logits [rows, vocab] (OURO_F32 or OURO_BF16), rows row_stride elements apart.
  *   logprob_dev [rows]: log probability of tokens_dev[row] (-inf where it lies outside the vocabulary); entropy_dev [rows] in nats;
  *   top_ids_dev, top_logprobs_dev [rows, n_top]: the n_top <= OURO_MAX_TOP best, best first, ties by the lowest id.

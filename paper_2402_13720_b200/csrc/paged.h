@@ -1,6 +1,7 @@
 // What the paged cache's translation units share: checks of a cache's description, the workspace's layout, errors without a context.
 #pragma once
 
+#include <atomic>
 #include <string>
 
 #include "ouro_internal.h"
@@ -47,6 +48,10 @@ inline int launched(const char *call) {
   ouro_set_global_error(std::string(call) + ": " + cudaGetErrorString(e));
   return OURO_ECUDA;
 }
+
+// Polls of the attention kernels' bounded waits.
+constexpr uint32_t WAIT_LIMIT = 1u << 22;
+extern std::atomic<uint32_t> wait_limit;
 
 inline const char *wrong_shape(const ouro_paged_cache *c) {
   if (!c) return "the cache is NULL";

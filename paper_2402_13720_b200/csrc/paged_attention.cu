@@ -42,7 +42,7 @@ constexpr int MIN_RUN = 2;                          // units for which another C
 // 4096 153 and 48.6; 64 rows of head dim 64, one of 700 9.5 and 11.0.  At 16 rows: 16 of 1000 (70B) 21.2 and 27.2, of the 1.1B shape 11.7 and 18.2.
 constexpr int MMA_ROWS = 16;
 constexpr float GROWTH = 8.f;                       // (log2) a maximum may grow by this before sums are rescaled: they stay below 2^8 per key
-constexpr uint32_t SPIN_LIMIT = 1u << 22;
+constexpr int DRAIN_POLLS = 1 << 14;                // of a call that gave up, for a copy still under way to end (some 200 us; a copy takes a few)
 
 // The pools as five dimensions (dim, head, row, page, layer); boxes of 64 dims x 16 rows.
 struct Maps {
@@ -66,6 +66,17 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
       "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ bool mbar_poll(uint32_t bar, uint32_t parity) {   // without suspending the thread
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
       "selp.u32 %0, 1, 0, p;\n\t}"
       : "=r"(ok)
       : "r"(bar), "r"(parity)
@@ -253,7 +264,7 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
     if constexpr (TMA) {
       const uint32_t parity = phases >> stage & 1;
       bool done = false;
-      for (uint32_t i = 0; i < SPIN_LIMIT && !done; ++i) {
+      for (uint32_t i = 0; i < p.wait_limit && !done; ++i) {
         done = mbar_test(bars + stage * 8, parity);
         if (!done && (i & 63) == 63 && *s_abort) break;
       }
@@ -755,9 +766,9 @@ __global__ void __launch_bounds__(THREADS, 2) paged_attention_kernel(const AttnP
   }
   if constexpr (!TMA) asm volatile("cp.async.wait_all;" ::: "memory");
   if constexpr (TMA)
-    if (*s_abort)                                                  // copies may be under way still: a bounded time for them to end
-      for (int i = 0; i < C::STAGES; ++i)
-        for (uint32_t j = 0; j < 4096 && !mbar_test(bars + i * 8, phases >> i & 1); ++j) {}
+    if (*s_abort)                                                  // copies may be under way still: a bounded time for them to end (a stage without one
+      for (int i = 0; i < C::STAGES; ++i)                          // is polled in vain)
+        for (int j = 0; j < DRAIN_POLLS && !mbar_poll(bars + i * 8, phases >> i & 1); ++j) {}
 }
 
 const char *CALL = "ouro_paged_attention";
@@ -817,6 +828,13 @@ int by_kind(const ouro_paged_cache *c, AttnParams p, bool tma, const Maps &maps,
 
 }  // namespace
 
+std::atomic<uint32_t> paged::wait_limit{paged::WAIT_LIMIT};
+
+extern "C" int ouro_paged_debug_set_wait_limit(int64_t polls) {
+  paged::wait_limit = polls < 0 || polls > paged::WAIT_LIMIT ? paged::WAIT_LIMIT : (uint32_t)polls;
+  return OURO_OK;
+}
+
 extern "C" int ouro_paged_attention(const ouro_paged_cache *c, int32_t layer, const int32_t *seqs, int32_t n, int32_t n_new, const void *q,
                                     int64_t q_stride, int32_t n_heads, float scale, void *out, float *lse, void *stream) {
   if (const char *w = paged::wrong(c)) return paged::refuse(CALL, w);
@@ -851,6 +869,7 @@ extern "C" int ouro_paged_attention(const ouro_paged_cache *c, int32_t layer, co
   p.page.set(c->page_size); p.group_of.set(p.group);
   p.n_pages = c->n_pages; p.max_pages = c->max_pages; p.max_seqs = c->max_seqs;
   p.scale_log2 = scale * 1.4426950408889634f;
+  p.wait_limit = paged::wait_limit.load(std::memory_order_relaxed);
   int status = OURO_OK;
   if (p.rows > MMA_ROWS && paged::attention_tc(c, p, (cudaStream_t)stream, &status)) return status;
   // The copy engine fetches 16 rows of a head at a time: where pages are multiples of that.

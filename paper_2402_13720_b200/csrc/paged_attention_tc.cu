@@ -32,7 +32,7 @@ constexpr int MIN_RUN = 3;                         // units for which another CT
 constexpr int R = 128;                             // query rows of a tile
 typedef paged::Runs<KEYS, ITEM_COST, SNAP, MIN_RUN> Share;
 constexpr float GROWTH = 8.f;                      // (log2) a maximum may grow by this before sums and outputs are rescaled
-constexpr uint32_t SPIN_LIMIT = 1u << 22;
+constexpr uint32_t DRAIN_POLLS = 1u << 20;         // for copies and contractions under way when their warp is done: they end by themselves
 constexpr int MAX_STAGES = 8, ODD_SLOTS = 16;      // (who looks at the ends of sequences is a ring ahead of the rows at most)
 
 struct Maps {
@@ -86,16 +86,16 @@ __device__ __forceinline__ bool mbar_test(uint64_t *bar, uint32_t parity) {
 }
 // Bounded wait for the phase-th completion (from 0).  Whoever gives up raises the cache's status; then nobody in the CTA issues or waits any more, and the
 // call ends with wrong results and an error.
-__device__ __forceinline__ void mbar_wait(uint64_t *bar, uint32_t phase, Misc *ms, int *status) {
-  bool done = mbar_test(bar, phase & 1);
-  for (uint32_t i = 0; i < SPIN_LIMIT && !done; ++i) done = mbar_test(bar, phase & 1) || ((i & 63) == 63 && *(volatile int *)&ms->dead);
+__device__ __forceinline__ void mbar_wait(uint64_t *bar, uint32_t phase, Misc *ms, const AttnParams &p) {
+  bool done = mbar_test(bar, phase & 1);           // (in front of the loop: 34B drafts 16.7 us, in it 17.1)
+  for (uint32_t i = 0; i < p.wait_limit && !done; ++i) done = mbar_test(bar, phase & 1) || ((i & 63) == 63 && *(volatile int *)&ms->dead);
   if (!done) {
     *(volatile int *)&ms->dead = 1;
-    atomicCAS(status, OURO_OK, OURO_ETIMEOUT);
+    atomicCAS(p.status, OURO_OK, OURO_ETIMEOUT);
   }
 }
-__device__ __forceinline__ void warp_wait(uint64_t *bar, uint32_t phase, Misc *ms, int *status) {
-  mbar_wait(bar, phase, ms, status);
+__device__ __forceinline__ void warp_wait(uint64_t *bar, uint32_t phase, Misc *ms, const AttnParams &p) {
+  mbar_wait(bar, phase, ms, p);
   __syncwarp();
 }
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, uint64_t *bar, int dim, int head, int row, int page, int layer) {
@@ -250,7 +250,8 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attention_tc_kernel(const At
           const int key = c.tile * KEYS + lane * 16;
           ids = key < c.len ? c.row[key < c.len ? p.page.quot(key) : 0] : -1;
         }
-        if (round > 0) warp_wait(&ms->empty[stage], round - 1, ms, p.status);
+        if (round > 0) warp_wait(&ms->empty[stage], round - 1, ms, p);
+        if (__any_sync(0xffffffffu, *dead)) break;                 // (the same for the warp: it shuffles and elects from here on)
         const int blocks = min(4, (c.len - c.tile * KEYS + 15) / 16);    // with keys of the sequence
         const int mine = __shfl_sync(0xffffffffu, ids, (c.tile - ids_tile) * 4 + (lane & 3));
         const bool on = (lane & 3) < blocks && mine >= 0 && mine < p.n_pages;
@@ -258,31 +259,29 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attention_tc_kernel(const At
         const int id0 = on ? mine : p.n_pages;                     // beyond the pool: zeros, nothing is read
         if (elect_one()) ms->there[stage] = there;
         __syncwarp();
-        if (!__any_sync(0xffffffffu, *dead)) {                     // (the same for the warp: it shuffles and elects in there)
-          const int step = box_rows / 16;                          // blocks in a box, all on one page
-          const int boxes = blocks <= 0 ? 0 : (blocks + step - 1) / step;
-          if (elect_one()) mbar_expect(&ms->full[stage], boxes * step * 16 * 128 * 2 * C::BOXES);
-          __syncwarp();
-          for (int b = 0; b < 4; b += step) {
-            const int page = __shfl_sync(0xffffffffu, id0, b);
-            if (b < blocks && elect_one()) {
-              const int key = c.tile * KEYS + b * 16, row = key - p.page.quot(key) * (int)p.page.d;
-              const uint32_t dst = sm + C::OFF_RING + stage * C::STAGE + b * 16 * 128;
+        const int step = box_rows / 16;                            // blocks in a box, all on one page
+        const int boxes = blocks <= 0 ? 0 : (blocks + step - 1) / step;
+        if (elect_one()) mbar_expect(&ms->full[stage], boxes * step * 16 * 128 * 2 * C::BOXES);
+        __syncwarp();
+        for (int b = 0; b < 4; b += step) {
+          const int page = __shfl_sync(0xffffffffu, id0, b);
+          if (b < blocks && elect_one()) {
+            const int key = c.tile * KEYS + b * 16, row = key - p.page.quot(key) * (int)p.page.d;
+            const uint32_t dst = sm + C::OFF_RING + stage * C::STAGE + b * 16 * 128;
 #pragma unroll
-              for (int x = 0; x < C::BOXES; ++x) {
-                tma_load(dst + x * C::KV_BOX, &maps.k, &ms->full[stage], x * 64, c.head, row, page, p.layer);
-                tma_load(dst + (C::BOXES + x) * C::KV_BOX, &maps.v, &ms->full[stage], x * 64, c.head, row, page, p.layer);
-              }
+            for (int x = 0; x < C::BOXES; ++x) {
+              tma_load(dst + x * C::KV_BOX, &maps.k, &ms->full[stage], x * 64, c.head, row, page, p.layer);
+              tma_load(dst + (C::BOXES + x) * C::KV_BOX, &maps.v, &ms->full[stage], x * 64, c.head, row, page, p.layer);
             }
-            __syncwarp();
           }
+          __syncwarp();
         }
         if (++stage == C::STAGES) stage = 0, ++round;
       }
-      if (*dead) {                                                 // copies may be under way still: a bounded time for them to end
-        for (int i = 0; i < C::STAGES; ++i)
-          for (uint32_t j = 0; j < 4096 && !mbar_test(&ms->full[i], (round - (i >= stage)) & 1); ++j) {}
-      }
+      // Nobody else is sure to wait for the copies under way once a wait has given up, so their last phases are waited for here.
+      for (int i = 0; i < C::STAGES; ++i)
+        if (round > 0 || i < stage)
+          for (uint32_t j = 0; j < DRAIN_POLLS && !mbar_test(&ms->full[i], (round - (i >= stage)) & 1); ++j) {}
     } else if (warp == ROW_WARPS + 1) {
       // ================================================================ contractions, one thread
       if (elect_one()) {
@@ -292,7 +291,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attention_tc_kernel(const At
         bool fresh = true, was_fresh = true;
         const uint64_t k0 = desc_k(sm + C::OFF_RING), v0 = desc_mn(sm + C::OFF_RING + C::BOXES * C::KV_BOX, C::KV_BOX);
         auto pv = [&](uint32_t v, int st, bool first) {            // O of unit v's item (+)= P V
-          mbar_wait(&ms->p_full[v & 1], v >> 1, ms, p.status);
+          mbar_wait(&ms->p_full[v & 1], v >> 1, ms, p);
           fence_after_sync();
           if (*dead) return;
           const uint64_t b = v0 + ((uint32_t)(st * C::STAGE) >> 4);
@@ -306,14 +305,14 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attention_tc_kernel(const At
         };
         for (; !paged::same(c, end); ++u) {
           if (fresh && u > 0) pv(u - 1, was_stage, was_fresh);     // (the rows ask for it before they bring the next queries)
-          if (fresh) mbar_wait(&ms->q_full, items++, ms, p.status);
+          if (fresh) mbar_wait(&ms->q_full, items++, ms, p);
           if (at_tail(c)) {
-            mbar_wait(&ms->fixed[stage], fixes >> stage & 1, ms, p.status);
+            mbar_wait(&ms->fixed[stage], fixes >> stage & 1, ms, p);
             fixes ^= 1u << stage;
           } else {
-            mbar_wait(&ms->full[stage], round, ms, p.status);
+            mbar_wait(&ms->full[stage], round, ms, p);
           }
-          if (u >= 2) mbar_wait(&ms->s_free[u & 1], (u - 2) >> 1, ms, p.status);
+          if (u >= 2) mbar_wait(&ms->s_free[u & 1], (u - 2) >> 1, ms, p);
           fence_after_sync();
           if (!*dead) {
             const uint64_t b = k0 + ((uint32_t)(stage * C::STAGE) >> 4);
@@ -330,10 +329,8 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attention_tc_kernel(const At
           if (++stage == C::STAGES) stage = 0, ++round;
         }
         pv(u - 1, was_stage, was_fresh);
-        if (*dead) {                                               // contractions may be under way still
-          mma_commit(&ms->drained);
-          for (uint32_t j = 0; j < 4096 && !mbar_test(&ms->drained, 0); ++j) {}
-        }
+        mma_commit(&ms->drained);                                  // (the same for the contractions)
+        for (uint32_t j = 0; j < DRAIN_POLLS && !mbar_test(&ms->drained, 0); ++j) {}
       }
     } else if (warp == ROW_WARPS + 2) {
       // ================================================================ units at a sequence's end
@@ -342,7 +339,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attention_tc_kernel(const At
       for (; !paged::same(c, end); runs.next(c)) {
         // (Of every unit, and each is given back here too: a phase's parity tells no more than two apart, so this warp may be neither ahead of
         // `full` nor lapped by it.)
-        warp_wait(&ms->full[stage], round, ms, p.status);
+        warp_wait(&ms->full[stage], round, ms, p);
         if (at_tail(c)) {
           const int rest = c.len - c.tile * KEYS;                  // keys of the sequence from here on
           uint8_t *vp = smem + C::OFF_RING + stage * C::STAGE + C::BOXES * C::KV_BOX;
@@ -422,7 +419,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attention_tc_kernel(const At
         bool item_ends = false;
         for (bool first = true;; first = false) {
           const int b = u & 1, key0 = c.tile * KEYS;
-          warp_wait(&ms->s_full[b], u >> 1, ms, p.status);
+          warp_wait(&ms->s_full[b], u >> 1, ms, p);
           fence_after_sync();
           float s[HALF];
           if (on) {
@@ -459,7 +456,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attention_tc_kernel(const At
                 l *= a;
               }
               if (!first) {
-                warp_wait(&ms->pv_done[(u - 1) & 1], (u - 1) >> 1, ms, p.status);
+                warp_wait(&ms->pv_done[(u - 1) & 1], (u - 1) >> 1, ms, p);
                 fence_after_sync();
 #pragma unroll
                 for (int x = 0; x < D / 2; x += 32) {
@@ -495,7 +492,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attention_tc_kernel(const At
             unpair(sum, s0, s1);
             l += s0 + s1;
             if (u >= 2) {                                          // (the buffer has been read)
-              warp_wait(&ms->pv_done[b], (u - 2) >> 1, ms, p.status);
+              warp_wait(&ms->pv_done[b], (u - 2) >> 1, ms, p);
               fence_after_sync();
             }
             tmem_st16(lanes + C::P_COL + b * KEYS + half * (HALF / 2), hi);
@@ -513,7 +510,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attention_tc_kernel(const At
         }
         // ---- the item's or the run's end
         if (!paged::same(c, end)) bring(c);
-        warp_wait(&ms->pv_done[(u - 1) & 1], (u - 1) >> 1, ms, p.status);
+        warp_wait(&ms->pv_done[(u - 1) & 1], (u - 1) >> 1, ms, p);
         fence_after_sync();
         const bool whole = item_ends && item.tile == 0;
         const int slot = item.tile == 0 ? 1 : 0;                   // pieces of a CTA: of an item it begins, of one it goes on with

@@ -38,6 +38,7 @@ struct AttnParams {
   int n_pages, max_pages, max_seqs, cap, layer;
   Div page, group_of;
   float scale_log2;
+  uint32_t wait_limit;                              // polls of a wait (ouro_paged_debug_set_wait_limit)
 };
 
 // The pool of a cache's keys or values as (dim, head, row, page, layer), boxes of 64 dims x rows in 128-byte swizzle (paged_attention.cu).

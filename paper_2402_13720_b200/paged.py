@@ -30,6 +30,11 @@ def rotary_tables(n_positions: int, head_dim: int, theta: float = 10000.0, devic
     return torch.cos(a).float(), torch.sin(a).float()
 
 
+def set_wait_limit(polls: int):
+    """Test aid: polls of the attention's bounded waits from now on, in this process (negative: the default)."""
+    _check(lib().ouro_paged_debug_set_wait_limit(polls))
+
+
 class PagedCache:
     """Pages of keys and values ``k``, ``v`` [layers, pages, page_size, kv heads, head_dim], and who names them: ``table`` [max_seqs, max_pages],
     ``lens`` [max_seqs], ``refs`` [pages], which lie side by side in ``state`` (so that a copy of ``state`` is all of it but the pages)."""

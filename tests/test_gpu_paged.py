@@ -407,6 +407,41 @@ def test_later_tokens_do_not_reach_earlier_ones(dtype, heads, d):
 
 
 @gpu
+@pytest.mark.parametrize("h,hkv,d,new,page,lens", [
+    (8, 2, 128, 1, 16, [0, 1, 700, 64, 4000]), (32, 4, 64, 2, 32, [33, 900]), (16, 2, 96, 1, 16, [300, 300]), (4, 4, 32, 1, 16, [90]),      # mma.sync
+    (64, 8, 128, 5, 64, [0, 3, 700, 64, 4000]), (32, 1, 64, 1, 16, [5000, 17]), (64, 4, 64, 16, 32, [40] * 30), (24, 1, 128, 1, 128, [9])])  # tcgen05
+def test_a_wait_that_runs_out_is_reported_and_leaves_nothing_behind(h, hkv, d, new, page, lens):
+    """The kernels return normally, the status says so, and the calls that follow give the bits they gave before."""
+    build.build()
+    cache, _ = filled("rows", page, hkv, d, torch.bfloat16, lens)
+    q = torch.randn((len(lens), new, h, d), device=DEV).to(torch.bfloat16)
+    want, lse = cache.attend(1, q, want_lse=True)
+    cache.check()
+    try:
+        for limit in (0, 0, 1, 2, 5, 20):
+            paged.set_wait_limit(limit)
+            for _ in range(3):
+                cache.attend(1, q)
+            if limit == 0:
+                with pytest.raises(binding.OuroError) as e:
+                    cache.check()
+                assert e.value.status == binding.OURO_ETIMEOUT
+            paged.set_wait_limit(-1)
+            got, got_lse = cache.attend(1, q, want_lse=True)
+            if limit == 0:
+                cache.check()
+            else:                                          # (so few polls may or may not do)
+                try:
+                    cache.check()
+                except binding.OuroError as err:
+                    assert err.status == binding.OURO_ETIMEOUT
+            assert torch.equal(got, want) and torch.equal(got_lse, lse)
+    finally:
+        paged.set_wait_limit(-1)
+    cache.check()
+
+
+@gpu
 def test_missing_and_foreign_pages_are_left_out():
     build.build()
     cache, table = filled("rows", 16, 2, 128, torch.bfloat16, [100, 40], garbage=False)
