@@ -141,6 +141,8 @@ class PagedCache:
     def append(self, layer: int, q, k, v, slots, positions, cos, sin, out=None):
         """Rotates the queries q [rows, heads, head_dim] (returned; ``out`` may be q) and the keys k [rows, kv heads, head_dim], and writes keys
         and values to their slots; rows with a negative slot are padding."""
+        if q.dim() != 3 or k.dim() != 3 or v.dim() != 3:
+            raise ValueError("q, k and v: [rows, heads, head_dim] is needed")
         rows, heads = q.shape[0], q.shape[1]
         q_stride, k_stride = self._rows(q, "q"), self._rows(k, "k", self.n_kv_heads)
         if self._rows(v, "v", self.n_kv_heads) != k_stride or k.shape[0] != rows or v.shape[0] != rows:

@@ -761,6 +761,21 @@ def test_python_refuses_what_does_not_fit():
 
 
 @gpu
+@pytest.mark.parametrize("q,k,v", [((5, 1, 4, 64), (5, 1, 2, 64), (5, 1, 2, 64)), ((5, 4, 64), (5, 2, 2, 64), (5, 2, 2, 64)), ((5, 4, 64), (5, 2, 64), (5, 1, 2, 64)),
+                                   ((1, 5, 4, 64), (1, 5, 2, 64), (1, 5, 2, 64)), ((5 * 4, 64), (5, 2, 64), (5, 2, 64)), ((64,), (64,), (64,))])
+def test_append_takes_rows_of_heads_only(q, k, v):
+    """Tensors as `attend` takes them, with a dimension for the new tokens, would be read as other numbers of rows and heads."""
+    build.build()
+    cache = paged.PagedCache(1, 8, 16, 2, 64, "bf16", max_seqs=4, max_pages=4)
+    cos, sin = paged.rotary_tables(16, 64)
+    q, k, v = (torch.ones(s, dtype=torch.bfloat16, device=DEV) for s in (q, k, v))
+    rows = i32(range(q.shape[0]))
+    with pytest.raises(ValueError):
+        cache.append(0, q, k, v, rows, rows, cos, sin)
+    assert not bool(cache.k.any()) and not bool(cache.v.any())
+
+
+@gpu
 def test_calls_run_on_the_current_stream():
     build.build()
     cache, table = filled("rows", 16, 2, 64, torch.bfloat16, [500, 30])
