@@ -151,7 +151,7 @@ class PagedCache:
             out = self._like(q, q.is_contiguous())
         elif out.shape != q.shape or not out.is_contiguous() or out.dtype is not q.dtype or out.device != self.device:
             raise ValueError("out has to be like q, and contiguous")
-        if cos.dtype is not torch.float32 or cos.shape != sin.shape or cos.shape[-1] * 2 != self.head_dim or not (cos.is_contiguous() and sin.is_contiguous()) \
+        if cos.dim() != 2 or cos.dtype is not torch.float32 or cos.shape != sin.shape or cos.shape[-1] * 2 != self.head_dim or not (cos.is_contiguous() and sin.is_contiguous()) \
                 or sin.dtype is not torch.float32 or cos.device != self.device or sin.device != self.device:
             raise ValueError("cos and sin are contiguous f32 tensors [positions, head_dim/2] on the cache's device")
         _check(self._L.ouro_paged_append(self._p, layer, q.data_ptr(), q_stride, k.data_ptr(), v.data_ptr(), k_stride, rows, heads,

@@ -776,6 +776,19 @@ def test_append_takes_rows_of_heads_only(q, k, v):
 
 
 @gpu
+@pytest.mark.parametrize("shape", [(32,), (1, 16, 32), (16, 1, 32), (16, 31), (0, 32), (16, 64)])
+def test_append_takes_tables_of_positions_only(shape):
+    """A single row of angles would be read as head_dim / 2 positions, beyond its end; a table with another dimension as one position."""
+    build.build()
+    cache = paged.PagedCache(1, 8, 16, 2, 64, "bf16", max_seqs=4, max_pages=4)
+    q, kv = torch.ones((3, 4, 64), dtype=torch.bfloat16, device=DEV), torch.ones((3, 2, 64), dtype=torch.bfloat16, device=DEV)
+    t = torch.ones(shape, device=DEV)
+    with pytest.raises((ValueError, binding.OuroError)):
+        cache.append(0, q, kv, kv, i32(range(3)), i32(range(3)), t, t)
+    assert not bool(cache.k.any())
+
+
+@gpu
 def test_calls_run_on_the_current_stream():
     build.build()
     cache, table = filled("rows", 16, 2, 64, torch.bfloat16, [500, 30])
