@@ -134,14 +134,16 @@ __global__ void __launch_bounds__(RETABLE_THREADS) retable_kernel(CacheDev c, co
 }
 
 // ---------------------------------------------------------------------------- planning
-// Sum over the CTA's threads in front of this one; total: of all.
+// (What an extend asks for may be more than 31 bits hold; more than there are pages is refused, so it may stop there.)
+__device__ __forceinline__ int add_up(int a, int b) { return (int)min((uint32_t)a + (uint32_t)b, (uint32_t)INT32_MAX); }
+// Sum of numbers not below 0 over the CTA's threads in front of this one; total: of all, at most INT32_MAX, and then the sums mean nothing.
 __device__ __forceinline__ int scan(int v, int *s_sums, int *total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int inc = v;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const int up = __shfl_up_sync(0xffffffffu, inc, o);
-    if (lane >= o) inc += up;
+    if (lane >= o) inc = add_up(inc, up);
   }
   __syncthreads();                                 // (the sums of an earlier call have been read)
   if (lane == 31) s_sums[warp] = inc;
@@ -151,10 +153,10 @@ __device__ __forceinline__ int scan(int v, int *s_sums, int *total) {
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const int up = __shfl_up_sync(0xffffffffu, w, o);
-    if (lane >= o) w += up;
+    if (lane >= o) w = add_up(w, up);
   }
   *total = __shfl_sync(0xffffffffu, w, 31);
-  return inc - v + __shfl_sync(0xffffffffu, w - mine, warp);
+  return (int)((uint32_t)(inc - v) + (uint32_t)__shfl_sync(0xffffffffu, w - mine, warp));
 }
 
 // One round over the counts of ids base .. base + ROUND * PLAN_THREADS - 1: for every chosen one, in ascending order, put(rank, id).

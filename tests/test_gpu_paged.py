@@ -224,6 +224,21 @@ def test_many_long_rows_and_the_last_sharer():
     cache.check()
 
 
+@gpu
+def test_extending_by_more_than_31_bits_of_pages_is_refused():
+    """Two sequences that together ask for 2^31 pages of one token."""
+    build.build()
+    cache = paged.PagedCache(1, 8, 1, 1, 32, "bf16", max_seqs=2, max_pages=2 ** 30)
+    seqs, new = i32([0, 1]), i32([2 ** 30, 2 ** 30])
+    binding._check(cache._L.ouro_paged_extend(cache._p, seqs.data_ptr(), new.data_ptr(), 2, 2 ** 30, None, None, cache._stream()))
+    with pytest.raises(binding.OuroError) as e:
+        cache.check()
+    assert e.value.status == binding.OURO_ECAPACITY and cache.lens.tolist() == [0, 0] and not bool(cache.refs.any())
+    slots, _ = cache.extend(seqs, i32([3, 4]), 4)          # and the pages are there for who asks for less
+    assert slots.tolist() == [[0, 1, 2, -1], [3, 4, 5, 6]]
+    cache.check()
+
+
 # ---------------------------------------------------------------------------------------------- attention
 def reference(k, v, table, lens, seqs, q, scale):
     n, t, h, d = q.shape
