@@ -285,7 +285,7 @@ int ouro_debug_static_scratch(void **dev_ptr, size_t *slot_bytes);
  * side; values likewise.  Sequence s has lens[s] tokens; entries 0 .. ceil(lens[s] / page_size) - 1 of its row of the table name
  * their pages, the others are -1.  refs[p] counts the entries that name page p: continuations share the pages of what they have in
  * common, and a page is free when nobody names it.  Pages are given out lowest id first, so a cache's state is a function of the
- * calls made on it. */
+ * calls made on it.  n_pages * page_size, max_pages * page_size and the 16-byte pieces of a page of a layer are at most 2^31 - 65536. */
 enum {
   OURO_MAX_LIST = 1024,   /* sequences in one call */
   OURO_MAX_SEQS = 65536,  /* rows of a table */

@@ -15,6 +15,8 @@ constexpr int ROW_TILE = 16;         // query rows a CTA works on at a time at m
 constexpr int TC_CTAS = 160;         // the same for many query rows to a kv head: one per SM
 constexpr int TC_ROWS = 128;
 constexpr int TEXT_DIM = 128;        // largest head dim
+// Tokens of a pool, of a row of the table, and 16-byte pieces of a page: kernels round them up to tiles and step over them in 32 bits.
+constexpr int MAX_TOKENS = INT32_MAX - 65535;
 
 // Workspace: counters that are zero between calls, then what a call needs while it runs.
 struct Layout {
@@ -59,8 +61,10 @@ inline const char *wrong_shape(const ouro_paged_cache *c) {
   if (c->head_dim < 32 || c->head_dim > TEXT_DIM || c->head_dim % 32) return "head_dim is not 32, 64, 96 or 128";
   if (c->dtype != OURO_F32 && c->dtype != OURO_BF16) return "dtype is neither OURO_F32 nor OURO_BF16";
   if (c->max_seqs > OURO_MAX_SEQS) return "max_seqs is above OURO_MAX_SEQS";
-  if ((int64_t)c->n_pages * c->page_size > INT32_MAX) return "n_pages * page_size is above 2^31 - 1";
-  if ((int64_t)c->max_pages * c->page_size > INT32_MAX) return "max_pages * page_size is above 2^31 - 1";
+  if ((int64_t)c->n_pages * c->page_size > MAX_TOKENS) return "n_pages * page_size is above 2^31 - 65536";
+  if ((int64_t)c->max_pages * c->page_size > MAX_TOKENS) return "max_pages * page_size is above 2^31 - 65536";
+  const int64_t row = (int64_t)c->n_kv_heads * (c->head_dim * (c->dtype == OURO_F32 ? 4 : 2) / 16);
+  if (row > MAX_TOKENS / c->page_size) return "a page of a layer is above 2^31 - 65536 pieces of 16 bytes";
   return nullptr;
 }
 inline const char *wrong(const ouro_paged_cache *c) {

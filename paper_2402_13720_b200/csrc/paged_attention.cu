@@ -855,7 +855,7 @@ extern "C" int ouro_paged_attention(const ouro_paged_cache *c, int32_t layer, co
   const int tile = (c->dtype == OURO_F32 ? 8 : 16) * WARPS, rows_of = c->dtype == OURO_F32 ? (p.rows == 1 ? 1 : p.rows <= 4 ? 4 : 8) : p.rows <= 8 ? 8 : 16;
   p.row_tiles = (p.rows + rows_of - 1) / rows_of;
   p.cap = c->max_pages * c->page_size;
-  const int64_t cost = ((int64_t)(p.cap + tile - 1) / tile + 8) * c->n_kv_heads * p.row_tiles;   // (8: no kernel's item costs more)
+  const int64_t cost = (((int64_t)p.cap + tile - 1) / tile + 8) * c->n_kv_heads * p.row_tiles;   // (8: no kernel's item costs more)
   if (cost > INT32_MAX || cost / (c->n_kv_heads * p.row_tiles) * n > INT32_MAX) return paged::refuse(CALL, "the sequences' work is above 2^31 units");
   const paged::Layout l = paged::layout(*c);
   p.k = (const uint8_t *)c->k + (int64_t)layer * c->layer_stride * esize;

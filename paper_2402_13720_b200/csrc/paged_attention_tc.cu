@@ -690,7 +690,7 @@ int launch(const ouro_paged_cache *c, AttnParams p, const Maps &maps, int box_ro
     ready[dev] = true;
   }
   p.row_tiles = (p.rows + R - 1) / R;
-  const int64_t cost = ((int64_t)(p.cap + KEYS - 1) / KEYS + ITEM_COST) * c->n_kv_heads * p.row_tiles * p.n;
+  const int64_t cost = (((int64_t)p.cap + KEYS - 1) / KEYS + ITEM_COST) * c->n_kv_heads * p.row_tiles * p.n;
   const int64_t most = sms < paged::TC_CTAS ? sms : paged::TC_CTAS, want = cost / MIN_RUN;
   const int grid = (int)(want < 1 ? 1 : want < most ? want : most);
   cudaError_t e = launch_pdl(paged_attention_tc_kernel<D>, dim3(grid), dim3(THREADS), C::BYTES, s, p, maps, box_rows);

@@ -23,7 +23,7 @@ struct CacheDev {
 CacheDev dev_of(const ouro_paged_cache *c) {
   return {c->table, c->lens, c->refs, c->status, c->n_pages, c->page_size, c->max_seqs, c->max_pages, c->max_pages * c->page_size};
 }
-__device__ __forceinline__ int pages_of(int len, int page) { return (len + page - 1) / page; }
+__device__ __forceinline__ int pages_of(int len, int page) { return len / page + (len % page != 0); }
 __device__ __forceinline__ bool page_ok(const CacheDev &c, int id) { return id >= 0 && id < c.n_pages; }
 __device__ __forceinline__ int len_of(const CacheDev &c, int seq) { return min(max(c.lens[seq], 0), c.cap); }
 

@@ -239,6 +239,84 @@ def test_extending_by_more_than_31_bits_of_pages_is_refused():
     cache.check()
 
 
+@gpu
+def test_pages_of_half_a_thousand_million_tokens():
+    """A sequence's tokens and a page's together are more than 31 bits hold: the pages of a sequence are counted all the same."""
+    build.build()
+    page = 500_000_000
+    one = torch.zeros((1, 1, 1, 1, 32), dtype=torch.bfloat16, device=DEV).expand(1, 4, page, 1, 32)     # (nobody reads it)
+    cache = paged.PagedCache(max_seqs=2, max_pages=4, k=one, v=one)
+
+    def extend(seq, n):
+        seqs, new = i32([seq]), i32([n])
+        binding._check(cache._L.ouro_paged_extend(cache._p, seqs.data_ptr(), new.data_ptr(), 1, n, None, None, cache._stream()))
+
+    extend(0, 1_200_000_000)
+    assert cache.lens.tolist() == [1_200_000_000, 0] and cache.refs.tolist() == [1, 1, 1, 0] and cache.table[0].tolist() == [0, 1, 2, -1]
+    extend(0, 800_000_000)
+    assert cache.refs.tolist() == [1, 1, 1, 1]
+    cache.fork(i32([0]), i32([1]))
+    assert cache.refs.tolist() == [2, 2, 2, 2]
+    cache.truncate(i32([0, 1]), i32([1_700_000_000, 0]))
+    assert cache.lens.tolist() == [1_700_000_000, 0] and cache.refs.tolist() == [1, 1, 1, 1]
+    cache.truncate(i32([0]), i32([0]))
+    assert not bool(cache.refs.any()) and bool((cache.table == -1).all())
+    cache.check()
+
+
+def test_sizes_near_31_bits_are_refused_on_the_host():
+    build.build()
+    L, top = binding.lib(), 2 ** 31 - 65536
+
+    def desc(**change):
+        c = binding.PagedCacheC()
+        for name, value in dict(dict(n_layers=1, n_pages=4, page_size=16, n_kv_heads=1, head_dim=32, dtype=1, max_seqs=1, max_pages=3, layer_stride=8192, page_stride=2048,
+                                     slot_stride=128, head_stride=64, k=256, v=256, table=256, lens=256, refs=256, status=256, workspace=256, workspace_bytes=1 << 50),
+                                **change).items():
+            setattr(c, name, value)
+        return C.byref(c)
+
+    for n in ("n_pages", "max_pages"):
+        assert L.ouro_paged_workspace_bytes(desc(page_size=1, **{n: top})) > 0
+        assert L.ouro_paged_workspace_bytes(desc(page_size=1, **{n: top + 1})) == 0
+        assert L.ouro_paged_workspace_bytes(desc(page_size=1, **{n: 2 ** 31 - 1})) == 0
+    assert L.ouro_paged_workspace_bytes(desc(n_pages=1, max_pages=1, page_size=top // 4)) > 0
+    assert L.ouro_paged_workspace_bytes(desc(n_pages=1, max_pages=1, page_size=top // 4 + 1)) == 0
+    assert L.ouro_paged_workspace_bytes(desc(n_kv_heads=2 ** 31 - 1)) == 0
+    # more units of work than 31 bits hold: refused, not rounded over
+    d = desc(page_size=1, max_pages=top, n_kv_heads=128)
+    assert L.ouro_paged_attention(d, 0, None, 1, 1, 256, 128 * 32, 128, 1.0, 256, None, None) == binding.OURO_EINVAL
+    assert b"2^31 units" in L.ouro_last_error(None)
+
+
+@gpu
+@pytest.mark.parametrize("h,d", [(1, 32), (4, 32), (20, 64)])
+def test_a_sequence_of_nearly_all_tokens_that_there_can_be(h, d):
+    """134 million entries that name one page over and over: units, their costs and page ids at the end of the range.  The last key is looked for twice,
+    once among equals, where the output is the mean of the values, and once alone.
+
+    2^31 keys on some 150 CTAs of 4 warps: a sum takes at most 250000 times 64 keys in a row, each rounded to 2^-24 of the sum, in l and in the output."""
+    build.build()
+    page, n = 16, 2 ** 27 - 4096
+    k, v = torch.zeros((2, 1, 2, page, 1, d), dtype=torch.bfloat16, device=DEV)
+    v[0, 0] = torch.randn((page, 1, d), device=DEV).to(torch.bfloat16)
+    v[0, 1] = 3.0
+    k[0, 1, -1, 0, 0] = 1.0                                # the last page's last key, in the first dim
+    cache = paged.PagedCache(max_seqs=1, max_pages=n, k=k, v=v)
+    cache.table.zero_()
+    cache.table[0, -1] = 1
+    cache.lens.fill_(n * page - 3)
+    q = torch.zeros((1, 1, h, d), dtype=torch.bfloat16, device=DEV)
+    mean = v[0, 0].double().mean(0)[0]
+    got = cache.attend(0, q, scale=1.0).double()
+    assert bool(((got - mean).abs() <= 2 ** -8 * mean.abs() + 2 * 250000 * 2 ** -24 * float(v[0, 0].abs().max())).all())
+    k[0, 1, -4, 0, 0] = 1.0                                # the last key of the sequence, and one behind its end
+    q[..., 0] = 64.0
+    v[0, 1, -4] = 7.0
+    assert bool((cache.attend(0, q, scale=1.0) == 7.0).all())      # e^64 for 2^31 others: 3e-19 of it is theirs
+    cache.check()
+
+
 # ---------------------------------------------------------------------------------------------- attention
 def reference(k, v, table, lens, seqs, q, scale):
     n, t, h, d = q.shape
