@@ -40,6 +40,10 @@ inline Layout layout(const ouro_paged_cache &c) {
   return l;
 }
 
+// Arrays of 32-bit numbers (NULL where one may be left out).
+template <typename... P>
+inline bool words(const P *...p) { return ((((uintptr_t)p % 4) == 0) && ...); }
+
 inline int refuse(const char *call, const char *why, int code = OURO_EINVAL) {
   ouro_set_global_error(std::string(call) + ": " + why);
   return code;
@@ -71,7 +75,7 @@ inline const char *wrong(const ouro_paged_cache *c) {
   if (const char *w = wrong_shape(c)) return w;
   if (!c->k || !c->v || !c->table || !c->lens || !c->refs || !c->status || !c->workspace) return "a pointer of the cache is NULL";
   if (((uintptr_t)c->k | (uintptr_t)c->v) % 16) return "k and v are not 16-byte aligned";
-  if (((uintptr_t)c->table | (uintptr_t)c->lens | (uintptr_t)c->refs | (uintptr_t)c->status) % 4) return "table, lens, refs and status are not 4-byte aligned";
+  if (!words(c->table, c->lens, c->refs, c->status)) return "table, lens, refs and status are not 4-byte aligned";
   if ((uintptr_t)c->workspace % 256) return "the workspace is not 256-byte aligned";
   const int64_t unit = c->dtype == OURO_F32 ? 4 : 8;
   if (c->layer_stride % unit || c->page_stride % unit || c->slot_stride % unit || c->head_stride % unit) return "a stride is not a multiple of 16 bytes";

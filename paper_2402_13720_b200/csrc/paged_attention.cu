@@ -845,6 +845,7 @@ extern "C" int ouro_paged_attention(const ouro_paged_cache *c, int32_t layer, co
   if (!(scale > 0.f) || scale > 1e30f) return paged::refuse(CALL, "scale is not a positive number");
   if (n == 0) return OURO_OK;
   if (!q || !out) return paged::refuse(CALL, "q or out is NULL");
+  if (!paged::words(seqs, lse)) return paged::refuse(CALL, "seqs or lse is not 4-byte aligned");
   if (!seqs && n > c->max_seqs) return paged::refuse(CALL, "more sequences than the table has");
   const int esize = c->dtype == OURO_F32 ? 4 : 2;
   if (((uintptr_t)q | (uintptr_t)out) % 16 || (q_stride * esize) % 16) return paged::refuse(CALL, "q, out or q_stride is not a multiple of 16 bytes");

@@ -520,10 +520,11 @@ __global__ void __launch_bounds__(APPEND_THREADS) append_kernel(const AppendPara
   }
 }
 
-int wrong_list(const char *call, const ouro_paged_cache *c, const void *a, const void *b, int n) {
+int wrong_list(const char *call, const ouro_paged_cache *c, const int32_t *a, const int32_t *b, int n) {
   if (const char *w = paged::wrong(c)) return paged::refuse(call, w);
   if (n < 0 || n > MAX_LIST) return paged::refuse(call, "n is below 0 or above OURO_MAX_LIST");
   if (n > 0 && (!a || !b)) return paged::refuse(call, "a list is NULL");
+  if (!paged::words(a, b)) return paged::refuse(call, "a list is not 4-byte aligned");
   return OURO_OK;
 }
 
@@ -595,6 +596,7 @@ extern "C" int ouro_paged_extend(const ouro_paged_cache *c, const int32_t *seqs,
   const int rc = wrong_list(call, c, seqs, add, n);
   if (rc != OURO_OK || n == 0) return rc;
   if (width < 0) return paged::refuse(call, "width is below 0");
+  if (!paged::words(slots, positions)) return paged::refuse(call, "slots or positions are not 4-byte aligned");
   const paged::Layout l = paged::layout(*c);
   const cudaError_t e = launch_pdl(extend_plan_kernel, dim3(1), dim3(PLAN_THREADS), 0, (cudaStream_t)stream, dev_of(c), seqs, add, n, width, lists_of(c, l));
   OURO_COUNT_LAUNCH();
@@ -609,6 +611,7 @@ extern "C" int ouro_paged_extend(const ouro_paged_cache *c, const int32_t *seqs,
 extern "C" int ouro_paged_compact(const ouro_paged_cache *c, int32_t *live, void *stream) {
   const char *call = "ouro_paged_compact";
   if (const char *w = paged::wrong(c)) return paged::refuse(call, w);
+  if (!paged::words(live)) return paged::refuse(call, "live is not 4-byte aligned");
   const paged::Layout l = paged::layout(*c);
   const cudaError_t e = launch_pdl(compact_plan_kernel, dim3(1), dim3(PLAN_THREADS), 0, (cudaStream_t)stream, dev_of(c), lists_of(c, l), live);
   OURO_COUNT_LAUNCH();
@@ -627,6 +630,7 @@ extern "C" int ouro_paged_append(const ouro_paged_cache *c, int32_t layer, const
   if (rows < 0 || n_heads < 1 || n_positions < 1) return paged::refuse(call, "rows is below 0, or n_heads or n_positions below 1");
   if (rows == 0) return OURO_OK;
   if (!q || !k || !v || !slots || !positions || !cos_t || !sin_t || !q_out) return paged::refuse(call, "a pointer is NULL");
+  if (!paged::words(slots, positions)) return paged::refuse(call, "slots or positions are not 4-byte aligned");
   const int e = c->dtype == OURO_F32 ? 4 : 2;
   if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)q_out | (uintptr_t)cos_t | (uintptr_t)sin_t) % 16 || q_stride * e % 16 || kv_stride * e % 16)
     return paged::refuse(call, "an array or a stride is not a multiple of 16 bytes");

@@ -644,6 +644,7 @@ extern "C" int ouro_token_logprobs(const void *logits, int32_t dtype, int64_t ro
   if ((tokens == nullptr) != (logprob == nullptr)) return paged::refuse(call, "tokens and logprob come together");
   if ((n_top > 0) != (top_ids != nullptr) || (n_top > 0) != (top_logprobs != nullptr)) return paged::refuse(call, "the top arrays come with n_top > 0");
   if ((uintptr_t)logits % (dtype == OURO_F32 ? 4 : 2)) return paged::refuse(call, "logits is not aligned to its type");
+  if (!paged::words(tokens, logprob, entropy, top_ids, top_logprobs)) return paged::refuse(call, "tokens or an output is not 4-byte aligned");
   if (row_stride < vocab && rows > 1) return paged::refuse(call, "row_stride is below vocab");
   int dev = 0, sms = 0;
   if (!paged::device(&dev, &sms)) return paged::refuse(call, "no usable current device", OURO_ECUDA);

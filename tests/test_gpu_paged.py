@@ -815,6 +815,27 @@ def test_refusals_that_need_no_gpu():
     assert sc(rows=0) == binding.OURO_OK
 
 
+def test_arrays_of_words_have_to_be_aligned():
+    build.build()
+    L, W = binding.lib(), 256
+    d = binding.PagedCacheC(n_layers=1, n_pages=4, page_size=16, n_kv_heads=2, head_dim=64, dtype=1, max_seqs=2, max_pages=3, layer_stride=8192, page_stride=2048, slot_stride=128,
+                            head_stride=64, k=W, v=W, table=W, lens=W, refs=W, status=W, workspace=W, workspace_bytes=1 << 30)
+    d = C.byref(d)
+    fork = lambda src=W, dst=W: L.ouro_paged_fork(d, src, dst, 1, None)
+    cut = lambda seqs=W, keep=W: L.ouro_paged_truncate(d, seqs, keep, 1, None)
+    extend = lambda seqs=W, new=W, slots=W, pos=W: L.ouro_paged_extend(d, seqs, new, 1, 1, slots, pos, None)
+    compact = lambda live=W: L.ouro_paged_compact(d, live, None)
+    append = lambda slots=W, pos=W: L.ouro_paged_append(d, 0, W, 128, W, W, 128, 1, 2, slots, pos, W, W, 4, 512, None)
+    attend = lambda seqs=W, lse=W: L.ouro_paged_attention(d, 0, seqs, 1, 1, W, 128, 2, 1.0, W, lse, None)
+    score = lambda tokens=W, lp=W, h=W, ids=W, top=W: L.ouro_token_logprobs(W, 0, 100, 2, 100, tokens, 1, lp, h, ids, top, None)
+    for call, names in ((fork, "src dst"), (cut, "seqs keep"), (extend, "seqs new slots pos"), (compact, "live"), (append, "slots pos"), (attend, "seqs lse"),
+                        (score, "tokens lp h ids top")):
+        for name in names.split():
+            for off in (1, 2, 3):
+                assert call(**{name: W + off}) == binding.OURO_EINVAL, (name, off)
+                assert b"4-byte" in L.ouro_last_error(None)
+
+
 def test_python_handles_need_a_gpu():
     if torch.cuda.is_available():
         pytest.skip("GPU present")
