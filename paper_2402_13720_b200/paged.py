@@ -21,6 +21,7 @@ from . import binding
 from .binding import OURO_BF16, OURO_F32, PagedCacheC, _check, current_stream, lib
 
 _DTYPES = {torch.float32: OURO_F32, torch.bfloat16: OURO_BF16}
+_NAMES = {"f32": torch.float32, "bf16": torch.bfloat16, torch.float32: torch.float32, torch.bfloat16: torch.bfloat16}
 
 
 def rotary_tables(n_positions: int, head_dim: int, theta: float = 10000.0, device="cuda:0"):
@@ -39,13 +40,15 @@ class PagedCache:
     """Pages of keys and values ``k``, ``v`` [layers, pages, page_size, kv heads, head_dim], and who names them: ``table`` [max_seqs, max_pages],
     ``lens`` [max_seqs], ``refs`` [pages], which lie side by side in ``state`` (so that a copy of ``state`` is all of it but the pages)."""
 
-    def __init__(self, n_layers: int = 0, n_pages: int = 0, page_size: int = 0, n_kv_heads: int = 0, head_dim: int = 0, dtype: str = "bf16", *,
+    def __init__(self, n_layers: int = 0, n_pages: int = 0, page_size: int = 0, n_kv_heads: int = 0, head_dim: int = 0, dtype: str | torch.dtype = "bf16", *,
                  max_seqs: int, max_pages: int, k: torch.Tensor | None = None, v: torch.Tensor | None = None, device="cuda:0"):
         """The sizes, from which pages are allocated (zeros), or tensors ``k`` and ``v`` of the caller, whose strides are kept (the last is 1)."""
         if (k is None) != (v is None):
             raise ValueError("k and v come together")
         if k is None:
-            k = torch.zeros((n_layers, n_pages, page_size, n_kv_heads, head_dim), dtype=torch.float32 if dtype == "f32" else torch.bfloat16, device=device)
+            if dtype not in _NAMES:
+                raise ValueError(f"dtype {dtype!r}: 'f32' or 'bf16' is needed")
+            k = torch.zeros((n_layers, n_pages, page_size, n_kv_heads, head_dim), dtype=_NAMES[dtype], device=device)
             v = torch.zeros_like(k)
         if k.shape != v.shape or k.dim() != 5 or k.dtype != v.dtype or k.dtype not in _DTYPES or k.stride() != v.stride() or k.stride(4) != 1:
             raise ValueError("k and v are [layers, pages, page_size, kv heads, head_dim] of one type (f32, bf16) and layout, the last dimension dense")

@@ -836,6 +836,13 @@ def test_arrays_of_words_have_to_be_aligned():
                 assert b"4-byte" in L.ouro_last_error(None)
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "float32", "f16", "fp8", torch.float16, torch.int32, None])
+def test_pages_of_a_type_that_there_is_not(dtype):
+    """(Refused before anything is allocated: no GPU is needed.)"""
+    with pytest.raises(ValueError, match="dtype"):
+        paged.PagedCache(1, 8, 16, 2, 64, dtype, max_seqs=1, max_pages=1)
+
+
 def test_python_handles_need_a_gpu():
     if torch.cuda.is_available():
         pytest.skip("GPU present")
@@ -843,6 +850,14 @@ def test_python_handles_need_a_gpu():
         paged.PagedCache(max_seqs=1, max_pages=1, k=torch.zeros(1, 1, 1, 1, 32), v=torch.zeros(1, 1, 1, 1, 32))
     with pytest.raises(ValueError):
         scores.token_logprobs(torch.zeros(1, 4))
+
+
+@gpu
+def test_pages_are_of_the_type_asked_for():
+    build.build()
+    for dtype, want in (("f32", torch.float32), ("bf16", torch.bfloat16), (torch.float32, torch.float32), (torch.bfloat16, torch.bfloat16)):
+        cache = paged.PagedCache(1, 8, 16, 2, 64, dtype, max_seqs=1, max_pages=1)
+        assert cache.k.dtype is want and cache.v.dtype is want
 
 
 @gpu
