@@ -61,12 +61,20 @@ class BeamDecoder:
             x = x + ((torch.nn.functional.silu(g) * u).to(m.torch_dtype) @ lw["w_down"].T).float()
         return self._norm(x, self.w["final_norm"]) @ self.w["lm_head"].T
 
+    def _text(self, prompt, more=(), new: int = 0):
+        """A prompt, and what follows it (`more`, or `new` tokens to come), as int32 arrays of tokens that the model has: the embedding is indexed with them."""
+        prompt, more = np.asarray(prompt, dtype=np.int32).reshape(-1), np.asarray(more, dtype=np.int32).reshape(-1)
+        if prompt.size < 1 or more.size + new < 1 or prompt.size + more.size + new > self.max_len:
+            raise ValueError("the prompt or what is to follow is empty, or the two are longer than max_len")
+        both = np.concatenate([prompt, more])
+        if both.min() < 0 or both.max() >= self.m.vocab:
+            raise ValueError(f"a token is not one of the model's {self.m.vocab}")
+        return prompt, more
+
     def search(self, prompt, max_new: int):
         """The ``beams`` best continuations of max_new tokens that a beam search finds: tokens [beams, max_new], sums of log probabilities
         [beams], best first."""
-        prompt = np.asarray(prompt, dtype=np.int32)
-        if prompt.size < 1 or prompt.size + max_new > self.max_len:
-            raise ValueError("the prompt is empty, or it and the new tokens are longer than max_len")
+        prompt, _ = self._text(prompt, new=max_new)
         m, B, c = self.m, self.beams, self.cache
         c.reset()
         ids = torch.as_tensor(prompt, device=self.device)
@@ -92,7 +100,7 @@ class BeamDecoder:
 
     def score(self, prompt, continuation):
         """Log probability and entropy of every token of a given continuation."""
-        prompt, cont = np.asarray(prompt, dtype=np.int32), np.asarray(continuation, dtype=np.int32)
+        prompt, cont = self._text(prompt, continuation)
         self.cache.reset()
         ids = torch.as_tensor(np.concatenate([prompt, cont])[:-1], device=self.device)
         logits = torch.cat([self.forward(ids[None, a: a + OURO_MAX_NEW], self.all[:1]) for a in range(0, ids.numel(), OURO_MAX_NEW)])
