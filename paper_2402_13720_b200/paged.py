@@ -166,9 +166,9 @@ class PagedCache:
         """Attention of the newest tokens of sequences ``seqs`` (None: 0, 1, ..): q [n, heads, head_dim] for one token each, or [n, t, heads,
         head_dim] for the t newest, each of which sees the keys up to its own.  Returns the output like q, with ``want_lse`` also the logarithm of
         the sum of exponentials [.., heads] f32."""
-        n, t, heads = q.shape[0], 1 if q.dim() == 3 else q.shape[1], q.shape[-2]
         if not 3 <= q.dim() <= 4:
             raise ValueError("q: [n, heads, head_dim] or [n, t, heads, head_dim] is needed")
+        n, t, heads = q.shape[0], 1 if q.dim() == 3 else q.shape[1], q.shape[-2]
         stride = self._rows(q, "q")
         if out is None:
             out = self._like(q, q.is_contiguous())

@@ -861,6 +861,15 @@ def test_pages_are_of_the_type_asked_for():
 
 
 @gpu
+@pytest.mark.parametrize("shape", [(), (64,), (4, 64), (1, 1, 1, 4, 64)])
+def test_attend_takes_three_or_four_dimensions(shape):
+    build.build()
+    cache = paged.PagedCache(1, 8, 16, 2, 64, "bf16", max_seqs=4, max_pages=4)
+    with pytest.raises(ValueError):
+        cache.attend(0, torch.zeros(shape, dtype=torch.bfloat16, device=DEV))
+
+
+@gpu
 def test_python_refuses_what_does_not_fit():
     build.build()
     cache = paged.PagedCache(1, 8, 16, 2, 64, "bf16", max_seqs=4, max_pages=4)
