@@ -48,12 +48,6 @@ inline int refuse(const char *call, const char *why, int code = OURO_EINVAL) {
   ouro_set_global_error(std::string(call) + ": " + why);
   return code;
 }
-inline int launched(const char *call) {
-  const cudaError_t e = cudaGetLastError();
-  if (e == cudaSuccess) return OURO_OK;
-  ouro_set_global_error(std::string(call) + ": " + cudaGetErrorString(e));
-  return OURO_ECUDA;
-}
 
 // Polls of the attention kernels' bounded waits.
 constexpr uint32_t WAIT_LIMIT = 1u << 22;
