@@ -342,7 +342,7 @@ int ouro_paged_append(const ouro_paged_cache *cache, int32_t layer, const void *
  * n_heads, head_dim], tokens q_stride elements apart; out [n, n_new, n_heads, head_dim] of the cache's type; lse_dev [n, n_new, n_heads]
  * (may be NULL) receives the natural logarithm of the sum of exponentials.  A token that sees no key gives zeros (lse -inf); entries of
  * the table outside 0 .. n_pages-1 are left out, and so are sequences outside the table.  Sums and maxima are held in 32 bits, probabilities
- * as two bf16 parts.  (n_new * n_heads / n_kv_heads > 16 with head dim 64 or 128, bf16 and a page_size that is a multiple of 16 takes two launches.) */
+ * as two bf16 parts (bf16: an infinity among the values that a token sees gives an infinity or NaN).  (n_new * n_heads / n_kv_heads > 16 with head dim 64 or 128, bf16 and a page_size that is a multiple of 16 takes two launches.) */
 int ouro_paged_attention(const ouro_paged_cache *cache, int32_t layer, const int32_t *seqs_dev, int32_t n, int32_t n_new, const void *q_dev,
                          int64_t q_stride, int32_t n_heads, float scale, void *out_dev, float *lse_dev, void *cuda_stream);
 

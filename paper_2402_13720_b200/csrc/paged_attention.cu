@@ -37,7 +37,7 @@ constexpr int ITEM_COST = 2;                        // what an item costs beside
 // 700 15.3, 14.2, 13.7; 16 of 512 15.1, 15.1, 13.7; one of 20000 with two kv heads 21.3, 21.2, 18.7; large calls the same.
 constexpr int SNAP = 1;                             // units in front of or behind a cut for which it is not worth its join
 constexpr int MIN_RUN = 2;                          // units for which another CTA is
-// More query rows of a kv head go to paged_attention_tc.cu (head dims 64 and 128).  us here and there: 35 rows, 34B drafts 16.8 and 16.6, 27 ragged up to 393
+// More query rows of a kv head go to paged_attention_tc.cu (head dims 64 and 128, pages of a multiple of 16).  us here and there: 35 rows, 34B drafts 16.8 and 16.6, 27 ragged up to 393
 // 27.2 and 22.2; 40 rows (70B shape), 64 ragged up to 300 40.5 and 27.1, one of 11993 34.1 and 26.8; 56 rows, two up to 4998 35.3 and 23.8; 128 rows, 8 of
 // 4096 153 and 48.6; 64 rows of head dim 64, one of 700 9.5 and 11.0.  At 16 rows: 16 of 1000 (70B) 21.2 and 27.2, of the 1.1B shape 11.7 and 18.2.
 constexpr int MMA_ROWS = 16;

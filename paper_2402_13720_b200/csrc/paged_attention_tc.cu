@@ -1,15 +1,15 @@
 // Attention of several newest tokens over a paged cache (more than 16 query rows to a kv head): tcgen05 with TMEM accumulators.
 //
 // mma.sync tiles of 16 rows read every key from L2 and shared memory once per 16 rows, and a step of 16 keys takes a warp two thousand cycles
-// whatever it does (128 rows behind 8 x 4096 keys of the 70B shape: 153 us for 21 us of keys and values, here 49).  Here a tile has up to 128 query rows
+// whatever it does (128 rows behind 8 x 4096 keys of the 70B shape: 153 us for 21 us of keys and values, here 48).  Here a tile has up to 128 query rows
 // (new tokens x query heads of a group), one TMEM lane each:
 //     S = Q K^T    128 x 64 keys, two buffers in TMEM; Q lies in TMEM as well;
 //     P            two threads per row, half of the keys each: S comes into their registers, and all that they exchange is whether a maximum grew;
 //                  P goes back to TMEM as two bf16 parts (P = hi + lo up to 2^-17, see paged_attention.cu), two buffers;
 //     O += P V     accumulates in TMEM over the units of an item.  It is rescaled only where a row's maximum grew by 2^8, so that nearly always
 //                  nothing waits for it; V is the MN-major operand and is never transposed.
-// 48 sequences of the 70B shape, up to 12345 tokens, 5 new: 228 us for 171 us of keys and values (334 with Q and P in shared memory, where a contraction
-// waits for 8 KB of operands; 214 with units of 128 keys, which cost 96 sequences of 5 tokens 48 us instead of 34 and 34B drafts 23 instead of 21).
+// 48 sequences of the 70B shape, up to 12345 tokens, 5 new: 213 us for 170 us of keys and values.  When it took 228, it took 334 with Q and P in shared
+// memory, where a contraction waits for 8 KB of operands, and 214 with units of 128 keys, which cost 96 sequences of 5 tokens 40 % and 34B drafts 10 %.
 // Warps 0-7 are the rows, warp 8 fetches (TMA straight from the pages, a box of 16, 32 or 64 rows of a page), warp 9 issues the contractions: the
 // scores of a unit before the P V of the one before it, so that the row threads always have scores to work on.  Warp 10 sees to the units at a
 // sequence's end before they are contracted.  Items, runs, pieces and their join are those of paged_attention.cu (paged_runs.cuh).
