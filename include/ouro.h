@@ -346,6 +346,30 @@ int ouro_paged_append(const ouro_paged_cache *cache, int32_t layer, const void *
 int ouro_paged_attention(const ouro_paged_cache *cache, int32_t layer, const int32_t *seqs_dev, int32_t n, int32_t n_new, const void *q_dev,
                          int64_t q_stride, int32_t n_heads, float scale, void *out_dev, float *lse_dev, void *cuda_stream);
 
+/* The same for a chunk of new tokens of each sequence, from one to thousands: prompts, and batches in which some sequences bring a piece of a prompt and
+ * others a single token.  q [rows, n_heads, head_dim], consecutive rows q_stride elements apart; sequence i's new tokens, the newest of its lens, are the
+ * rows starts_dev[i] .. starts_dev[i+1]-1 (starts_dev [n+1], not descending, within 0 .. rows; none is allowed).  Of m new tokens the t-th sees the keys
+ * 0 .. lens - m + t.  out [rows, n_heads, head_dim], lse_dev [rows, n_heads] (may be NULL): rows of no sequence are left as they are.  Tokens that see no
+ * key, missing pages and sequences outside the table as above; starts that descend or leave 0 .. rows make the call do nothing (OURO_EINVAL in the cache's
+ * status).  seqs_dev may name a sequence twice.  Two launches; a page_size that is a multiple of 8 is faster in bf16.  Sums and maxima are held in 32 bits; in
+ * bf16 a probability may go into the second product rounded to bf16, so that an output is off by up to 2^-8 of its probabilities' weighted |values| besides
+ * its own rounding.  rows * n_heads / n_kv_heads is at most 2^31 - 65536. */
+int ouro_paged_chunk_attention(const ouro_paged_cache *cache, int32_t layer, const int32_t *seqs_dev, const int32_t *starts_dev, int32_t n, int32_t rows,
+                               const void *q_dev, int64_t q_stride, int32_t n_heads, float scale, void *out_dev, float *lse_dev, void *cuda_stream);
+
+/* ouro_paged_append for other rotary positions than whole heads of half-split pairs, and without tables: the pairs of a head's first rotary_dim dims (a
+ * multiple of 16) lie side by side (interleaved = 1: 2i, 2i+1) or in halves (0: i, i + rotary_dim/2); the other dims pass.  Pair i of a row at position p is
+ * turned by p * turns[i] whole turns, computed in 64 bits, and scaled by magnitude > 0 (1 but for stretched contexts); how a context is
+ * stretched is in the turns.  Positions from 0 to 2^31-1; below 0 as outside the tables. */
+typedef struct {
+  const double *turns;                                           /* [rotary_dim/2], device memory */
+  int32_t rotary_dim, interleaved;
+  float magnitude;
+} ouro_rotary;
+int ouro_paged_append_rotary(const ouro_paged_cache *cache, int32_t layer, const void *q_dev, int64_t q_stride, const void *k_dev, const void *v_dev,
+                             int64_t kv_stride, int32_t rows, int32_t n_heads, const int32_t *slots_dev, const int32_t *positions_dev,
+                             const ouro_rotary *rotary, void *q_out_dev, void *cuda_stream);
+
 /* Test aid: how often the attention kernels' bounded waits for their own copies and contractions poll, in calls made from now on in this process (default
  * 1 << 22; negative restores it).  0 makes a wait for what is not there yet give up at once: the kernels return normally with wrong outputs, ouro_paged_status returns
  * OURO_ETIMEOUT, and the next call with the default is right again.  (Caches in f32 and with a page_size that is no multiple of 16 wait without a limit of
@@ -359,6 +383,18 @@ int ouro_paged_debug_set_wait_limit(int64_t polls);
  * nothing else gives -inf and entropy 0.  NaN or +inf in a row leaves no distribution: its log probabilities and entropy are NaN, NaN ranks first. */
 int ouro_token_logprobs(const void *logits_dev, int32_t dtype, int64_t row_stride, int32_t rows, int32_t vocab, const int32_t *tokens_dev,
                         int32_t n_top, float *logprob_dev, float *entropy_dev, int32_t *top_ids_dev, float *top_logprobs_dev, void *cuda_stream);
+
+/* Rules on which tokens may come, on rows of logits [rows, vocab] (OURO_F32 or OURO_BF16), rows row_stride elements apart, into out (rows out_stride apart; may
+ * be logits itself with the same stride).  In this order, in 32 bits, rounded once:
+ *   a token that is c > 0 times among the first lens_dev[row] (NULL: width) of the row's tokens_dev [rows, width] (rows token_stride apart; ids outside the
+ *   vocabulary count for nothing):  y = y > 0 ? y / repetition[row] : y * repetition[row], then y -= frequency[row] * c + presence[row];
+ *   y += bias[row, token] (rows bias_stride apart, 0: one row for all);
+ *   y = -inf, whatever it was, where bit token % 32 of word token / 32 of the row's allowed_dev (rows allowed_stride apart, 0: one row for all) is 0.
+ * repetition, presence, frequency [rows] f32.  Every array but logits and out may be NULL (repetition 1, the others 0 or allowed); lens and penalties come with tokens. */
+int ouro_constrain_logits(const void *logits_dev, int32_t dtype, int64_t row_stride, int32_t rows, int32_t vocab, const int32_t *tokens_dev,
+                          int64_t token_stride, int32_t width, const int32_t *lens_dev, const float *repetition_dev, const float *presence_dev,
+                          const float *frequency_dev, const float *bias_dev, int64_t bias_stride, const uint32_t *allowed_dev, int64_t allowed_stride,
+                          void *out_dev, int64_t out_stride, void *cuda_stream);
 
 #ifdef __cplusplus
 }

@@ -57,6 +57,10 @@ class PagedCacheC(C.Structure):
                [(n, C.c_void_p) for n in ("k", "v", "table", "lens", "refs", "status", "workspace")] + [("workspace_bytes", C.c_size_t)]
 
 
+class RotaryC(C.Structure):
+    _fields_ = [("turns", C.c_void_p), ("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("magnitude", C.c_float)]
+
+
 DRAFTER_FN = C.CFUNCTYPE(C.c_int, C.c_void_p, C.POINTER(C.c_int32), C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_int32))
 
 _PAGED = C.POINTER(PagedCacheC)
@@ -103,7 +107,13 @@ _SIGNATURES = {
                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]),
     "ouro_paged_attention": (C.c_int, [_PAGED, C.c_int32, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_int32, C.c_float,
                                        C.c_void_p, C.c_void_p, C.c_void_p]),
+    "ouro_paged_chunk_attention": (C.c_int, [_PAGED, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_int32, C.c_float,
+                                             C.c_void_p, C.c_void_p, C.c_void_p]),
+    "ouro_paged_append_rotary": (C.c_int, [_PAGED, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_void_p,
+                                           C.c_void_p, C.POINTER(RotaryC), C.c_void_p, C.c_void_p]),
     "ouro_paged_debug_set_wait_limit": (C.c_int, [C.c_int64]),
+    "ouro_constrain_logits": (C.c_int, [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p,
+                                        C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]),
     "ouro_token_logprobs": (C.c_int, [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p,
                                       C.c_void_p, C.c_void_p, C.c_void_p]),
     "ouro_generate": (C.c_int, [C.c_void_p, _I32P, C.c_int32, C.c_int32, C.c_int32, _I32P, _I32P, C.POINTER(StatsC)]),

@@ -1,0 +1,191 @@
+// Rules on which tokens may come, on rows of logits: penalties for tokens that a text has already, biases, grammar masks.
+//
+//     c = how often the row's history has the token
+//     y = x;  where c > 0:  y = y > 0 ? y / repetition : y * repetition,  y -= frequency * c + presence;   y += bias;   not allowed: y = -inf
+//
+// Bound by HBM: a logit is read and written once.  The counts never leave the SM: a CTA has a slice of a row, clears a count in shared memory for every
+// token of it, goes through the row's whole history (a few KB, from L2 but for the first CTA) and adds up what falls into the slice.  Its logits are asked
+// for before that and are there when the counts are.  Counts are whole numbers, so that the order of additions changes nothing.
+#include "paged.h"
+#include "row_ops.cuh"
+
+namespace {
+
+struct ConstrainParams {
+  const void *in;
+  void *out;
+  const int32_t *tokens, *lens;
+  const float *repetition, *presence, *frequency, *bias;
+  const uint32_t *allowed;
+  int64_t in_stride, out_stride, token_stride, bias_stride, allowed_stride;
+  int rows, vocab, width, slices;
+};
+constexpr int THREADS = 256;
+
+template <typename T> struct Piece;                // 16 bytes of logits
+template <> struct Piece<float> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ void unpack(const uint4 &t, float *x) {
+    x[0] = __uint_as_float(t.x); x[1] = __uint_as_float(t.y); x[2] = __uint_as_float(t.z); x[3] = __uint_as_float(t.w);
+  }
+  static __device__ __forceinline__ uint4 pack(const float *x) {
+    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+  }
+  static __device__ __forceinline__ float get(const float *p) { return *p; }
+  static __device__ __forceinline__ void put(float *p, float x) { *p = x; }
+};
+template <> struct Piece<__nv_bfloat16> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ void unpack(const uint4 &t, float *x) {
+    const uint32_t w[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+  }
+  static __device__ __forceinline__ uint4 pack(const float *x) {
+    return make_uint4(rowops::pack(x[0], x[1]), rowops::pack(x[2], x[3]), rowops::pack(x[4], x[5]), rowops::pack(x[6], x[7]));
+  }
+  static __device__ __forceinline__ float get(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
+  static __device__ __forceinline__ void put(__nv_bfloat16 *p, float x) { *p = __float2bfloat16_rn(x); }
+};
+
+// A slice has U pieces a thread.  Pieces begin where the row's addresses are multiples of 16 bytes: the row's first may begin in front of it, its last
+// may end behind it; those two go element by element, and all do where the output's row is aligned differently.
+template <typename T, int U, bool COUNTS>
+__global__ void __launch_bounds__(THREADS) constrain_kernel(const ConstrainParams p) {
+  using P = Piece<T>;
+  constexpr int N = P::N, SLICE = THREADS * N * U;
+  __shared__ __align__(16) uint32_t s_count[COUNTS ? SLICE : 1];
+  const int tid = threadIdx.x, row = blockIdx.x / p.slices, slice = blockIdx.x - row * p.slices;
+  const T *in = (const T *)p.in + row * p.in_stride;
+  T *out = (T *)p.out + row * p.out_stride;
+  const int skew = (int)((uintptr_t)in % 16 / sizeof(T));          // elements of the first piece in front of the row
+  const bool alike = (int)((uintptr_t)out % 16 / sizeof(T)) == skew;
+  const int base = slice * SLICE - skew;                           // token of the slice's first element
+  if (COUNTS)
+    for (int i = tid; i < SLICE / 4; i += THREADS) ((uint4 *)s_count)[i] = make_uint4(0, 0, 0, 0);
+  pdl_wait();
+  pdl_trigger();
+  uint4 raw[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int e0 = base + (u * THREADS + tid) * N;
+    if (alike && e0 >= 0 && e0 + N <= p.vocab) raw[u] = __ldcs((const uint4 *)(in + e0));
+  }
+  float rep = 1.f, pres = 0.f, freq = 0.f;
+  if (COUNTS) {
+    __syncthreads();
+    const int len = p.lens ? min(max(p.lens[row], 0), p.width) : p.width;
+    const int32_t *told = p.tokens + row * p.token_stride;
+    for (int i = tid; i < len; i += THREADS) {
+      const int t = told[i];
+      if (t >= 0 && t < p.vocab && (uint32_t)(t - base) < (uint32_t)SLICE) atomicAdd(&s_count[t - base], 1u);
+    }
+    if (p.repetition) rep = p.repetition[row];
+    if (p.presence) pres = p.presence[row];
+    if (p.frequency) freq = p.frequency[row];
+    __syncthreads();
+  }
+  const float *bias = p.bias ? p.bias + row * p.bias_stride : nullptr;
+  const uint32_t *allowed = p.allowed ? p.allowed + row * p.allowed_stride : nullptr;
+  auto told_of = [&](float x, uint32_t c) { return (x > 0.f ? x / rep : x * rep) - fmaf(freq, (float)c, pres); };
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int local = (u * THREADS + tid) * N, e0 = base + local;
+    if (e0 >= p.vocab) break;
+    if (alike && e0 >= 0 && e0 + N <= p.vocab) {
+      float x[N];
+      P::unpack(raw[u], x);
+      if (COUNTS) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+          const uint4 c = *(const uint4 *)(s_count + local + i);
+          if (c.x | c.y | c.z | c.w) {
+            if (c.x) x[i] = told_of(x[i], c.x);
+            if (c.y) x[i + 1] = told_of(x[i + 1], c.y);
+            if (c.z) x[i + 2] = told_of(x[i + 2], c.z);
+            if (c.w) x[i + 3] = told_of(x[i + 3], c.w);
+          }
+        }
+      }
+      if (bias) {
+        if (((uintptr_t)(bias + e0) & 15) == 0) {
+#pragma unroll
+          for (int i = 0; i < N; i += 4) {
+            const float4 b = *(const float4 *)(bias + e0 + i);
+            x[i] += b.x; x[i + 1] += b.y; x[i + 2] += b.z; x[i + 3] += b.w;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < N; ++i) x[i] += bias[e0 + i];
+        }
+      }
+      if (allowed) {
+        const uint32_t bits = __funnelshift_r(allowed[e0 >> 5], allowed[(e0 + N - 1) >> 5], e0 & 31);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          if (!(bits >> i & 1)) x[i] = -INFINITY;
+      }
+      __stcs((uint4 *)(out + e0), P::pack(x));
+    } else {
+      for (int i = 0; i < N; ++i) {
+        const int e = e0 + i;
+        if (e < 0 || e >= p.vocab) continue;
+        float x = P::get(in + e);
+        if (COUNTS && s_count[local + i]) x = told_of(x, s_count[local + i]);
+        if (bias) x += bias[e];
+        if (allowed && !(allowed[e >> 5] >> (e & 31) & 1)) x = -INFINITY;
+        P::put(out + e, x);
+      }
+    }
+  }
+}
+
+template <typename T, int U>
+cudaError_t launch(ConstrainParams p, cudaStream_t s) {
+  constexpr int SLICE = THREADS * Piece<T>::N * U;
+  p.slices = (int)(((int64_t)p.vocab + Piece<T>::N - 1 + SLICE - 1) / SLICE);    // (a row may begin N - 1 elements behind its first piece)
+  const dim3 grid((unsigned)(p.slices * p.rows));
+  return p.tokens ? launch_pdl(constrain_kernel<T, U, true>, grid, dim3(THREADS), 0, s, p) : launch_pdl(constrain_kernel<T, U, false>, grid, dim3(THREADS), 0, s, p);
+}
+template <typename T>
+cudaError_t by_size(const ConstrainParams &p, int sms, cudaStream_t s) {
+  const int64_t pieces = (int64_t)p.rows * (p.vocab / Piece<T>::N + 1);
+  return pieces < (int64_t)sms * THREADS * 8 ? launch<T, 1>(p, s) : launch<T, sizeof(T) == 4 ? 8 : 4>(p, s);
+}
+
+}  // namespace
+
+extern "C" int ouro_constrain_logits(const void *logits, int32_t dtype, int64_t row_stride, int32_t rows, int32_t vocab, const int32_t *tokens,
+                                     int64_t token_stride, int32_t width, const int32_t *lens, const float *repetition, const float *presence,
+                                     const float *frequency, const float *bias, int64_t bias_stride, const uint32_t *allowed, int64_t allowed_stride,
+                                     void *out, int64_t out_stride, void *stream) {
+  const char *call = "ouro_constrain_logits";
+  if (dtype != OURO_F32 && dtype != OURO_BF16) return paged::refuse(call, "dtype is neither OURO_F32 nor OURO_BF16");
+  if (rows < 0 || rows > (1 << 24) || vocab < 1 || vocab > (1 << 28)) return paged::refuse(call, "rows is below 0 or above 2^24, or vocab below 1 or above 2^28");
+  if ((int64_t)rows * (vocab / 1024 + 2) > INT32_MAX) return paged::refuse(call, "rows * vocab is above 2^41");
+  if (rows == 0) return OURO_OK;
+  if (!logits || !out) return paged::refuse(call, "logits or out is NULL");
+  const int e = dtype == OURO_F32 ? 4 : 2;
+  if (((uintptr_t)logits | (uintptr_t)out) % e) return paged::refuse(call, "logits or out is not aligned to its type");
+  if (!paged::words(tokens, lens, repetition, presence, frequency, bias, allowed)) return paged::refuse(call, "an array of 32-bit numbers is not 4-byte aligned");
+  if (rows > 1 && (row_stride < vocab || out_stride < vocab)) return paged::refuse(call, "row_stride or out_stride is below vocab");
+  if (logits == out && rows > 1 && row_stride != out_stride) return paged::refuse(call, "out is logits, with other rows");
+  if (tokens) {
+    if (width < 0 || (rows > 1 && token_stride < width && token_stride != 0)) return paged::refuse(call, "width is below 0, or token_stride below width");
+  } else if (lens || repetition || presence || frequency) {
+    return paged::refuse(call, "lens and penalties come with tokens");
+  }
+  const int words = (vocab + 31) / 32;
+  if (bias && bias_stride != 0 && bias_stride < vocab) return paged::refuse(call, "bias_stride is neither 0 nor a row's length");
+  if (allowed && allowed_stride != 0 && allowed_stride < words) return paged::refuse(call, "allowed_stride is neither 0 nor a row's length");
+  int dev = 0, sms = 0;
+  if (!paged::device(&dev, &sms)) return paged::refuse(call, "no usable current device", OURO_ECUDA);
+  ConstrainParams p{};
+  p.in = logits; p.out = out; p.tokens = tokens; p.lens = lens;
+  p.repetition = repetition; p.presence = presence; p.frequency = frequency; p.bias = bias; p.allowed = allowed;
+  p.in_stride = row_stride; p.out_stride = out_stride; p.token_stride = token_stride; p.bias_stride = bias_stride; p.allowed_stride = allowed_stride;
+  p.rows = rows; p.vocab = vocab; p.width = width;
+  const cudaError_t r = dtype == OURO_F32 ? by_size<float>(p, sms, (cudaStream_t)stream) : by_size<__nv_bfloat16>(p, sms, (cudaStream_t)stream);
+  OURO_COUNT_LAUNCH();
+  return r == cudaSuccess ? OURO_OK : paged::refuse(call, cudaGetErrorString(r), OURO_ECUDA);
+}

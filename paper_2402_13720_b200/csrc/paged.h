@@ -14,13 +14,17 @@ constexpr int MAX_CTAS = 444;        // of the attention kernel: three per SM at
 constexpr int ROW_TILE = 16;         // query rows a CTA works on at a time at most
 constexpr int TC_CTAS = 160;         // the same for many query rows to a kv head: one per SM
 constexpr int TC_ROWS = 128;
+constexpr int CHUNK_CTAS = 320;       // of the attention kernel for chunks: two per SM
+constexpr int CHUNK_ROWS = 64;
+constexpr int CHUNK_TC_CTAS = 160;    // and of its tcgen05 form: one per SM
+constexpr int CHUNK_TC_ROWS = 256;
 constexpr int TEXT_DIM = 128;        // largest head dim
 // Tokens of a pool, of a row of the table, and 16-byte pieces of a page: kernels round them up to tiles and step over them in 32 bits.
 constexpr int MAX_TOKENS = INT32_MAX - 65535;
 
 // Workspace: counters that are zero between calls, then what a call needs while it runs.
 struct Layout {
-  size_t counters, pieces, staged, lists, bytes;
+  size_t counters, pieces, staged, lists, begins, chunk_pieces, bytes;
 };
 inline size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 inline Layout layout(const ouro_paged_cache &c) {
@@ -36,7 +40,13 @@ inline Layout layout(const ouro_paged_cache &c) {
   l.lists = up256(l.staged + rows * c.max_pages * sizeof(int));
   const size_t lists = l.lists + up256((4 * (size_t)(c.n_pages > OURO_MAX_LIST ? c.n_pages : OURO_MAX_LIST) + 64) * sizeof(int));
   const size_t attn = l.pieces + pieces;
-  l.bytes = up256(lists > attn ? lists : attn);
+  // attention for chunks: where the runs begin, and two pieces a CTA
+  l.begins = l.pieces;
+  l.chunk_pieces = up256(l.begins + CHUNK_CTAS * 4 * sizeof(int));
+  const size_t chunk_rows = (size_t)CHUNK_CTAS * CHUNK_ROWS, chunk_tc_rows = (size_t)CHUNK_TC_CTAS * CHUNK_TC_ROWS;
+  const size_t chunk = l.chunk_pieces + 2 * (chunk_rows > chunk_tc_rows ? chunk_rows : chunk_tc_rows) * (c.head_dim + 2) * sizeof(float);
+  l.bytes = lists > attn ? lists : attn;
+  l.bytes = up256(l.bytes > chunk ? l.bytes : chunk);
   return l;
 }
 

@@ -1,0 +1,336 @@
+// Attention of a chunk of new tokens for each of several sequences over a paged cache: checks of the call, the kernel for f32 and for pages that no copy
+// of the copy engine fits, and the kernel that joins what was cut.
+//
+//     o_i = sum_j e^(s_ij) v_j / sum_j e^(s_ij),   s_ij = scale q_i . k_j,   j = 0 .. len - m + i for the i-th of a sequence's m new tokens
+//
+// Four operations a query head, key and dimension: behind a few dozen query rows the contractions are what counts, not the keys' bytes.  bf16 goes to
+// paged_chunk_tc.cu.  Here a CTA has 64 query rows in shared memory, passes over the keys 64 at a time and keeps maximum, sum and output of its rows in
+// registers; all in 32 bits.  A thread has 4 rows and every sixteenth key, then 4 rows and every sixteenth group of four dims, so that a value that it
+// reads from shared memory serves four multiply-adds.
+#include "paged_chunk.cuh"
+#include "row_ops.cuh"
+
+namespace {
+
+using paged::ChunkParams;
+using paged::ChunkWalk;
+
+const char *CALL = "ouro_paged_chunk_attention";
+
+constexpr int R = paged::CHUNK_ROWS, KEYS = 64, THREADS = 256;
+constexpr int ITEM_COST = 2, SNAP = 1, MIN_RUN = 2;
+typedef paged::ChunkRuns<R, KEYS, ITEM_COST, SNAP, MIN_RUN> Share;
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
+__device__ __forceinline__ float4 load4(const float *p) { return *(const float4 *)p; }
+__device__ __forceinline__ float4 load4(const __nv_bfloat16 *p) {
+  const uint2 t = *(const uint2 *)p;
+  const float2 a = rowops::unpack(t.x), b = rowops::unpack(t.y);
+  return make_float4(a.x, a.y, b.x, b.y);
+}
+__device__ __forceinline__ void store4(float *p, float4 x) { *(float4 *)p = x; }
+__device__ __forceinline__ void store4(__nv_bfloat16 *p, float4 x) { *(uint2 *)p = make_uint2(rowops::pack(x.x, x.y), rowops::pack(x.z, x.w)); }
+__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f; }
+
+template <int D>
+struct Cfg {
+  static constexpr int PITCH = D + 4;                              // (eight threads that read eight rows meet different banks)
+  static constexpr int P_PITCH = KEYS + 4;
+  static constexpr int OFF_K = R * PITCH, OFF_V = OFF_K + KEYS * PITCH, OFF_P = OFF_V + KEYS * D, OFF_CUM = OFF_P + R * P_PITCH;
+  static constexpr int OFF_MISC = OFF_CUM + OURO_MAX_LIST + 4;
+  static constexpr int BYTES = (OFF_MISC + 64) * 4;
+};
+
+template <typename T, int D>
+__global__ void __launch_bounds__(THREADS, 2) paged_chunk_kernel(const ChunkParams p) {
+  using C = Cfg<D>;
+  constexpr int D4 = D / 4, OUT = (D4 + 15) / 16;                  // groups of four dims; those of a thread
+  extern __shared__ __align__(16) float smem[];
+  float *qs = smem, *ks = smem + C::OFF_K, *vs = smem + C::OFF_V, *ps = smem + C::OFF_P;
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+  pdl_wait();
+  pdl_trigger();
+  const Share runs(p, gridDim.x, (int *)(smem + C::OFF_CUM), (int *)(smem + C::OFF_MISC), THREADS);
+  const bool any = blockIdx.x < runs.G;
+  ChunkWalk w = runs.place(any ? blockIdx.x : runs.G);
+  const ChunkWalk end = runs.place(any ? blockIdx.x + 1 : runs.G);
+  if (tid == 0) p.begins[blockIdx.x] = paged::same(w, end) ? make_int4(-1, 0, 0, 0) : make_int4(w.s, w.head, w.rt, w.unit);
+
+  while (!paged::same(w, end)) {
+    // ---- an item, or the part of it in this run
+    const int rows = min(R, w.m * p.group - w.rt * R), part_begin = w.unit;
+    __syncthreads();                                               // (what was there has been read)
+    for (int e = tid; e < R * D4; e += THREADS) {
+      const int r = e / D4, col = e - r * D4;
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (r < rows) {
+        const int at = w.rt * R + r, tok = p.group_of.quot(at);
+        x = load4((const T *)p.q + (int64_t)(w.start + tok) * p.q_stride + (int64_t)(w.head * p.group + at - tok * p.group) * D + col * 4);
+      }
+      *(float4 *)(qs + r * C::PITCH + col * 4) = x;
+    }
+    int vis[4];
+    float m[4], l[4], o[4][OUT][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      vis[i] = ty * 4 + i < rows ? runs.sees(w, w.rt * R + ty * 4 + i) : 0;
+      m[i] = -INFINITY;
+      l[i] = 0.f;
+#pragma unroll
+      for (int x = 0; x < OUT; ++x)
+#pragma unroll
+        for (int d = 0; d < 4; ++d) o[i][x][d] = 0.f;
+    }
+    const int all_see = runs.sees(w, w.rt * R);                    // keys that every row sees
+    const int last = w.s == end.s && w.head == end.head && w.rt == end.rt ? end.unit : w.units;
+    for (; w.unit < last; ++w.unit) {
+      const int key0 = w.unit * KEYS;
+      bool missing = false;
+      __syncthreads();                                             // keys and values have been read
+      for (int e = tid; e < KEYS * D4; e += THREADS) {
+        const int r = e / D4, col = e - r * D4, key = key0 + r;
+        float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+        if (key < w.len) {
+          const int pg = p.page.quot(key), id = w.row[pg];
+          if (id >= 0 && id < p.n_pages) {
+            const int64_t at = (int64_t)id * p.page_bytes + (int64_t)(key - pg * (int)p.page.d) * p.slot_bytes + (int64_t)w.head * p.head_bytes;
+            a = load4((const T *)(p.k + at) + col * 4);
+            b = load4((const T *)(p.v + at) + col * 4);
+          } else {
+            missing = true;
+          }
+        }
+        *(float4 *)(ks + r * C::PITCH + col * 4) = a;
+        *(float4 *)(vs + r * D + col * 4) = b;
+      }
+      missing = __syncthreads_or(missing);
+      float s[4][4];                                               // [row][key tx + 16 j]
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
+#pragma unroll 4
+      for (int d = 0; d < D; d += 4) {
+        float4 a[4], b[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] = *(const float4 *)(qs + (ty * 4 + i) * C::PITCH + d);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) b[j] = *(const float4 *)(ks + (tx + 16 * j) * C::PITCH + d);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s[i][j] = fmaf(a[i].w, b[j].w, fmaf(a[i].z, b[j].z, fmaf(a[i].y, b[j].y, fmaf(a[i].x, b[j].x, s[i][j]))));
+      }
+      const bool edge = missing || key0 + KEYS > all_see;          // (the same for the CTA) not every row sees every key
+      if (edge) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int key = key0 + tx + 16 * j;
+          bool there = key < w.len;
+          if (missing && there) {
+            const int id = w.row[p.page.quot(key)];
+            there = id >= 0 && id < p.n_pages;
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (!there || key >= vis[i]) s[i][j] = -INFINITY;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float top = fmaxf(fmaxf(s[i][0], s[i][1]), fmaxf(s[i][2], s[i][3]));
+#pragma unroll
+        for (int x = 8; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+        top = fmaxf(m[i], top * p.scale_log2);
+        const float base = base_of(top), a = ex2(m[i] - base);
+        m[i] = top;
+        l[i] *= a;
+#pragma unroll
+        for (int x = 0; x < OUT; ++x)
+#pragma unroll
+          for (int d = 0; d < 4; ++d) o[i][x][d] *= a;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float y = ex2(fmaf(s[i][j], p.scale_log2, -base));
+          l[i] += y;
+          ps[(ty * 4 + i) * C::P_PITCH + tx + 16 * j] = y;
+        }
+      }
+      __syncwarp();                                                // (a warp's rows are its own)
+      // At an edge, 0 times a value that is no finite number must be 0 for the rows that do not see it.
+      auto pv = [&](auto at_edge) {
+#pragma unroll 2
+        for (int key = 0; key < KEYS; key += 4) {
+          float4 a[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) a[i] = *(const float4 *)(ps + (ty * 4 + i) * C::P_PITCH + key);
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+            for (int x = 0; x < OUT; ++x) {
+              if (tx + 16 * x >= D4) continue;
+              const float4 b = *(const float4 *)(vs + (key + kk) * D + (tx + 16 * x) * 4);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                if (decltype(at_edge)::value && key0 + key + kk >= vis[i]) continue;
+                const float y = kk == 0 ? a[i].x : kk == 1 ? a[i].y : kk == 2 ? a[i].z : a[i].w;
+                o[i][x][0] = fmaf(y, b.x, o[i][x][0]);
+                o[i][x][1] = fmaf(y, b.y, o[i][x][1]);
+                o[i][x][2] = fmaf(y, b.z, o[i][x][2]);
+                o[i][x][3] = fmaf(y, b.w, o[i][x][3]);
+              }
+            }
+        }
+      };
+      if (edge) pv(std::true_type{});
+      else pv(std::false_type{});
+      __syncwarp();
+    }
+    // ---- its end
+    const bool whole = part_begin == 0 && w.unit == w.units;
+    const int slot = part_begin == 0 ? 1 : 0;
+    float *mls = p.pieces + (int64_t)paged::CHUNK_CTAS * 2 * R * D;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = ty * 4 + i;
+#pragma unroll
+      for (int x = 8; x; x >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
+      if (r >= rows) continue;
+      const int at = w.rt * R + r, tok = p.group_of.quot(at);
+      const int64_t to = (int64_t)(w.start + tok) * p.H + w.head * p.group + at - tok * p.group, piece = ((int64_t)blockIdx.x * 2 + slot) * R + r;
+      const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
+#pragma unroll
+      for (int x = 0; x < OUT; ++x) {
+        const int col = (tx + 16 * x) * 4;
+        if (col >= D) continue;
+        if (whole) store4((T *)p.out + to * D + col, make_float4(o[i][x][0] * inv, o[i][x][1] * inv, o[i][x][2] * inv, o[i][x][3] * inv));
+        else __stcg((float4 *)(p.pieces + piece * D + col), make_float4(o[i][x][0], o[i][x][1], o[i][x][2], o[i][x][3]));
+      }
+      if (tx == 0) {
+        if (!whole) __stcg((float2 *)(mls + piece * 2), make_float2(m[i], l[i]));
+        else if (p.lse) p.lse[to] = lse_of(m[i], l[i]);
+      }
+    }
+    if (w.unit == w.units) runs.next_item(w);
+  }
+}
+
+// Items that are cut, by the first run that begins within one: its pieces are the second of the CTA before and the first of that CTA and of those behind
+// that begin within the item too.  The rows of an item are shared by gridDim.y CTAs; a thread has four columns of a row.
+constexpr int JOIN_THREADS = 128, JOIN_SLICES = 16;
+template <typename T, int ROWS, int CTAS>
+__global__ void __launch_bounds__(JOIN_THREADS) paged_chunk_join_kernel(const ChunkParams p, const int grid, const int D) {
+  pdl_wait();
+  pdl_trigger();
+  const int c = blockIdx.x + 1;
+  const int4 b = p.begins[c], before = p.begins[c - 1];
+  auto within = [&](const int4 &x) { return x.x == b.x && x.y == b.y && x.z == b.z && x.w > 0; };
+  if (b.x < 0 || b.w == 0 || within(before)) return;
+  int c1 = c;
+  while (c1 + 1 < grid && within(p.begins[c1 + 1])) ++c1;
+  const int start = p.starts[b.x], m = p.starts[b.x + 1] - start, rows = min(ROWS, m * p.group - b.z * ROWS);
+  const int r0 = rows * blockIdx.y / JOIN_SLICES, r1 = rows * (blockIdx.y + 1) / JOIN_SLICES, C4 = D / 4;
+  const float *mls = p.pieces + (int64_t)CTAS * 2 * ROWS * D;
+  for (int e = threadIdx.x; e < (r1 - r0) * C4; e += JOIN_THREADS) {
+    const int r = r0 + e / C4, col = e % C4 * 4;
+    float M = -INFINITY, L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int j = c - 1; j <= c1; ++j) {
+      const int64_t at = ((int64_t)j * 2 + (j == c - 1 ? 1 : 0)) * ROWS + r;
+      const float2 ml = __ldcg((const float2 *)(mls + at * 2));
+      const float4 y = __ldcg((const float4 *)(p.pieces + at * D + col));
+      const float mx = fmaxf(M, ml.x), base = base_of(mx), a = ex2(M - base), x = ex2(ml.x - base);
+      M = mx;
+      L = fmaf(L, a, x * ml.y);
+      o[0] = fmaf(o[0], a, x * y.x);
+      o[1] = fmaf(o[1], a, x * y.y);
+      o[2] = fmaf(o[2], a, x * y.z);
+      o[3] = fmaf(o[3], a, x * y.w);
+    }
+    const int at = b.z * ROWS + r, tok = p.group_of.quot(at);
+    const int64_t to = (int64_t)(start + tok) * p.H + b.y * p.group + at - tok * p.group;
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+    store4((T *)p.out + to * D + col, make_float4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv));
+    if (p.lse && col == 0) p.lse[to] = lse_of(M, L);
+  }
+}
+
+template <typename T, int D>
+int launch(const ChunkParams &p, int64_t cost, cudaStream_t s) {
+  using C = Cfg<D>;
+  static int fit[paged::MAX_DEVICES] = {};                         // CTAs that are resident at once, per device
+  int dev = 0, sms = 0;
+  if (!paged::device(&dev, &sms)) return paged::refuse(CALL, "no usable current device", OURO_ECUDA);
+  if (!fit[dev]) {
+    int per_sm = 0;
+    cudaError_t e = cudaFuncSetAttribute(paged_chunk_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::BYTES);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, paged_chunk_kernel<T, D>, THREADS, C::BYTES);
+    if (e != cudaSuccess) return paged::refuse(CALL, cudaGetErrorString(e), OURO_ECUDA);
+    if (per_sm < 1) return paged::refuse(CALL, "the kernel does not fit this device", OURO_ECUDA);
+    fit[dev] = min(paged::CHUNK_CTAS, sms * per_sm);
+  }
+  const int grid = (int)min((int64_t)fit[dev], max((int64_t)1, cost / MIN_RUN));
+  cudaError_t e = launch_pdl(paged_chunk_kernel<T, D>, dim3(grid), dim3(THREADS), C::BYTES, s, p);
+  OURO_COUNT_LAUNCH();
+  if (e == cudaSuccess && grid > 1) {
+    e = launch_pdl(paged_chunk_join_kernel<T, R, paged::CHUNK_CTAS>, dim3(grid - 1, JOIN_SLICES), dim3(JOIN_THREADS), 0, s, p, grid, D);
+    OURO_COUNT_LAUNCH();
+  }
+  return e == cudaSuccess ? OURO_OK : paged::refuse(CALL, cudaGetErrorString(e), OURO_ECUDA);
+}
+
+template <typename T>
+int by_dim(const ChunkParams &p, int64_t cost, cudaStream_t s) {
+  switch (p.head_dim) {
+    case 32: return launch<T, 32>(p, cost, s);
+    case 64: return launch<T, 64>(p, cost, s);
+    case 96: return launch<T, 96>(p, cost, s);
+    default: return launch<T, 128>(p, cost, s);
+  }
+}
+
+}  // namespace
+
+extern "C" int ouro_paged_chunk_attention(const ouro_paged_cache *c, int32_t layer, const int32_t *seqs, const int32_t *starts, int32_t n, int32_t rows,
+                                          const void *q, int64_t q_stride, int32_t n_heads, float scale, void *out, float *lse, void *stream) {
+  if (const char *w = paged::wrong(c)) return paged::refuse(CALL, w);
+  if (layer < 0 || layer >= c->n_layers) return paged::refuse(CALL, "no such layer");
+  if (n < 0 || n > OURO_MAX_LIST) return paged::refuse(CALL, "n is below 0 or above OURO_MAX_LIST");
+  if (rows < 0) return paged::refuse(CALL, "rows is below 0");
+  if (n_heads < 1 || n_heads % c->n_kv_heads) return paged::refuse(CALL, "n_heads is not a multiple of the cache's n_kv_heads");
+  if (!(scale > 0.f) || scale > 1e30f) return paged::refuse(CALL, "scale is not a positive number");
+  if (n == 0 || rows == 0) return OURO_OK;
+  if (!q || !out || !starts) return paged::refuse(CALL, "q, out or starts is NULL");
+  if (!paged::words(seqs, starts, lse)) return paged::refuse(CALL, "seqs, starts or lse is not 4-byte aligned");
+  if (!seqs && n > c->max_seqs) return paged::refuse(CALL, "more sequences than the table has");
+  const int esize = c->dtype == OURO_F32 ? 4 : 2;
+  if (((uintptr_t)q | (uintptr_t)out) % 16 || (q_stride * esize) % 16) return paged::refuse(CALL, "q, out or q_stride is not a multiple of 16 bytes");
+  if (q_stride < (int64_t)n_heads * c->head_dim) return paged::refuse(CALL, "q_stride is below n_heads * head_dim");
+  ChunkParams p{};
+  p.group = n_heads / c->n_kv_heads;
+  p.cap = c->max_pages * c->page_size;
+  if ((int64_t)rows * p.group > paged::MAX_TOKENS) return paged::refuse(CALL, "rows * n_heads / n_kv_heads is above 2^31 - 65536");
+  // units of the finest kind: every tile may see all keys of the longest sequence
+  const int64_t tiles = ((int64_t)rows * p.group + R - 1) / R + (n < rows ? n : rows), item = ((int64_t)p.cap + KEYS - 1) / KEYS + 8;
+  if (tiles > INT32_MAX / item / c->n_kv_heads) return paged::refuse(CALL, "the sequences' work may be above 2^31 units");
+  const paged::Layout l = paged::layout(*c);
+  p.k = (const uint8_t *)c->k + (int64_t)layer * c->layer_stride * esize;
+  p.v = (const uint8_t *)c->v + (int64_t)layer * c->layer_stride * esize;
+  p.table = c->table; p.lens = c->lens; p.seqs = seqs; p.starts = starts; p.status = c->status;
+  p.q = q; p.out = out; p.lse = lse;
+  p.begins = (int4 *)((char *)c->workspace + l.begins);
+  p.pieces = (float *)((char *)c->workspace + l.chunk_pieces);
+  p.page_bytes = c->page_stride * esize; p.slot_bytes = c->slot_stride * esize; p.head_bytes = c->head_stride * esize; p.q_stride = q_stride;
+  p.n = n; p.rows = rows; p.H = n_heads; p.Hkv = c->n_kv_heads; p.layer = layer; p.head_dim = c->head_dim;
+  p.page.set(c->page_size); p.group_of.set(p.group);
+  p.n_pages = c->n_pages; p.max_pages = c->max_pages; p.max_seqs = c->max_seqs;
+  p.scale_log2 = scale * 1.4426950408889634f;
+  p.wait_limit = paged::wait_limit.load(std::memory_order_relaxed);
+  const int64_t cost = tiles * item * c->n_kv_heads;
+  return c->dtype == OURO_F32 ? by_dim<float>(p, cost, (cudaStream_t)stream) : by_dim<__nv_bfloat16>(p, cost, (cudaStream_t)stream);
+}

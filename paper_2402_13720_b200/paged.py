@@ -4,6 +4,7 @@
     slots, positions = cache.extend(seqs, new_tokens, width)          # room for a prompt, or for the next token
     q = cache.append(layer, q, k, v, slots.view(-1), positions.view(-1), cos, sin)
     out = cache.attend(layer, q.view(n, 1, heads, head_dim), seqs)    # the newest token of every sequence
+    out = cache.attend_chunk(layer, q, starts, seqs)                  # a prompt's or several tokens of each, q [rows, heads, head_dim]
     cache.fork(parents, beams)                                        # beams[i] goes on from what parents[i] was
 
 Arguments are CUDA tensors on the cache's device (lists: int32).  Calls are enqueued on torch's current stream; all calls on one cache
@@ -141,25 +142,46 @@ class PagedCache:
             each *= t.shape[i]
         return t.shape[-2] * self.head_dim if step is None else step
 
+    def _out(self, out, q):
+        if out is None:
+            return self._like(q, q.is_contiguous())
+        if out.shape != q.shape or not out.is_contiguous() or out.dtype is not q.dtype or out.device != self.device:
+            raise ValueError("out has to be like q, and contiguous")
+        return out
+
+    def _new_rows(self, q, k, v):
+        """Distances between the rows of new queries, and of new keys and values."""
+        if q.dim() != 3 or k.dim() != 3 or v.dim() != 3:
+            raise ValueError("q, k and v: [rows, heads, head_dim] is needed")
+        q_stride, k_stride = self._rows(q, "q"), self._rows(k, "k", self.n_kv_heads)
+        if self._rows(v, "v", self.n_kv_heads) != k_stride or k.shape[0] != q.shape[0] or v.shape[0] != q.shape[0]:
+            raise ValueError("q, k and v need the same number of rows, k and v the same distance between them")
+        return q_stride, k_stride
+
     def append(self, layer: int, q, k, v, slots, positions, cos, sin, out=None):
         """Rotates the queries q [rows, heads, head_dim] (returned; ``out`` may be q) and the keys k [rows, kv heads, head_dim], and writes keys
         and values to their slots; rows with a negative slot are padding."""
-        if q.dim() != 3 or k.dim() != 3 or v.dim() != 3:
-            raise ValueError("q, k and v: [rows, heads, head_dim] is needed")
+        q_stride, k_stride = self._new_rows(q, k, v)
         rows, heads = q.shape[0], q.shape[1]
-        q_stride, k_stride = self._rows(q, "q"), self._rows(k, "k", self.n_kv_heads)
-        if self._rows(v, "v", self.n_kv_heads) != k_stride or k.shape[0] != rows or v.shape[0] != rows:
-            raise ValueError("q, k and v need the same number of rows, k and v the same distance between them")
-        if out is None:
-            out = self._like(q, q.is_contiguous())
-        elif out.shape != q.shape or not out.is_contiguous() or out.dtype is not q.dtype or out.device != self.device:
-            raise ValueError("out has to be like q, and contiguous")
+        out = self._out(out, q)
         if cos.dim() != 2 or cos.dtype is not torch.float32 or cos.shape != sin.shape or cos.shape[-1] * 2 != self.head_dim or not (cos.is_contiguous() and sin.is_contiguous()) \
                 or sin.dtype is not torch.float32 or cos.device != self.device or sin.device != self.device:
             raise ValueError("cos and sin are contiguous f32 tensors [positions, head_dim/2] on the cache's device")
         _check(self._L.ouro_paged_append(self._p, layer, q.data_ptr(), q_stride, k.data_ptr(), v.data_ptr(), k_stride, rows, heads,
                                          self._list(slots, "slots", rows), self._list(positions, "positions", rows), cos.data_ptr(), sin.data_ptr(),
                                          cos.shape[0], out.data_ptr(), self._stream()))
+        return out
+
+    def append_rotary(self, layer: int, q, k, v, slots, positions, rotary, out=None):
+        """``append`` with the positions of a ``rotary.Rotary``: interleaved pairs, part of the head, stretched contexts; no tables."""
+        q_stride, k_stride = self._new_rows(q, k, v)
+        rows, heads = q.shape[0], q.shape[1]
+        out = self._out(out, q)
+        if rotary.head_dim != self.head_dim or rotary.turns.device != self.device:
+            raise ValueError(f"rotary: positions for heads of {self.head_dim} on {self.device} are needed")
+        _check(self._L.ouro_paged_append_rotary(self._p, layer, q.data_ptr(), q_stride, k.data_ptr(), v.data_ptr(), k_stride, rows, heads,
+                                                self._list(slots, "slots", rows), self._list(positions, "positions", rows), rotary._p, out.data_ptr(),
+                                                self._stream()))
         return out
 
     def attend(self, layer: int, q, seqs=None, scale: float | None = None, out=None, want_lse: bool = False):
@@ -170,12 +192,26 @@ class PagedCache:
             raise ValueError("q: [n, heads, head_dim] or [n, t, heads, head_dim] is needed")
         n, t, heads = q.shape[0], 1 if q.dim() == 3 else q.shape[1], q.shape[-2]
         stride = self._rows(q, "q")
-        if out is None:
-            out = self._like(q, q.is_contiguous())
-        elif out.shape != q.shape or not out.is_contiguous() or out.dtype is not q.dtype or out.device != self.device:
-            raise ValueError("out has to be like q, and contiguous")
+        out = self._out(out, q)
         lse = torch.empty(q.shape[:-1], dtype=torch.float32, device=self.device) if want_lse else None
         _check(self._L.ouro_paged_attention(self._p, layer, None if seqs is None else self._list(seqs, "seqs", n), n, t, q.data_ptr(), stride, heads,
                                             1.0 / math.sqrt(self.head_dim) if scale is None else scale, out.data_ptr(),
                                             lse.data_ptr() if want_lse else None, self._stream()))
+        return (out, lse) if want_lse else out
+
+    def attend_chunk(self, layer: int, q, starts, seqs=None, scale: float | None = None, out=None, want_lse: bool = False):
+        """Attention of a chunk of the newest tokens of each of the sequences ``seqs`` (None: 0, 1, ..), from one to thousands: those of sequence i
+        are the rows starts[i] .. starts[i + 1] - 1 of q [rows, heads, head_dim]; each sees the keys up to its own.  Returns the output like q, with ``want_lse`` also
+        the logarithm of the sum of exponentials [rows, heads] f32; rows of no sequence are left as they are (in a new output: undefined)."""
+        if q.dim() != 3:
+            raise ValueError("q: [rows, heads, head_dim] is needed")
+        stride = self._rows(q, "q")
+        n = starts.numel() - 1
+        if n < 0:
+            raise ValueError("starts: one more element than there are sequences is needed")
+        out = self._out(out, q)
+        lse = torch.empty(q.shape[:-1], dtype=torch.float32, device=self.device) if want_lse else None
+        _check(self._L.ouro_paged_chunk_attention(self._p, layer, None if seqs is None else self._list(seqs, "seqs", n), self._list(starts, "starts"), n, q.shape[0],
+                                                  q.data_ptr(), stride, q.shape[1], 1.0 / math.sqrt(self.head_dim) if scale is None else scale, out.data_ptr(),
+                                                  lse.data_ptr() if want_lse else None, self._stream()))
         return (out, lse) if want_lse else out

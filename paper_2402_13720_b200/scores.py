@@ -1,4 +1,5 @@
-"""What rows of logits say about tokens: log probabilities, entropy, the best alternatives (ouro_token_logprobs of include/ouro.h)."""
+"""What rows of logits say about tokens: log probabilities, entropy, the best alternatives (ouro_token_logprobs of include/ouro.h); and rules on which
+tokens may come: penalties, biases, grammar masks (ouro_constrain_logits)."""
 from __future__ import annotations
 
 from typing import NamedTuple
@@ -34,3 +35,59 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None, n_t
                                      None if tokens is None else tokens.data_ptr(), n_top, None if tokens is None else logprob.data_ptr(), entropy.data_ptr(),
                                      None if ids is None else ids.data_ptr(), None if top is None else top.data_ptr(), current_stream(dev.index)))
     return TokenScores(logprob, entropy, ids, top)
+
+
+def allowed_words(mask: torch.Tensor) -> torch.Tensor:
+    """A mask [.., vocab] of truth values (True: may come) as the words [.., ceil(vocab / 32)] int32 that ``constrain_logits`` takes."""
+    bits = torch.nn.functional.pad(mask, (0, -mask.shape[-1] % 32)).unflatten(-1, (-1, 32))
+    words = (bits.long() << torch.arange(32, device=mask.device)).sum(-1)
+    return torch.where(words >= 1 << 31, words - (1 << 32), words).int()
+
+
+def constrain_logits(logits: torch.Tensor, *, tokens: torch.Tensor | None = None, lens: torch.Tensor | None = None, repetition: torch.Tensor | None = None,
+                     presence: torch.Tensor | None = None, frequency: torch.Tensor | None = None, bias: torch.Tensor | None = None,
+                     allowed: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """logits [rows, vocab], f32 or bf16, rows at any distance.  A token that is c > 0 times among the first lens [rows] (None: all) of the row's ``tokens``
+    [rows, width] int32 is divided (above 0) or multiplied by ``repetition`` and lowered by ``frequency`` * c + ``presence`` ([rows] f32 each); ``bias`` [vocab] or
+    [rows, vocab] f32 is added; what ``allowed`` ([words] or [rows, words] int32, see ``allowed_words``) does not allow becomes -inf.  ``out`` may be logits.
+    Enqueued on torch's current stream."""
+    if logits.dim() != 2 or logits.dtype not in _DTYPES or not logits.is_cuda or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("logits: a CUDA tensor [rows, vocab], f32 or bf16, with dense rows is needed (this library has no CPU path)")
+    rows, vocab = logits.shape
+    dev = logits.device
+    if out is None:
+        out = torch.empty_strided((rows, vocab), (vocab, 1), dtype=logits.dtype, device=dev)
+    elif out.shape != logits.shape or out.dtype is not logits.dtype or out.device != dev or (vocab > 1 and out.stride(1) != 1):
+        raise ValueError("out has to be like logits")
+
+    def of_rows(t, name, dtype, width, shared):
+        """Distance between the rows of an argument (0: one for all) and its address."""
+        if t is None:
+            return 0, None
+        if t.dtype is not dtype or t.device != dev or t.shape[-1] != width or not (t.dim() == 2 and t.shape[0] == rows or shared and t.dim() == 1) or \
+                (width > 1 and t.stride(-1) != 1):
+            raise ValueError(f"{name}: [rows, {width}]{f' or [{width}]' if shared else ''} of {dtype} on {dev}, with dense rows, is needed")
+        return (t.stride(0) if t.dim() == 2 else 0), t.data_ptr()
+
+    def of_row(t, name, dtype):
+        if t is None:
+            return None
+        if t.dtype is not dtype or t.device != dev or t.dim() != 1 or t.shape[0] != rows or not t.is_contiguous():
+            raise ValueError(f"{name}: a contiguous tensor of {rows} elements of {dtype} on {dev} is needed")
+        return t.data_ptr()
+
+    width = 0 if tokens is None else tokens.shape[-1]
+    token_stride, token_p = of_rows(tokens, "tokens", torch.int32, width, False)
+    bias_stride, bias_p = of_rows(bias, "bias", torch.float32, vocab, True)
+    allowed_stride, allowed_p = of_rows(allowed, "allowed", torch.int32, (vocab + 31) // 32, True)
+    if width == 0:
+        token_p = None                                             # nothing has been said
+    per_row = [of_row(t, name, dtype) for t, name, dtype in ((lens, "lens", torch.int32), (repetition, "repetition", torch.float32),
+                                                             (presence, "presence", torch.float32), (frequency, "frequency", torch.float32))]
+    if tokens is None and any(x is not None for x in (lens, repetition, presence, frequency)):
+        raise ValueError("lens, repetition, presence and frequency come with tokens")
+    if token_p is None:
+        per_row = [None] * 4
+    _check(lib().ouro_constrain_logits(logits.data_ptr(), _DTYPES[logits.dtype], logits.stride(0), rows, vocab, token_p, token_stride, width, *per_row, bias_p,
+                                       bias_stride, allowed_p, allowed_stride, out.data_ptr(), out.stride(0), current_stream(dev.index)))
+    return out
