@@ -224,7 +224,8 @@ __global__ void __launch_bounds__(THREADS, 2) paged_chunk_kernel(const ChunkPara
 // that begin within the item too.  The rows of an item are shared by gridDim.y CTAs; a thread has four columns of a row.
 constexpr int JOIN_THREADS = 128, JOIN_SLICES = 16;
 template <typename T, int ROWS, int CTAS>
-__global__ void __launch_bounds__(JOIN_THREADS) paged_chunk_join_kernel(const ChunkParams p, const int grid, const int D) {
+__global__ void __launch_bounds__(JOIN_THREADS) paged_chunk_join_kernel(const ChunkParams p, const int grid) {
+  const int D = p.head_dim;
   pdl_wait();
   pdl_trigger();
   const int c = blockIdx.x + 1;
@@ -260,6 +261,13 @@ __global__ void __launch_bounds__(JOIN_THREADS) paged_chunk_join_kernel(const Ch
   }
 }
 
+template <typename T, int ROWS, int CTAS>
+int join(const ChunkParams &p, int grid, cudaStream_t s) {
+  const cudaError_t e = launch_pdl(paged_chunk_join_kernel<T, ROWS, CTAS>, dim3(grid - 1, JOIN_SLICES), dim3(JOIN_THREADS), 0, s, p, grid);
+  OURO_COUNT_LAUNCH();
+  return e == cudaSuccess ? OURO_OK : paged::refuse(CALL, cudaGetErrorString(e), OURO_ECUDA);
+}
+
 template <typename T, int D>
 int launch(const ChunkParams &p, int64_t cost, cudaStream_t s) {
   using C = Cfg<D>;
@@ -275,13 +283,10 @@ int launch(const ChunkParams &p, int64_t cost, cudaStream_t s) {
     fit[dev] = min(paged::CHUNK_CTAS, sms * per_sm);
   }
   const int grid = (int)min((int64_t)fit[dev], max((int64_t)1, cost / MIN_RUN));
-  cudaError_t e = launch_pdl(paged_chunk_kernel<T, D>, dim3(grid), dim3(THREADS), C::BYTES, s, p);
+  const cudaError_t e = launch_pdl(paged_chunk_kernel<T, D>, dim3(grid), dim3(THREADS), C::BYTES, s, p);
   OURO_COUNT_LAUNCH();
-  if (e == cudaSuccess && grid > 1) {
-    e = launch_pdl(paged_chunk_join_kernel<T, R, paged::CHUNK_CTAS>, dim3(grid - 1, JOIN_SLICES), dim3(JOIN_THREADS), 0, s, p, grid, D);
-    OURO_COUNT_LAUNCH();
-  }
-  return e == cudaSuccess ? OURO_OK : paged::refuse(CALL, cudaGetErrorString(e), OURO_ECUDA);
+  if (e != cudaSuccess) return paged::refuse(CALL, cudaGetErrorString(e), OURO_ECUDA);
+  return grid > 1 ? join<T, R, paged::CHUNK_CTAS>(p, grid, s) : OURO_OK;
 }
 
 template <typename T>
@@ -295,6 +300,8 @@ int by_dim(const ChunkParams &p, int64_t cost, cudaStream_t s) {
 }
 
 }  // namespace
+
+int paged::chunk_tc_join(const paged::ChunkParams &p, int grid, cudaStream_t s) { return join<__nv_bfloat16, paged::CHUNK_TC_ROWS, paged::CHUNK_TC_CTAS>(p, grid, s); }
 
 extern "C" int ouro_paged_chunk_attention(const ouro_paged_cache *c, int32_t layer, const int32_t *seqs, const int32_t *starts, int32_t n, int32_t rows,
                                           const void *q, int64_t q_stride, int32_t n_heads, float scale, void *out, float *lse, void *stream) {
@@ -332,5 +339,7 @@ extern "C" int ouro_paged_chunk_attention(const ouro_paged_cache *c, int32_t lay
   p.scale_log2 = scale * 1.4426950408889634f;
   p.wait_limit = paged::wait_limit.load(std::memory_order_relaxed);
   const int64_t cost = tiles * item * c->n_kv_heads;
+  int status = OURO_OK;
+  if (paged::chunk_tc(c, p, cost, (cudaStream_t)stream, &status)) return status;
   return c->dtype == OURO_F32 ? by_dim<float>(p, cost, (cudaStream_t)stream) : by_dim<__nv_bfloat16>(p, cost, (cudaStream_t)stream);
 }

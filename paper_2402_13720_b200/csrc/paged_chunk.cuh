@@ -28,8 +28,9 @@ struct ChunkParams {
   uint32_t wait_limit;
 };
 
-// 0: does not take the call (paged_chunk_tc.cu).
-int chunk_tc(const ouro_paged_cache *c, const ChunkParams &p, cudaStream_t s, int *status);
+// The tcgen05 kernel (paged_chunk_tc.cu); cost: the call's at most; 0: does not take the call.  And the join of its pieces (paged_chunk.cu).
+int chunk_tc(const ouro_paged_cache *c, const ChunkParams &p, int64_t cost, cudaStream_t s, int *status);
+int chunk_tc_join(const ChunkParams &p, int grid, cudaStream_t s);
 
 // A place in the list of units.
 struct ChunkWalk {
