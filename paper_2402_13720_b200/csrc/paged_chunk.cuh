@@ -44,7 +44,7 @@ template <int R, int KEYS, int ITEM_COST, int SNAP, int MIN_RUN>
 struct ChunkRuns {
   const ChunkParams &p;
   const int *s_cum;                                 // [n + 1] cost of a head of the sequences before
-  int64_t cost, G, each_run, rest;                  // cost = G * each_run + rest; G = 0: the lists are wrong
+  int cost, G, each_run, rest;                      // cost = G * each_run + rest (below 2^31: the host checks what it may be); G = 0: the lists are wrong
 
   // What is known of a sequence; no tokens outside the table.
   __device__ __forceinline__ void enter(ChunkWalk &w) const {
@@ -54,7 +54,7 @@ struct ChunkRuns {
     w.row = p.table + (int64_t)(known ? sid : 0) * p.max_pages;
     w.start = p.starts[w.s];
     w.m = p.starts[w.s + 1] - w.start;
-    w.tiles = (int)(((int64_t)w.m * p.group + R - 1) / R);
+    w.tiles = (w.m * p.group + R - 1) / R;
   }
   __device__ __forceinline__ bool wrong(const ChunkWalk &w) const { return w.start < 0 || w.m < 0 || w.start > p.rows - w.m; }
   // Keys that row r (of the sequence's m * group) sees; below 1: none.
@@ -108,9 +108,9 @@ struct ChunkRuns {
       if (lane == 0) cum[0] = 0;
     }
     __syncthreads();
-    cost = (int64_t)cum[p.n] * p.Hkv;
-    G = bad || cost == 0 ? 0 : min((int64_t)grid, max((int64_t)1, cost / MIN_RUN));
-    each_run = G ? cost / G : 0;
+    cost = cum[p.n] * p.Hkv;
+    G = bad || cost == 0 ? 0 : min(grid, max(1, cost / MIN_RUN));
+    each_run = G ? (int)((uint32_t)cost / (uint32_t)G) : 0;
     rest = cost - each_run * G;
     if (bad && blockIdx.x == 0 && tid == 0) atomicCAS(p.status, OURO_OK, OURO_EINVAL);
   }
@@ -138,17 +138,17 @@ struct ChunkRuns {
     if (++w.unit >= w.units) next_item(w);
   }
   // Where the c-th run begins, c <= G; a warp looks for it together.
-  __device__ __forceinline__ ChunkWalk place(int64_t c) const {
+  __device__ __forceinline__ ChunkWalk place(int c) const {
     ChunkWalk w{p.n};
     if (G == 0) return w;
-    const int64_t at = each_run * c + rest * c / G;                 // cost * c / G
+    const int at = each_run * c + (int)((uint32_t)(rest * c) / (uint32_t)G);    // cost * c / G
     if (at >= cost) return w;
     const int lane = threadIdx.x & 31;
     // the last sequence that begins at or in front of it and has something (sequences without tokens cost nothing)
     int lo = 0, hi = p.n;                                           // (all before lo begin in front; all from hi on behind)
     while (hi - lo > 1) {
       const int step = (hi - lo + 31) / 32, i = lo + lane * step;
-      const int k = __popc(__ballot_sync(0xffffffffu, i < hi && (int64_t)s_cum[min(i, p.n)] * p.Hkv <= at));
+      const int k = __popc(__ballot_sync(0xffffffffu, i < hi && s_cum[min(i, p.n)] * p.Hkv <= at));
       const int new_lo = lo + (k - 1) * step;
       hi = min(hi, new_lo + step);
       lo = new_lo;
@@ -156,7 +156,7 @@ struct ChunkRuns {
     w.s = lo;
     enter(w);
     const int each = s_cum[lo + 1] - s_cum[lo];
-    int in = (int)(at - (int64_t)s_cum[lo] * p.Hkv);
+    int in = at - s_cum[lo] * p.Hkv;
     w.head = in / each;
     in -= w.head * each;
     for (int t0 = 0; t0 < w.tiles; t0 += 32) {

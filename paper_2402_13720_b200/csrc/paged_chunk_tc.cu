@@ -1,16 +1,17 @@
 // Attention of chunks of new tokens over a paged cache in bf16: tcgen05 with TMEM accumulators (the formula stands in paged_chunk.cu).
 //
 // A CTA has an item's 256 query rows (new tokens x query heads of a group) as two tiles A and B of 128, one TMEM lane and one thread a row, and passes
-// over the keys 128 at a time:
-//     S = Q K^T    128 x 128 in TMEM; Q and K in shared memory;
-//     P            the row's thread has all of S in its registers, so that maximum and sum need nobody else; P goes back to TMEM as bf16, over S;
+// over the keys 64 at a time:
+//     S = Q K^T    128 x 64 in TMEM; Q and K in shared memory;
+//     P            the row's thread has all of S in its registers, so that maximum and sum need nobody else, and S is free for the next unit's scores
+//                  before the exponentials are begun; P goes back to TMEM as bf16, two buffers;
 //     O += P V     accumulates in TMEM.  It is rescaled only where a row's maximum grew by 2^8 (by the row's own thread), so that nearly always nothing
 //                  waits for it; V is the MN-major operand and is never transposed.
-// The tiles take turns: while the threads of one work on their scores, the tensor cores have the other's P V and next Q K^T.
+// TMEM is full with that: two S of 64 columns, four P of 32, two O of 128.
 // P is rounded to bf16 once.  It could go in as two bf16 parts, as it does in paged_attention_tc.cu, which is bound by memory; here that would be half as
 // many contractions again.  The rounding errors of P are independent and average out as the values do: their sum is about as large as the output's own
-// rounding (over all cases 2.3e-3 of the output's norm, 1.6e-3 of them the output's rounding).
-// Warps 0-3 and 4-7 are the rows of A and B, warp 8 issues the contractions, warp 9 fetches keys and values (TMA straight from the pages, boxes of 8 to 128 rows
+// rounding.
+// Warps 0-3 and 4-7 are the rows of A and B, warp 8 issues the contractions, warp 9 fetches keys and values (TMA straight from the pages, boxes of 8 to 64 rows
 // of a page), warps 10 and 11 bring the queries of A and B and see to the values at a sequence's end and at the causal edge before they are contracted.
 // Items, runs, pieces and their join: paged_chunk.cuh, paged_chunk.cu.
 #include <cuda.h>
@@ -23,16 +24,13 @@ using paged::ChunkParams;
 using paged::ChunkWalk;
 
 constexpr int TILE = 128, R = 2 * TILE;            // query rows of a tile, of an item
-constexpr int KEYS = 128;                          // of a unit
+constexpr int KEYS = 64;                           // of a unit
 constexpr int ROW_WARPS = 8, THREADS = 32 * (ROW_WARPS + 4);
-// The registers that the CTA is launched with, 168 a thread, as its warpgroups share them: a row's 128 scores stay in registers.
-constexpr int LAUNCH_REGS = 168, ROW_REGS = 208, OTHER_REGS = 88;
-static_assert(ROW_WARPS * ROW_REGS + (THREADS / 32 - ROW_WARPS) * OTHER_REGS <= THREADS / 32 * LAUNCH_REGS, "");
-constexpr int ITEM_COST = 2, SNAP = 1, MIN_RUN = 2;
+constexpr int ITEM_COST = 4, SNAP = 2, MIN_RUN = 4;
 typedef paged::ChunkRuns<R, KEYS, ITEM_COST, SNAP, MIN_RUN> Share;
 constexpr float GROWTH = 8.f;                      // (log2) a maximum may grow by this before sums and outputs are rescaled
 constexpr uint32_t DRAIN_POLLS = 1u << 20;         // for copies and contractions under way when their warp is done: they end by themselves
-constexpr int MAX_SLOTS = 5, ODD_SLOTS = 8;        // (whoever sees to the values is a ring ahead of the rows at most)
+constexpr int MAX_SLOTS = 12, ODD_SLOTS = 16;      // (whoever sees to the values is a ring ahead of the rows at most)
 
 struct Maps {
   CUtensorMap k, v;                                // (dim, head, row, page, layer); boxes of 64 dims x box_rows rows
@@ -42,29 +40,31 @@ struct Maps {
 template <int D>
 struct Cfg {
   static constexpr int BOXES = D / 64;
-  static constexpr int BOX = KEYS * 128;                           // bytes of 64 dims of 128 rows or keys, 128-byte swizzle
-  static constexpr int SLOT = BOXES * BOX;                         // a tile of Q, a unit's K or V: [box of 64 dims][row][128 bytes]
-  // A slot of K is free when both tiles have had their scores, one of V a step later: one more of V, so that nobody waits for it in front of K.
-  static constexpr int K_SLOTS = D == 64 ? 4 : 2, V_SLOTS = K_SLOTS + 1;
-  static constexpr int OFF_Q = 0, OFF_K = 2 * SLOT, OFF_V = OFF_K + K_SLOTS * SLOT, OFF_MISC = OFF_V + V_SLOTS * SLOT;
+  static constexpr int Q_BOX = TILE * 128, KV_BOX = KEYS * 128;    // bytes of 64 dims of all rows or keys, 128-byte swizzle
+  static constexpr int Q_TILE = BOXES * Q_BOX, SLOT = BOXES * KV_BOX;          // a tile of Q, a unit's K or V: [box of 64 dims][row][128 bytes]
+  // A slot of K is free when both tiles have had their scores, one of V two steps later.
+  static constexpr int K_SLOTS = D == 64 ? 8 : 4, V_SLOTS = K_SLOTS + 2;
+  static constexpr int OFF_Q = 0, OFF_K = 2 * Q_TILE, OFF_V = OFF_K + K_SLOTS * SLOT, OFF_MISC = OFF_V + V_SLOTS * SLOT;
   static constexpr int OFF_CUM = OFF_K;                            // [n + 1], until the first copy
-  static constexpr int BYTES = OFF_MISC + 512;
-  // TMEM columns: S (and P, two keys a column) of A and B, O of A and B
-  static constexpr int O_COL = 2 * KEYS;
+  static constexpr int BYTES = OFF_MISC + 1024;
+  // TMEM columns: S of A and B, two P (two keys a column) of A and of B, O of A and B
+  static constexpr int P_COL = 2 * KEYS, O_COL = P_COL + 2 * KEYS;
   static constexpr uint32_t COLS = 512;
-  static_assert(TILE == KEYS && V_SLOTS <= MAX_SLOTS && R == paged::CHUNK_TC_ROWS && BYTES <= 227 * 1024 && K_SLOTS * SLOT >= (OURO_MAX_LIST + 1) * 4, "");
+  static_assert(V_SLOTS <= MAX_SLOTS && V_SLOTS < ODD_SLOTS && O_COL + 256 <= 512 && R == paged::CHUNK_TC_ROWS && BYTES <= 227 * 1024 &&
+                    K_SLOTS * SLOT >= (OURO_MAX_LIST + 1) * 4, "");
 };
 
 struct Misc {
   uint64_t k_full[MAX_SLOTS], k_empty[MAX_SLOTS], v_full[MAX_SLOTS], v_ready[MAX_SLOTS], v_empty[MAX_SLOTS];
-  uint64_t q_full[2], q_free[2], s_full[2], p_full[2], o_done[2], drained;
+  uint64_t q_full[2], q_free[2], s_full[2], s_free[2], p_full[2][2], o_done[2][2], drained;   // [tile] ([buffer of P])
+  ChunkWalk places[2];                             // where the run begins and ends
   uint32_t tmem;
   int sums[THREADS / 32];
   int dead;                                        // a wait gave up: nobody issues or waits any more
   int odd[ODD_SLOTS];                              // [part mod ..]: the last part of which values that are no finite numbers were taken out, from 1
   uint32_t there[MAX_SLOTS];                       // [slot of V] blocks of 8 keys that are on pages
 };
-static_assert(sizeof(Misc) <= 512, "");
+static_assert(sizeof(Misc) <= 1024, "");
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void mbar_init(uint64_t *bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(count) : "memory"); }
@@ -85,14 +85,12 @@ __device__ __forceinline__ bool mbar_test(uint64_t *bar, uint32_t parity) {
 }
 // Bounded wait for the phase-th completion (from 0).  Whoever gives up raises the cache's status; then nobody in the CTA issues or waits any more, and the
 // call ends with wrong results and an error.
-__device__ __forceinline__ void mbar_wait_here(uint64_t *bar, uint32_t phase, Misc *ms, uint32_t limit, int *status) {
+__device__ __noinline__ void mbar_wait_on(uint64_t *bar, uint32_t phase, Misc *ms, uint32_t limit, int *status) {
   for (uint32_t i = 0; i < limit; ++i)
     if (mbar_test(bar, phase & 1) || ((i & 63) == 63 && *(volatile int *)&ms->dead)) return;
   *(volatile int *)&ms->dead = 1;
   atomicCAS(status, OURO_OK, OURO_ETIMEOUT);
 }
-// (Out of line, but for where a call would have to put a row's scores aside.)
-__device__ __forceinline__ void mbar_wait_on(uint64_t *bar, uint32_t phase, Misc *ms, uint32_t limit, int *status) { mbar_wait_here(bar, phase, ms, limit, status); }
 __device__ __forceinline__ void mbar_wait(uint64_t *bar, uint32_t phase, Misc *ms, const ChunkParams &p) {
   if (!mbar_test(bar, phase & 1)) mbar_wait_on(bar, phase, ms, p.wait_limit, p.status);
 }
@@ -198,20 +196,25 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
 __device__ __forceinline__ bool odd_pair(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }   // not finite
 
+// Where a run ends.
+struct End {
+  int s, head, rt, unit;
+  __device__ __forceinline__ bool at(const ChunkWalk &w) const { return w.unit == unit && w.rt == rt && w.head == head && w.s == s; }
+};
+
 // The part of an item that lies in a run, and what each of its tiles has to do there.
 struct Part {
   int first, last;                                 // units
-  int rows[2], units[2];                           // of the tiles: query rows; units that they see anything of (all tokens of B are later than A's)
-  __device__ __forceinline__ Part(const Share &runs, const ChunkParams &p, const ChunkWalk &w, const ChunkWalk &end) {
-    const int all = min(R, w.m * p.group - w.rt * R);
+  int rows, until_a, until_b;                      // query rows of the item; where the units end that A and B see anything of (B's tokens are later than A's)
+  __device__ __forceinline__ Part(const Share &runs, const ChunkParams &p, const ChunkWalk &w, const End &end) {
+    rows = min(R, w.m * p.group - w.rt * R);
     first = w.unit;
     last = w.s == end.s && w.head == end.head && w.rt == end.rt ? end.unit : w.units;
-    rows[0] = min(TILE, all);
-    rows[1] = all - rows[0];
-    units[0] = rows[1] > 0 ? min(w.units, max(1, (runs.sees(w, w.rt * R + TILE - 1) + KEYS - 1) / KEYS)) : w.units;
-    units[1] = rows[1] > 0 ? w.units : 0;
+    until_a = rows > TILE ? min(last, max(1, (runs.sees(w, w.rt * R + TILE - 1) + KEYS - 1) / KEYS)) : last;
+    until_b = rows > TILE ? last : 0;
   }
-  __device__ __forceinline__ int until(int t) const { return min(last, units[t]); }   // of the tile's units here
+  __device__ __forceinline__ int until(int t) const { return t == 0 ? until_a : until_b; }
+  __device__ __forceinline__ int rows_of(int t) const { return t == 0 ? min(rows, TILE) : rows - min(rows, TILE); }
 };
 
 template <int D>
@@ -233,8 +236,11 @@ __global__ void __launch_bounds__(THREADS, 1) paged_chunk_tc_kernel(const ChunkP
       mbar_init(&ms->q_full[i], 1);
       mbar_init(&ms->q_free[i], 1);
       mbar_init(&ms->s_full[i], 1);
-      mbar_init(&ms->p_full[i], ROW_WARPS / 2);
-      mbar_init(&ms->o_done[i], 1);
+      mbar_init(&ms->s_free[i], ROW_WARPS / 2);
+      mbar_init(&ms->p_full[i][0], ROW_WARPS / 2);
+      mbar_init(&ms->p_full[i][1], ROW_WARPS / 2);
+      mbar_init(&ms->o_done[i][0], 1);
+      mbar_init(&ms->o_done[i][1], 1);
     }
     mbar_init(&ms->drained, 1);
     for (int i = 0; i < ODD_SLOTS; ++i) ms->odd[i] = 0;
@@ -252,76 +258,87 @@ __global__ void __launch_bounds__(THREADS, 1) paged_chunk_tc_kernel(const ChunkP
   fence_before_sync();
   const Share runs(p, gridDim.x, (int *)(smem + C::OFF_CUM), ms->sums, THREADS);      // (two barriers)
   const bool any = blockIdx.x < runs.G;
-  ChunkWalk w = runs.place(any ? blockIdx.x : runs.G);
-  const ChunkWalk end = runs.place(any ? blockIdx.x + 1 : runs.G);
-  if (tid == 0) p.begins[blockIdx.x] = paged::same(w, end) ? make_int4(-1, 0, 0, 0) : make_int4(w.s, w.head, w.rt, w.unit);
+  if (warp < 2) {
+    const ChunkWalk x = runs.place(any ? blockIdx.x + warp : runs.G);
+    if (lane == 0) ms->places[warp] = x;
+  }
   fence_async_smem();
   __syncthreads();                                                 // (the costs lie where keys will)
   fence_after_sync();
+  ChunkWalk w = ms->places[0];
+  const End end{ms->places[1].s, ms->places[1].head, ms->places[1].rt, ms->places[1].unit};
+  if (tid == 0) p.begins[blockIdx.x] = end.at(w) ? make_int4(-1, 0, 0, 0) : make_int4(w.s, w.head, w.rt, w.unit);
   const uint32_t tmem = ms->tmem;
   volatile int *dead = &ms->dead;
 
   if (warp >= ROW_WARPS) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
-    if (paged::same(w, end)) {
+    if (end.at(w)) {
       // (nothing to do)
     } else if (warp == ROW_WARPS) {
       // ================================================================ contractions, one thread
       if (elect_one()) {
-        uint32_t ku = 0, vu = 0, parts[2] = {0, 0}, steps[2] = {0, 0};         // units so far; of the tiles: parts, P V
-        const uint64_t q0 = desc_k(sm + C::OFF_Q), k0 = desc_k(sm + C::OFF_K), v0 = desc_mn(sm + C::OFF_V, C::BOX);
-        // Scores of tile t for unit u of a part, whose keys are the ku-th.
-        auto qk = [&](int t, const Part &part, int u) {
-          if (u >= part.until(t)) return;
-          const uint32_t slot = ku % C::K_SLOTS;
-          if (u == part.first) mbar_wait(&ms->q_full[t], parts[t]++, ms, p);
-          mbar_wait(&ms->k_full[slot], ku / C::K_SLOTS, ms, p);
+        uint32_t ks = 0, kph = 0;                                  // slot and phase of the next keys
+        uint32_t va = 0, vaph = 0, vb = 0, vbph = 0;               // of the next values for A and for B
+        uint32_t parts_a = 0, parts_b = 0, scores_a = 0, scores_b = 0, steps_a = 0, steps_b = 0;       // of the tiles: parts, Q K^T, P V
+        const uint64_t q0 = desc_k(sm + C::OFF_Q), k0 = desc_k(sm + C::OFF_K), v0 = desc_mn(sm + C::OFF_V, C::KV_BOX);
+        // Scores of a tile for the next keys.
+        auto qk = [&](int t, bool first, bool last, uint32_t &parts, uint32_t &scores) {
+          if (first) mbar_wait(&ms->q_full[t], parts++, ms, p);
+          mbar_wait(&ms->k_full[ks], kph, ms, p);
+          if (scores > 0) mbar_wait(&ms->s_free[t], scores - 1, ms, p);
+          ++scores;
           fence_after_sync();
           if (*dead) return;
-          const uint64_t a = q0 + (uint32_t)(t * C::SLOT >> 4), b = k0 + (slot * C::SLOT >> 4);
+          const uint64_t a = q0 + (uint32_t)(t * C::Q_TILE >> 4), b = k0 + (ks * C::SLOT >> 4);
 #pragma unroll
-          for (int ks = 0; ks < D / 16; ++ks) {
-            const uint32_t at = ((ks >> 2) * C::BOX + (ks & 3) * 32) >> 4;
-            mma_ss(tmem + t * KEYS, a + at, b + at, idesc(KEYS, 0), ks > 0);
-          }
+          for (int k = 0; k < D / 16; ++k)
+            mma_ss(tmem + t * KEYS, a + (((k >> 2) * C::Q_BOX + (k & 3) * 32) >> 4), b + (((k >> 2) * C::KV_BOX + (k & 3) * 32) >> 4), idesc(KEYS, 0), k > 0);
           mma_commit(&ms->s_full[t]);
-          if (u + 1 == part.until(t)) mma_commit(&ms->q_free[t]);
+          if (last) mma_commit(&ms->q_free[t]);
         };
-        auto pv = [&](int t, const Part &part, int u) {
-          if (u >= part.until(t)) return;
-          const uint32_t slot = vu % C::V_SLOTS;
-          mbar_wait(&ms->p_full[t], steps[t]++, ms, p);
-          mbar_wait(&ms->v_ready[slot], vu / C::V_SLOTS, ms, p);
+        auto keys_done = [&]() {
+          mma_commit(&ms->k_empty[ks]);
+          if (++ks == C::K_SLOTS) ks = 0, ++kph;
+        };
+        // O of a tile (+)= P V with its next values.
+        auto pv = [&](int t, bool first, uint32_t v, uint32_t vph, uint32_t &steps) {
+          const uint32_t buf = steps & 1;
+          mbar_wait(&ms->p_full[t][buf], steps >> 1, ms, p);       // (the rows may be a step ahead: a barrier for each buffer)
+          mbar_wait(&ms->v_ready[v], vph, ms, p);
+          ++steps;
           fence_after_sync();
           if (*dead) return;
-          const uint64_t b = v0 + (slot * C::SLOT >> 4);
+          const uint64_t b = v0 + (v * C::SLOT >> 4);
 #pragma unroll
-          for (int kk = 0; kk < KEYS / 16; ++kk)
-            mma_ts(tmem + C::O_COL + t * 128, tmem + t * KEYS + kk * 8, b + ((kk * 2048) >> 4), idesc(D, 1), u > part.first || kk > 0);
-          mma_commit(&ms->o_done[t]);
+          for (int k = 0; k < KEYS / 16; ++k)
+            mma_ts(tmem + C::O_COL + t * 128, tmem + C::P_COL + t * KEYS + buf * (KEYS / 2) + k * 8, b + ((k * 2048) >> 4), idesc(D, 1), !first || k > 0);
+          mma_commit(&ms->o_done[t][buf]);
         };
-        Part part(runs, p, w, end);
-        int u = w.unit;
-        qk(0, part, u);
-        qk(1, part, u);
-        mma_commit(&ms->k_empty[ku % C::K_SLOTS]);
-        while (true) {
-          ++ku;
-          ChunkWalk nw = w;
-          runs.next(nw);
-          const bool more = !paged::same(nw, end);
-          const Part next = nw.unit == 0 && more ? Part(runs, p, nw, end) : part;
-          pv(0, part, u);
-          if (more) qk(0, next, nw.unit);
-          pv(1, part, u);
-          mma_commit(&ms->v_empty[vu % C::V_SLOTS]);
-          ++vu;
-          if (!more) break;
-          qk(1, next, nw.unit);
-          mma_commit(&ms->k_empty[ku % C::K_SLOTS]);
-          w = nw;
-          part = next;
-          u = w.unit;
+        auto pv_a = [&](const Part &x, int u) {
+          if (u < x.until_a) pv(0, u == x.first, va, vaph, steps_a);
+          if (++va == C::V_SLOTS) va = 0, ++vaph;
+        };
+        auto pv_b = [&](const Part &x, int u) {
+          if (u < x.until_b) pv(1, u == x.first, vb, vbph, steps_b);
+          mma_commit(&ms->v_empty[vb]);
+          if (++vb == C::V_SLOTS) vb = 0, ++vbph;
+        };
+        // The tiles are half a step apart: A's next scores, B's last P V, B's next scores, A's P V.
+        while (!end.at(w)) {
+          const Part part(runs, p, w, end);
+          if (part.first < part.until_a) qk(0, true, part.first + 1 == part.until_a, parts_a, scores_a);
+          if (part.first < part.until_b) qk(1, true, part.first + 1 == part.until_b, parts_b, scores_b);
+          keys_done();
+          for (int u = part.first; u < part.last; ++u) {
+            if (u + 1 < part.until_a) qk(0, false, u + 2 == part.until_a, parts_a, scores_a);
+            if (u > part.first) pv_b(part, u - 1);
+            if (u + 1 < part.until_b) qk(1, false, u + 2 == part.until_b, parts_b, scores_b);
+            if (u + 1 < part.last) keys_done();
+            pv_a(part, u);
+          }
+          pv_b(part, part.last - 1);
+          w.unit = part.last;
+          if (w.unit == w.units) runs.next_item(w);
         }
         mma_commit(&ms->drained);                                  // (nobody else is sure to wait for them once a wait has given up)
         for (uint32_t j = 0; j < DRAIN_POLLS && !mbar_test(&ms->drained, 0); ++j) {}
@@ -330,76 +347,88 @@ __global__ void __launch_bounds__(THREADS, 1) paged_chunk_tc_kernel(const ChunkP
       // ================================================================ fetching
       const int per = box_rows / 8;                                // blocks of 8 keys in a box, all on one page
       auto ids_of = [&](const ChunkWalk &x) {                      // page of a unit's lane-th block
-        const int key = x.unit * KEYS + (lane & 15) * 8;
+        const int key = x.unit * KEYS + (lane & 7) * 8;
         return key < x.len ? x.row[p.page.quot(key)] : -1;
       };
       int ids = ids_of(w);
-      uint32_t u = 0;
-      for (;; ++u) {
+      uint32_t ks = 0, kph = 0, vs = 0, vph = 0;                   // slots, and how often they have been filled
+      for (;;) {
         ChunkWalk nw = w;
         runs.next(nw);
-        const bool more = !paged::same(nw, end);
+        const bool more = !end.at(nw);
         const int ids_next = more ? ids_of(nw) : -1;
-        const uint32_t ks = u % C::K_SLOTS, vs = u % C::V_SLOTS;
-        if (u >= C::K_SLOTS) warp_wait(&ms->k_empty[ks], u / C::K_SLOTS - 1, ms, p);
-        if (u >= C::V_SLOTS) warp_wait(&ms->v_empty[vs], u / C::V_SLOTS - 1, ms, p);
+        if (kph > 0) warp_wait(&ms->k_empty[ks], kph - 1, ms, p);
+        if (vph > 0) warp_wait(&ms->v_empty[vs], vph - 1, ms, p);
         if (__any_sync(0xffffffffu, *dead)) break;                 // (the same for the warp: it shuffles and elects from here on)
-        const int blocks = min(16, (w.len - w.unit * KEYS + 7) / 8);           // with keys of the sequence
-        const bool on = (lane & 15) < blocks && ids >= 0 && ids < p.n_pages;
-        const uint32_t there = __ballot_sync(0xffffffffu, on) & 0xffffu;
+        const int blocks = min(KEYS / 8, (w.len - w.unit * KEYS + 7) / 8);     // with keys of the sequence
+        const bool on = (lane & 7) < blocks && ids >= 0 && ids < p.n_pages;
+        const uint32_t there = __ballot_sync(0xffffffffu, on) & 0xffu;
         const int id = on ? ids : p.n_pages;                       // beyond the pool: zeros, nothing is read
         const int boxes = blocks <= 0 ? 0 : (blocks + per - 1) / per;
         if (elect_one()) {
           ms->there[vs] = there;
-          mbar_expect(&ms->k_full[ks], boxes * per * 8 * 128 * C::BOXES);
-          mbar_expect(&ms->v_full[vs], boxes * per * 8 * 128 * C::BOXES);
+          mbar_expect(&ms->k_full[ks], boxes * box_rows * 128 * C::BOXES);
+          mbar_expect(&ms->v_full[vs], boxes * box_rows * 128 * C::BOXES);
         }
         __syncwarp();
 #pragma unroll 1
-        for (int kv = 0; kv < 2; ++kv)
-#pragma unroll 1
-          for (int b = 0; b < boxes; ++b) {
-            const int page = __shfl_sync(0xffffffffu, id, b * per);
-            if (elect_one()) {
-              const int key = w.unit * KEYS + b * box_rows, row = key - p.page.quot(key) * (int)p.page.d;
-              const uint32_t dst = sm + (kv ? C::OFF_V + vs * C::SLOT : C::OFF_K + ks * C::SLOT) + b * box_rows * 128;
+        for (int b = 0; b < boxes; ++b) {
+          const int page = __shfl_sync(0xffffffffu, id, b * per);
+          if (elect_one()) {
+            const int key = w.unit * KEYS + b * box_rows, row = key - p.page.quot(key) * (int)p.page.d;
 #pragma unroll
-              for (int x = 0; x < C::BOXES; ++x)
-                tma_load(dst + x * C::BOX, kv ? &maps.v : &maps.k, kv ? &ms->v_full[vs] : &ms->k_full[ks], x * 64, w.head, row, page, p.layer);
+            for (int x = 0; x < C::BOXES; ++x) {
+              tma_load(sm + C::OFF_K + ks * C::SLOT + x * C::KV_BOX + b * box_rows * 128, &maps.k, &ms->k_full[ks], x * 64, w.head, row, page, p.layer);
+              tma_load(sm + C::OFF_V + vs * C::SLOT + x * C::KV_BOX + b * box_rows * 128, &maps.v, &ms->v_full[vs], x * 64, w.head, row, page, p.layer);
             }
-            __syncwarp();
           }
-        if (!more) {
-          ++u;
-          break;
+          __syncwarp();
         }
+        if (++ks == C::K_SLOTS) ks = 0, ++kph;
+        if (++vs == C::V_SLOTS) vs = 0, ++vph;
+        if (!more) break;
         w = nw;
         ids = ids_next;
       }
       // Nobody else is sure to wait for the copies under way once a wait has given up, so their last phases are waited for here.
-      for (uint32_t i = u > C::V_SLOTS ? u - C::V_SLOTS : 0; i < u; ++i) {
-        for (uint32_t j = 0; j < DRAIN_POLLS && i + C::K_SLOTS >= u && !mbar_test(&ms->k_full[i % C::K_SLOTS], i / C::K_SLOTS & 1); ++j) {}
-        for (uint32_t j = 0; j < DRAIN_POLLS && !mbar_test(&ms->v_full[i % C::V_SLOTS], i / C::V_SLOTS & 1); ++j) {}
+      for (uint32_t i = 0; i < C::V_SLOTS; ++i) {
+        if (i < C::K_SLOTS && (kph > 0 || i < ks))
+          for (uint32_t j = 0; j < DRAIN_POLLS && !mbar_test(&ms->k_full[i], (kph - (i >= ks)) & 1); ++j) {}
+        if (vph > 0 || i < vs)
+          for (uint32_t j = 0; j < DRAIN_POLLS && !mbar_test(&ms->v_full[i], (vph - (i >= vs)) & 1); ++j) {}
       }
     } else {
       // ================================================================ queries; values that not every row sees
       const int t = warp - ROW_WARPS - 2;
-      uint32_t u = 0, brought = 0;
+      uint32_t slot = 0, phase = 0, brought = 0;
       int parts = 0;
-      while (!paged::same(w, end)) {
+      while (!end.at(w)) {
         const Part part(runs, p, w, end);
         ++parts;
         if (part.first < part.until(t)) {
           if (brought > 0) warp_wait(&ms->q_free[t], brought - 1, ms, p);
           ++brought;
-          constexpr int PIECES = D / 8;                            // of 16 bytes in a row
-          const int col = lane % PIECES;
-          for (int r = lane / PIECES; r < TILE; r += 32 / PIECES) {
-            const bool on = r < part.rows[t] && col * 8 < p.head_dim;
-            const int at = w.rt * R + t * TILE + (on ? r : 0), tok = p.group_of.quot(at);
-            const __nv_bfloat16 *src = (const __nv_bfloat16 *)p.q + (int64_t)(w.start + tok) * p.q_stride +
-                                       (int64_t)(w.head * p.group + at - tok * p.group) * p.head_dim + (on ? col * 8 : 0);
-            cp_async16(sm + C::OFF_Q + t * C::SLOT + (col >> 3) * C::BOX + r * 128 + (((col & 7) ^ (r & 7)) << 4), src, on);
+          // A row is D / 8 pieces of 16 bytes; the warp brings STEP rows at a time.  The place of the next ones follows from that of the last: STEP rows are
+          // so many tokens and heads further.
+          constexpr int PIECES = D / 8, STEP = 32 / PIECES;
+          const int col = lane % PIECES, rows = part.rows_of(t), at = w.rt * R + t * TILE + lane / PIECES;
+          const bool dims = col * 8 < p.head_dim;
+          int tok = p.group_of.quot(at), head = at - tok * p.group;
+          const int step_tok = p.group_of.quot(STEP), step_head = STEP - step_tok * p.group;
+          const int64_t step = step_tok * p.q_stride + (int64_t)step_head * p.head_dim, wrap = p.q_stride - (int64_t)p.group * p.head_dim;
+          const __nv_bfloat16 *src = (const __nv_bfloat16 *)p.q + (int64_t)(w.start + tok) * p.q_stride + ((int64_t)w.head * p.group + head) * p.head_dim + col * 8;
+          uint32_t dst = sm + C::OFF_Q + t * C::Q_TILE + (col >> 3) * C::Q_BOX + (lane / PIECES) * 128;
+#pragma unroll 4
+          for (int r = lane / PIECES; r < TILE; r += STEP) {
+            const bool on = r < rows && dims;
+            cp_async16(dst + (((col & 7) ^ (r & 7)) << 4), on ? src : p.q, on);
+            dst += STEP * 128;
+            src += step;
+            head += step_head;
+            if (head >= p.group) {
+              head -= p.group;
+              src += wrap;
+            }
           }
           asm volatile("cp.async.wait_all;" ::: "memory");
           fence_async_smem();
@@ -407,195 +436,232 @@ __global__ void __launch_bounds__(THREADS, 1) paged_chunk_tc_kernel(const ChunkP
           if (lane == 0) mbar_arrive(&ms->q_full[t]);
         }
         const int edge = max(0, runs.sees(w, w.rt * R));           // keys in front of it are seen by every row
-        for (; w.unit < part.last; ++w.unit, ++u) {
-          const uint32_t slot = u % C::V_SLOTS;
-          warp_wait(&ms->v_full[slot], u / C::V_SLOTS, ms, p);
+        for (; w.unit < part.last; ++w.unit) {
+          warp_wait(&ms->v_full[slot], phase, ms, p);
           const int key0 = w.unit * KEYS;
           if (key0 + KEYS > edge) {
-            uint8_t *vp = smem + C::OFF_V + slot * C::SLOT;
             // Keys that some rows do not see: 0 times their values must be 0, so what is not finite is taken out here and put in again, for the
             // rows that see it, at the part's end.  Behind the sequence's end lie other sequences' rows, or nothing.
+            // A lane has 16 bytes of every fourth key of the warp's half.  A number times 0 is 0, but for what is not finite.
+            uint8_t *vp = smem + C::OFF_V + slot * C::SLOT + t * (KEYS / 2) * 128 + lane * 16;
+            const int key = key0 + t * (KEYS / 2) + (lane >> 3);
             bool odd = false;
-            for (int e = lane; e < (KEYS / 2) * 8 * C::BOXES; e += 32) {
-              const int r = t * (KEYS / 2) + (e >> 3) / C::BOXES, key = key0 + r;
-              if (key < edge) continue;
-              uint4 *at = (uint4 *)(vp + ((e >> 3) % C::BOXES) * C::BOX + r * 128 + (e & 7) * 16);
-              if (key >= w.len) {
-                *at = make_uint4(0, 0, 0, 0);
-                continue;
-              }
-              const uint4 x = *at;
-              uint32_t v[4] = {x.x, x.y, x.z, x.w};
-              bool here = false;
 #pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (odd_pair(v[i])) {
-                  here = true;
-                  if ((v[i] & 0x7f80u) == 0x7f80u) v[i] &= 0xffff0000u;
-                  if ((v[i] & 0x7f800000u) == 0x7f800000u) v[i] &= 0xffffu;
-                }
-              if (here) *at = make_uint4(v[0], v[1], v[2], v[3]);
-              odd |= here;
+            for (int x = 0; x < C::BOXES; ++x) {
+              uint4 v[KEYS / 8];
+              __nv_bfloat162 sum = __floats2bfloat162_rn(0.f, 0.f), more = sum;
+              const __nv_bfloat162 zero = sum;
+#pragma unroll
+              for (int i = 0; i < KEYS / 8; ++i) {
+                if (key + 4 * i >= w.len) *(uint4 *)(vp + x * C::KV_BOX + i * 512) = make_uint4(0, 0, 0, 0);
+                v[i] = *(const uint4 *)(vp + x * C::KV_BOX + i * 512);
+              }
+#pragma unroll
+              for (int i = 0; i < KEYS / 8; ++i) {
+                sum = __hfma2(*(const __nv_bfloat162 *)&v[i].x, zero, sum);
+                more = __hfma2(*(const __nv_bfloat162 *)&v[i].y, zero, more);
+                sum = __hfma2(*(const __nv_bfloat162 *)&v[i].z, zero, sum);
+                more = __hfma2(*(const __nv_bfloat162 *)&v[i].w, zero, more);
+              }
+              sum = __hadd2(sum, more);
+              if (!__any_sync(0xffffffffu, odd_pair(*(const uint32_t *)&sum))) continue;
+#pragma unroll 1
+              for (int i = 0; i < KEYS / 8; ++i) {                 // (rare)
+                if (key + 4 * i < edge) continue;
+                uint4 *at = (uint4 *)(vp + x * C::KV_BOX + i * 512);
+                const uint4 y = *at;
+                uint32_t z[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                  if (odd_pair(z[c])) {
+                    odd = true;
+                    if ((z[c] & 0x7f80u) == 0x7f80u) z[c] &= 0xffff0000u;
+                    if ((z[c] & 0x7f800000u) == 0x7f800000u) z[c] &= 0xffffu;
+                  }
+                *at = make_uint4(z[0], z[1], z[2], z[3]);
+              }
             }
             if (__any_sync(0xffffffffu, odd) && lane == 0) *(volatile int *)&ms->odd[parts % ODD_SLOTS] = parts;
             fence_async_smem();
             __syncwarp();
           }
           if (lane == 0) mbar_arrive(&ms->v_ready[slot]);
+          if (++slot == C::V_SLOTS) slot = 0, ++phase;
         }
         if (__any_sync(0xffffffffu, *dead)) break;
         if (w.unit == w.units) runs.next_item(w);
       }
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(ROW_REGS));
-    {
-      // ================================================================ rows
-      const int t = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
-      const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), s_col = t * KEYS, o_col = C::O_COL + t * 128;
-      uint32_t steps = 0, units = 0;                               // the tile's; the run's
-      int parts = 0;
-      while (!paged::same(w, end)) {
-        const Part part(runs, p, w, end);
-        ++parts;
-        const int rows = part.rows[t], until = part.until(t);
-        const bool on = quarter * 32 < rows, mine = r < rows;      // the warp has rows; this thread has one
-        const int at = w.rt * R + t * TILE + (rows > 0 ? min(r, rows - 1) : 0);
-        const int tok = p.group_of.quot(at), head = w.head * p.group + at - tok * p.group;
-        const int vis = runs.sees(w, at), all_see = runs.sees(w, w.rt * R + t * TILE), edge = max(0, runs.sees(w, w.rt * R));
-        float m = -INFINITY, l = 0.f;
-        for (int u = part.first; u < until; ++u, ++steps) {
-          const int key0 = u * KEYS;
-          warp_wait(&ms->s_full[t], steps, ms, p);
-          fence_after_sync();
-          if (on) {
-            float s[KEYS];
+    // ================================================================ rows
+    const int t = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
+    const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), s_at = lanes + t * KEYS, p_at = lanes + C::P_COL + t * KEYS, o_at = lanes + C::O_COL + t * 128;
+    uint32_t steps = 0, unit0 = 0;                                 // of the tile so far; of the run, in front of the part, modulo V_SLOTS
+    int parts = 0;
+    while (!end.at(w)) {
+      const Part part(runs, p, w, end);
+      ++parts;
+      const int rows = part.rows_of(t), until = part.until(t), at0 = w.rt * R + t * TILE;
+      const bool on = quarter * 32 < rows, mine = r < rows;        // the warp has rows; this thread has one
+      const int at = at0 + (rows > 0 ? min(r, rows - 1) : 0);
+      const int vis = runs.sees(w, at), all_see = runs.sees(w, at0);
+      float m = -INFINITY, l = 0.f;
+      uint32_t there_at = unit0;
+      // A unit; cut: not every row sees every key (`there`: blocks of 8 that are on pages, n: keys in front of the row's end).
+      auto unit = [&](auto cut, int u, uint32_t there, int n) {
+        float s[KEYS];
+        tmem_ld32(s_at, s);
+        tmem_ld32(s_at + 32, s + 32);
+        tmem_ld_wait32(s);
+        tmem_ld_wait32(s + 32);
+        fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&ms->s_free[t]);
+        if (decltype(cut)::value) {
 #pragma unroll
-            for (int x = 0; x < KEYS; x += 32) tmem_ld32(lanes + s_col + x, s + x);
+          for (int x = 0; x < KEYS; x += 32) {                     // a bit for each key that the row sees
+            const int ahead = min(max(n - x, 0), 32);
+            const uint32_t bits = (uint32_t)((1ull << ahead) - 1) & ((((there >> (x / 8) & 15u) * 0x00204081u) & 0x01010101u) * 0xffu);
 #pragma unroll
-            for (int x = 0; x < KEYS; x += 32) tmem_ld_wait32(s + x);
-            const uint32_t there = *(volatile uint32_t *)&ms->there[(units + u - part.first) % C::V_SLOTS];
-            if (there != 0xffffu || key0 + KEYS > all_see) {       // (uniform) not every row sees every key
-              const int n = vis - key0;
+            for (int i = 0; i < 32; ++i) s[x + i] = bits >> i & 1 ? s[x + i] : -INFINITY;
+          }
+        }
+        float mx = max3(s[0], s[1], s[2]), my = max3(s[3], s[4], s[5]);
 #pragma unroll
-              for (int i = 0; i < KEYS; ++i)
-                if (i >= n || !(there >> (i / 8) & 1)) s[i] = -INFINITY;
+        for (int i = 6; i + 3 < KEYS; i += 4) {
+          mx = max3(mx, s[i], s[i + 1]);
+          my = max3(my, s[i + 2], s[i + 3]);
+        }
+        mx = max3(mx, s[KEYS - 2], s[KEYS - 1]);
+        const float top = fmaxf(mx, my) * p.scale_log2;
+        const bool grown = top > m + GROWTH;
+        if (__any_sync(0xffffffffu, grown)) {                      // (rare)
+          const float a = grown ? ex2(m - top) : 1.f;
+          if (grown) {
+            m = top;
+            l *= a;
+          }
+          if (u > part.first) {
+            warp_wait(&ms->o_done[t][(steps - 1) & 1], (steps - 1) >> 1, ms, p);
+            fence_after_sync();
+#pragma unroll 1
+            for (int x = 0; x < D; x += 32) {
+              float o[32];
+              tmem_ld32(o_at + x, o);
+              tmem_ld_wait32(o);
+#pragma unroll
+              for (int i = 0; i < 32; ++i) o[i] *= a;
+              tmem_st32(o_at + x, o);
             }
-            float mx = max3(s[0], s[1], s[2]), my = max3(s[3], s[4], s[5]);
-#pragma unroll
-            for (int i = 6; i + 3 < KEYS; i += 4) {
-              mx = max3(mx, s[i], s[i + 1]);
-              my = max3(my, s[i + 2], s[i + 3]);
-            }
-            mx = max3(mx, s[KEYS - 2], s[KEYS - 1]);
-            const float top = fmaxf(mx, my) * p.scale_log2;
-            const bool grown = top > m + GROWTH;
-            if (__any_sync(0xffffffffu, grown)) {                  // (rare)
-              const float a = grown ? ex2(m - top) : 1.f;
-              if (grown) {
-                m = top;
-                l *= a;
-              }
-              if (u > part.first) {
-                mbar_wait_here(&ms->o_done[t], steps - 1, ms, p.wait_limit, p.status);
-                __syncwarp();
-                fence_after_sync();
-#pragma unroll
-                for (int x = 0; x < D; x += 32) {
-                  float o[32];
-                  tmem_ld32(lanes + o_col + x, o);
-                  tmem_ld_wait32(o);
-#pragma unroll
-                  for (int i = 0; i < 32; ++i) o[i] *= a;
-                  tmem_st32(lanes + o_col + x, o);
-                }
-                tmem_st_wait();
-              }
-            }
-            const float base = -base_of(m);
-            const u64 base2 = pair(base, base), scale2 = pair(p.scale_log2, p.scale_log2);
-            u64 sum = pair(0.f, 0.f);
-#pragma unroll
-            for (int x = 0; x < KEYS; x += 32) {
-              uint32_t w16[16];
-#pragma unroll
-              for (int i = 0; i < 32; i += 2) {
-                float a, b;
-                unpair(fma2(pair(s[x + i], s[x + i + 1]), scale2, base2), a, b);
-                a = ex2(a);
-                b = ex2(b);
-                sum = add2(sum, pair(a, b));
-                w16[i / 2] = pack(a, b);
-              }
-              tmem_st16(lanes + s_col + x / 2, w16);
-            }
-            float s0, s1;
-            unpair(sum, s0, s1);
-            l += s0 + s1;
             tmem_st_wait();
           }
-          fence_before_sync();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&ms->p_full[t]);
         }
-        units += part.last - part.first;
-        // ---- the part's end
-        if (until > part.first) {
-          warp_wait(&ms->o_done[t], steps - 1, ms, p);
+        const float base = -base_of(m);
+        const u64 base2 = pair(base, base), scale2 = pair(p.scale_log2, p.scale_log2);
+        u64 sum = pair(0.f, 0.f);
+        const uint32_t buf = steps & 1;
+        if (steps >= 2) {                                          // (the buffer has been read)
+          warp_wait(&ms->o_done[t][buf], (steps - 2) >> 1, ms, p);
           fence_after_sync();
         }
+#pragma unroll
+        for (int x = 0; x < KEYS; x += 32) {
+          uint32_t w16[16];
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) {
+            float a, b;
+            unpair(fma2(pair(s[x + i], s[x + i + 1]), scale2, base2), a, b);
+            a = ex2(a);
+            b = ex2(b);
+            sum = add2(sum, pair(a, b));
+            w16[i / 2] = pack(a, b);
+          }
+          tmem_st16(p_at + buf * (KEYS / 2) + x / 2, w16);
+        }
+        tmem_st_wait();
+        fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&ms->p_full[t][buf]);
+        float s0, s1;
+        unpair(sum, s0, s1);
+        l += s0 + s1;
+      };
+      for (int u = part.first; u < until; ++u, ++steps) {
+        warp_wait(&ms->s_full[t], steps, ms, p);
+        fence_after_sync();
+        const uint32_t there = *(volatile uint32_t *)&ms->there[there_at];
+        if (++there_at == C::V_SLOTS) there_at = 0;
+        if (!on) {
+          fence_before_sync();
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(&ms->s_free[t]);
+            mbar_arrive(&ms->p_full[t][steps & 1]);
+          }
+        } else if (there == 0xffu && u * KEYS + KEYS <= all_see) {
+          unit(std::false_type{}, u, there, KEYS);
+        } else {
+          unit(std::true_type{}, u, there, vis - u * KEYS);
+        }
+      }
+      unit0 = (unit0 + part.last - part.first) % C::V_SLOTS;
+      // ---- the part's end
+      if (until > part.first) {
+        warp_wait(&ms->o_done[t][(steps - 1) & 1], (steps - 1) >> 1, ms, p);
+        fence_after_sync();
+      }
+      if (on) {
         const bool whole = part.first == 0 && part.last == w.units;
         const int slot = part.first == 0 ? 1 : 0;                  // pieces of a CTA: of an item it begins, of one it goes on with
-        float *mls = p.pieces + (int64_t)paged::CHUNK_TC_CTAS * 2 * R * p.head_dim;
-        if (on) {
-          const int64_t to = (int64_t)(w.start + tok) * p.H + head, piece = ((int64_t)blockIdx.x * 2 + slot) * R + t * TILE + r;
-          const float inv = l == 0.f ? 0.f : 1.f / l;
-          const bool odd = *(volatile int *)&ms->odd[parts % ODD_SLOTS] == parts;
+        int mine_at = at;
+        asm volatile("" : "+r"(mine_at));                          // (so that what follows is not worked out before the units and kept)
+        const int tok = p.group_of.quot(mine_at), head = w.head * p.group + mine_at - tok * p.group, edge = max(0, runs.sees(w, w.rt * R));
+        const int64_t to = (int64_t)(w.start + tok) * p.H + head, piece = ((int64_t)blockIdx.x * 2 + slot) * R + mine_at - w.rt * R;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const bool odd = *(volatile int *)&ms->odd[parts % ODD_SLOTS] == parts;
+#pragma unroll 1
+        for (int x = 0; x < p.head_dim; x += 32) {
+          float o[32];
+          if (until > part.first) {
+            tmem_ld32(o_at + x, o);
+            tmem_ld_wait32(o);
+          } else {
 #pragma unroll
-          for (int x = 0; x < D; x += 32) {
-            if (x >= p.head_dim) break;
-            float o[32];
-            if (until > part.first) {
-              tmem_ld32(lanes + o_col + x, o);
-              tmem_ld_wait32(o);
+            for (int i = 0; i < 32; ++i) o[i] = 0.f;
+          }
+          if (odd && mine)                                         // what the values have that is not finite (rare)
+            for (int key = max(edge, part.first * KEYS); key < min(vis, part.last * KEYS); ++key) {
+              const int pg = p.page.quot(key), id = w.row[pg];
+              if (id < 0 || id >= p.n_pages) continue;
+              const __nv_bfloat16 *src = (const __nv_bfloat16 *)(p.v + (int64_t)id * p.page_bytes + (int64_t)(key - pg * (int)p.page.d) * p.slot_bytes +
+                                                                 (int64_t)w.head * p.head_bytes) + x;
+#pragma unroll
+              for (int i = 0; i < 32; ++i) {
+                const float y = __bfloat162float(src[i]);
+                if (!(fabsf(y) < INFINITY)) o[i] += y;
+              }
+            }
+          if (mine) {
+            if (whole) {
+              uint4 *dst = (uint4 *)((__nv_bfloat16 *)p.out + to * p.head_dim + x);
+#pragma unroll
+              for (int i = 0; i < 32; i += 8)
+                dst[i / 8] = make_uint4(pack(o[i] * inv, o[i + 1] * inv), pack(o[i + 2] * inv, o[i + 3] * inv), pack(o[i + 4] * inv, o[i + 5] * inv),
+                                        pack(o[i + 6] * inv, o[i + 7] * inv));
             } else {
 #pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] = 0.f;
+              for (int i = 0; i < 32; i += 4) __stcg((float4 *)(p.pieces + piece * p.head_dim + x + i), make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]));
             }
-            if (odd && mine)                                       // what the values have that is not finite (rare)
-              for (int key = max(edge, part.first * KEYS); key < min(vis, part.last * KEYS); ++key) {
-                const int pg = p.page.quot(key), id = w.row[pg];
-                if (id < 0 || id >= p.n_pages) continue;
-                const __nv_bfloat16 *src = (const __nv_bfloat16 *)(p.v + (int64_t)id * p.page_bytes + (int64_t)(key - pg * (int)p.page.d) * p.slot_bytes +
-                                                                   (int64_t)w.head * p.head_bytes) + x;
-#pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                  const float y = __bfloat162float(src[i]);
-                  if (!(fabsf(y) < INFINITY)) o[i] += y;
-                }
-              }
-            if (mine) {
-              if (whole) {
-                uint4 *dst = (uint4 *)((__nv_bfloat16 *)p.out + to * p.head_dim + x);
-#pragma unroll
-                for (int i = 0; i < 32; i += 8)
-                  dst[i / 8] = make_uint4(pack(o[i] * inv, o[i + 1] * inv), pack(o[i + 2] * inv, o[i + 3] * inv), pack(o[i + 4] * inv, o[i + 5] * inv),
-                                          pack(o[i + 6] * inv, o[i + 7] * inv));
-              } else {
-#pragma unroll
-                for (int i = 0; i < 32; i += 4) __stcg((float4 *)(p.pieces + piece * p.head_dim + x + i), make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]));
-              }
-            }
-          }
-          if (mine) {
-            if (!whole) __stcg((float2 *)(mls + piece * 2), make_float2(m, l));
-            else if (p.lse) p.lse[to] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
           }
         }
-        fence_before_sync();
-        w.unit = part.last;
-        if (w.unit == w.units) runs.next_item(w);
+        if (mine) {
+          if (!whole) __stcg((float2 *)(p.pieces + (int64_t)paged::CHUNK_TC_CTAS * 2 * R * p.head_dim + piece * 2), make_float2(m, l));
+          else if (p.lse) p.lse[to] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+        }
       }
+      fence_before_sync();
+      w.unit = part.last;
+      if (w.unit == w.units) runs.next_item(w);
     }
   }
   fence_before_sync();
@@ -615,11 +681,8 @@ int launch(const ChunkParams &p, int64_t cost, const Maps &maps, int box_rows, c
   int dev = 0, sms = 0;
   if (!paged::device(&dev, &sms)) return paged::refuse(CALL, "no usable current device", OURO_ECUDA);
   if (!ready[dev]) {
-    cudaFuncAttributes at;
-    cudaError_t e = cudaFuncSetAttribute(paged_chunk_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::BYTES);
-    if (e == cudaSuccess) e = cudaFuncGetAttributes(&at, paged_chunk_tc_kernel<D>);
+    const cudaError_t e = cudaFuncSetAttribute(paged_chunk_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::BYTES);
     if (e != cudaSuccess) return paged::refuse(CALL, cudaGetErrorString(e), OURO_ECUDA);
-    if (at.numRegs < LAUNCH_REGS) return paged::refuse(CALL, "the kernel was built with fewer registers than it shares out", OURO_ECUDA);
     ready[dev] = true;
   }
   const int64_t most = sms < paged::CHUNK_TC_CTAS ? sms : paged::CHUNK_TC_CTAS, want = cost / MIN_RUN;
@@ -636,7 +699,7 @@ int launch(const ChunkParams &p, int64_t cost, const Maps &maps, int box_rows, c
 int paged::chunk_tc(const ouro_paged_cache *c, const paged::ChunkParams &p, int64_t cost, cudaStream_t s, int *status) {
   if (c->dtype != OURO_BF16 || c->page_size % 8) return 0;
   int box_rows = 8;
-  while (box_rows < 128 && c->page_size % (2 * box_rows) == 0) box_rows *= 2;
+  while (box_rows < KEYS && c->page_size % (2 * box_rows) == 0) box_rows *= 2;
   Maps maps;
   if (!make_map(&maps.k, c, c->k, box_rows) || !make_map(&maps.v, c, c->v, box_rows)) return 0;
   *status = c->head_dim <= 64 ? launch<64>(p, cost, maps, box_rows, s) : launch<128>(p, cost, maps, box_rows, s);
