@@ -11,8 +11,8 @@
 // P is rounded to bf16 once.  It could go in as two bf16 parts, as it does in paged_attention_tc.cu, which is bound by memory; here that would be half as
 // many contractions again.  The rounding errors of P are independent and average out as the values do: their sum is about as large as the output's own
 // rounding.
-// Warps 0-3 and 4-7 are the rows of A and B, warp 8 issues the contractions, warp 9 fetches keys and values (TMA straight from the pages, boxes of 8 to 64 rows
-// of a page), warps 10 and 11 bring the queries of A and B and see to the values at a sequence's end and at the causal edge before they are contracted.
+// Warps 0-3 and 4-7 are the rows of A and B, who also bring their queries; warps 8 and 9 issue the contractions of A and of B; warp 10 fetches keys and values (TMA
+// straight from the pages, boxes of 8 to 64 rows of a page); warp 11 sees to the values at a sequence's end and at the causal edge before they are contracted.
 // Items, runs, pieces and their join: paged_chunk.cuh, paged_chunk.cu.
 #include <cuda.h>
 
@@ -25,7 +25,8 @@ using paged::ChunkWalk;
 
 constexpr int TILE = 128, R = 2 * TILE;            // query rows of a tile, of an item
 constexpr int KEYS = 64;                           // of a unit
-constexpr int ROW_WARPS = 8, THREADS = 32 * (ROW_WARPS + 4);
+constexpr int ROW_WARPS = 8, MMA_WARP = ROW_WARPS, FETCH_WARP = MMA_WARP + 2, VALUE_WARP = FETCH_WARP + 1,
+              THREADS = 32 * (VALUE_WARP + 1);
 constexpr int ITEM_COST = 4, SNAP = 2, MIN_RUN = 4;
 typedef paged::ChunkRuns<R, KEYS, ITEM_COST, SNAP, MIN_RUN> Share;
 constexpr float GROWTH = 8.f;                      // (log2) a maximum may grow by this before sums and outputs are rescaled
@@ -42,7 +43,7 @@ struct Cfg {
   static constexpr int BOXES = D / 64;
   static constexpr int Q_BOX = TILE * 128, KV_BOX = KEYS * 128;    // bytes of 64 dims of all rows or keys, 128-byte swizzle
   static constexpr int Q_TILE = BOXES * Q_BOX, SLOT = BOXES * KV_BOX;          // a tile of Q, a unit's K or V: [box of 64 dims][row][128 bytes]
-  // A slot of K is free when both tiles have had their scores, one of V two steps later.
+  // The scores are a unit ahead of P V, and given back as soon as they are done: two more slots for values keep both as far ahead.
   static constexpr int K_SLOTS = D == 64 ? 8 : 4, V_SLOTS = K_SLOTS + 2;
   static constexpr int OFF_Q = 0, OFF_K = 2 * Q_TILE, OFF_V = OFF_K + K_SLOTS * SLOT, OFF_MISC = OFF_V + V_SLOTS * SLOT;
   static constexpr int OFF_CUM = OFF_K;                            // [n + 1], until the first copy
@@ -56,7 +57,7 @@ struct Cfg {
 
 struct Misc {
   uint64_t k_full[MAX_SLOTS], k_empty[MAX_SLOTS], v_full[MAX_SLOTS], v_ready[MAX_SLOTS], v_empty[MAX_SLOTS];
-  uint64_t q_full[2], q_free[2], s_full[2], s_free[2], p_full[2][2], o_done[2][2], drained;   // [tile] ([buffer of P])
+  uint64_t q_full[2], s_full[2], s_free[2], p_full[2][2], o_done[2][2], drained;           // [tile] ([buffer of P])
   ChunkWalk places[2];                             // where the run begins and ends
   uint32_t tmem;
   int sums[THREADS / 32];
@@ -94,9 +95,12 @@ __device__ __noinline__ void mbar_wait_on(uint64_t *bar, uint32_t phase, Misc *m
 __device__ __forceinline__ void mbar_wait(uint64_t *bar, uint32_t phase, Misc *ms, const ChunkParams &p) {
   if (!mbar_test(bar, phase & 1)) mbar_wait_on(bar, phase, ms, p.wait_limit, p.status);
 }
+// The same for a warp together.
 __device__ __forceinline__ void warp_wait(uint64_t *bar, uint32_t phase, Misc *ms, const ChunkParams &p) {
-  mbar_wait(bar, phase, ms, p);
-  __syncwarp();
+  if (!__all_sync(0xffffffffu, mbar_test(bar, phase & 1))) {
+    mbar_wait_on(bar, phase, ms, p.wait_limit, p.status);
+    __syncwarp();
+  }
 }
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, uint64_t *bar, int dim, int head, int row, int page, int layer) {
   asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];" ::"r"(dst),
@@ -117,21 +121,21 @@ __device__ __forceinline__ uint64_t desc_mn(uint32_t addr, uint32_t box) {
 }
 // fp32 += bf16 x bf16, 128 x n; mn: the B operand is MN-major
 __host__ __device__ constexpr uint32_t idesc(uint32_t n, uint32_t mn) { return (1u << 4) | (1u << 7) | (1u << 10) | (mn << 16) | ((n >> 3) << 17) | ((128u >> 4) << 24); }
-// A in shared memory, or in TMEM: a lane per row, two values of K a column.
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
+// A in shared memory, or in TMEM: a lane per row, two values of K a column.  Descriptors by their lower halves, which have the addresses.
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t a_hi, uint32_t b, uint32_t b_hi, uint32_t id, uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-      "l"(a), "l"(b), "r"(id), "r"(accumulate)
+      "{\n\t.reg .pred p;\n\t.reg .b64 x, y;\n\t"
+      "setp.ne.b32 p, %6, 0;\n\tmov.b64 x, {%1, %2};\n\tmov.b64 y, {%3, %4};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %5, p;\n\t}" ::"r"(d),
+      "r"(a), "r"(a_hi), "r"(b), "r"(b_hi), "r"(id), "r"(accumulate)
       : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t b_hi, uint32_t id, uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-      "r"(a), "l"(b), "r"(id), "r"(accumulate)
+      "{\n\t.reg .pred p;\n\t.reg .b64 y;\n\t"
+      "setp.ne.b32 p, %5, 0;\n\tmov.b64 y, {%2, %3};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %4, p;\n\t}" ::"r"(d),
+      "r"(a), "r"(b), "r"(b_hi), "r"(id), "r"(accumulate)
       : "memory");
 }
 __device__ __forceinline__ void mma_commit(uint64_t *bar) {
@@ -193,6 +197,10 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
   return y;
 }
+// The warps of A and B that share a scheduler take turns at the exponentials, A first: both at once they would be twice as slow, and then both leave the
+// unit for exponentials idle while they wait for scores and look for maxima.  (A wait of the other warp for its scores is bounded, and so is this one.)
+__device__ __forceinline__ void turn_wait(int t, int quarter) { asm volatile("barrier.cta.sync %0, 64;" ::"r"(1 + t * 4 + quarter) : "memory"); }
+__device__ __forceinline__ void turn_over(int t, int quarter) { asm volatile("barrier.cta.arrive %0, 64;" ::"r"(1 + (t ^ 1) * 4 + quarter) : "memory"); }
 __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
 __device__ __forceinline__ bool odd_pair(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }   // not finite
 
@@ -227,29 +235,28 @@ __global__ void __launch_bounds__(THREADS, 1) paged_chunk_tc_kernel(const ChunkP
   if (tid == 0) {
     for (int i = 0; i < MAX_SLOTS; ++i) {
       mbar_init(&ms->k_full[i], 1);
-      mbar_init(&ms->k_empty[i], 1);
+      mbar_init(&ms->k_empty[i], 2);               // both tiles
       mbar_init(&ms->v_full[i], 1);
-      mbar_init(&ms->v_ready[i], 2);               // warps 10 and 11
-      mbar_init(&ms->v_empty[i], 1);
+      mbar_init(&ms->v_ready[i], 1);
+      mbar_init(&ms->v_empty[i], 2);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&ms->q_full[i], 1);
-      mbar_init(&ms->q_free[i], 1);
+      mbar_init(&ms->q_full[i], ROW_WARPS / 2);
       mbar_init(&ms->s_full[i], 1);
       mbar_init(&ms->s_free[i], ROW_WARPS / 2);
-      mbar_init(&ms->p_full[i][0], ROW_WARPS / 2);
-      mbar_init(&ms->p_full[i][1], ROW_WARPS / 2);
-      mbar_init(&ms->o_done[i][0], 1);
-      mbar_init(&ms->o_done[i][1], 1);
+      for (int b = 0; b < 2; ++b) {
+        mbar_init(&ms->p_full[i][b], ROW_WARPS / 2);
+        mbar_init(&ms->o_done[i][b], 1);
+      }
     }
-    mbar_init(&ms->drained, 1);
+    mbar_init(&ms->drained, 2);
     for (int i = 0; i < ODD_SLOTS; ++i) ms->odd[i] = 0;
     ms->dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.k) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.v) : "memory");
   }
-  if (warp == ROW_WARPS) {
+  if (warp == MMA_WARP) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ms->tmem)), "r"(C::COLS) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -274,76 +281,67 @@ __global__ void __launch_bounds__(THREADS, 1) paged_chunk_tc_kernel(const ChunkP
   if (warp >= ROW_WARPS) {
     if (end.at(w)) {
       // (nothing to do)
-    } else if (warp == ROW_WARPS) {
-      // ================================================================ contractions, one thread
+    } else if (warp < FETCH_WARP) {
+      // ================================================================ contractions of a tile, one thread
       if (elect_one()) {
-        uint32_t ks = 0, kph = 0;                                  // slot and phase of the next keys
-        uint32_t va = 0, vaph = 0, vb = 0, vbph = 0;               // of the next values for A and for B
-        uint32_t parts_a = 0, parts_b = 0, scores_a = 0, scores_b = 0, steps_a = 0, steps_b = 0;       // of the tiles: parts, Q K^T, P V
-        const uint64_t q0 = desc_k(sm + C::OFF_Q), k0 = desc_k(sm + C::OFF_K), v0 = desc_mn(sm + C::OFF_V, C::KV_BOX);
-        // Scores of a tile for the next keys.
-        auto qk = [&](int t, bool first, bool last, uint32_t &parts, uint32_t &scores) {
-          if (first) mbar_wait(&ms->q_full[t], parts++, ms, p);
+        const int t = warp - MMA_WARP;
+        uint32_t ks = 0, kph = 0, vs = 0, vph = 0;                 // slot and phase of the next keys and values
+        uint32_t parts = 0, scores = 0, steps = 0;                 // of the tile: parts, Q K^T, P V
+        const uint64_t q0 = desc_k(sm + C::OFF_Q + t * C::Q_TILE), k0 = desc_k(sm + C::OFF_K), v0 = desc_mn(sm + C::OFF_V, C::KV_BOX);
+        const uint32_t q_lo = (uint32_t)q0, q_hi = (uint32_t)(q0 >> 32), k_lo = (uint32_t)k0, k_hi = (uint32_t)(k0 >> 32), v_lo = (uint32_t)v0, v_hi = (uint32_t)(v0 >> 32);
+        const uint32_t s_at = tmem + t * KEYS, p_at = tmem + C::P_COL + t * KEYS, o_at = tmem + C::O_COL + t * 128;
+        // Scores for the next keys.  Keys that the tile does not see are given back (but not before they have come: a phase's parity tells no more than two
+        // apart).
+        auto qk = [&](bool on, bool first) {
           mbar_wait(&ms->k_full[ks], kph, ms, p);
-          if (scores > 0) mbar_wait(&ms->s_free[t], scores - 1, ms, p);
-          ++scores;
-          fence_after_sync();
-          if (*dead) return;
-          const uint64_t a = q0 + (uint32_t)(t * C::Q_TILE >> 4), b = k0 + (ks * C::SLOT >> 4);
+          if (on) {
+            if (first) mbar_wait(&ms->q_full[t], parts++, ms, p);
+            if (scores > 0) mbar_wait(&ms->s_free[t], scores - 1, ms, p);
+            ++scores;
+            fence_after_sync();
+            if (!*dead) {
+              const uint32_t b = k_lo + (ks * C::SLOT >> 4);
 #pragma unroll
-          for (int k = 0; k < D / 16; ++k)
-            mma_ss(tmem + t * KEYS, a + (((k >> 2) * C::Q_BOX + (k & 3) * 32) >> 4), b + (((k >> 2) * C::KV_BOX + (k & 3) * 32) >> 4), idesc(KEYS, 0), k > 0);
-          mma_commit(&ms->s_full[t]);
-          if (last) mma_commit(&ms->q_free[t]);
-        };
-        auto keys_done = [&]() {
+              for (int k = 0; k < D / 16; ++k)
+                mma_ss(s_at, q_lo + (((k >> 2) * C::Q_BOX + (k & 3) * 32) >> 4), q_hi, b + (((k >> 2) * C::KV_BOX + (k & 3) * 32) >> 4), k_hi, idesc(KEYS, 0), k > 0);
+              mma_commit(&ms->s_full[t]);
+            }
+          }
           mma_commit(&ms->k_empty[ks]);
           if (++ks == C::K_SLOTS) ks = 0, ++kph;
         };
-        // O of a tile (+)= P V with its next values.
-        auto pv = [&](int t, bool first, uint32_t v, uint32_t vph, uint32_t &steps) {
-          const uint32_t buf = steps & 1;
-          mbar_wait(&ms->p_full[t][buf], steps >> 1, ms, p);       // (the rows may be a step ahead: a barrier for each buffer)
-          mbar_wait(&ms->v_ready[v], vph, ms, p);
-          ++steps;
-          fence_after_sync();
-          if (*dead) return;
-          const uint64_t b = v0 + (v * C::SLOT >> 4);
+        // O (+)= P V with the next values.
+        auto pv = [&](bool on, bool first) {
+          mbar_wait(&ms->v_ready[vs], vph, ms, p);
+          if (on) {
+            const uint32_t buf = steps & 1;
+            mbar_wait(&ms->p_full[t][buf], steps >> 1, ms, p);     // (the rows may be a step ahead: a barrier for each buffer)
+            ++steps;
+            fence_after_sync();
+            if (!*dead) {
+              const uint32_t b = v_lo + (vs * C::SLOT >> 4);
 #pragma unroll
-          for (int k = 0; k < KEYS / 16; ++k)
-            mma_ts(tmem + C::O_COL + t * 128, tmem + C::P_COL + t * KEYS + buf * (KEYS / 2) + k * 8, b + ((k * 2048) >> 4), idesc(D, 1), !first || k > 0);
-          mma_commit(&ms->o_done[t][buf]);
+              for (int k = 0; k < KEYS / 16; ++k) mma_ts(o_at, p_at + buf * (KEYS / 2) + k * 8, b + ((k * 2048) >> 4), v_hi, idesc(D, 1), !first || k > 0);
+              mma_commit(&ms->o_done[t][buf]);
+            }
+          }
+          mma_commit(&ms->v_empty[vs]);
+          if (++vs == C::V_SLOTS) vs = 0, ++vph;
         };
-        auto pv_a = [&](const Part &x, int u) {
-          if (u < x.until_a) pv(0, u == x.first, va, vaph, steps_a);
-          if (++va == C::V_SLOTS) va = 0, ++vaph;
-        };
-        auto pv_b = [&](const Part &x, int u) {
-          if (u < x.until_b) pv(1, u == x.first, vb, vbph, steps_b);
-          mma_commit(&ms->v_empty[vb]);
-          if (++vb == C::V_SLOTS) vb = 0, ++vbph;
-        };
-        // The tiles are half a step apart: A's next scores, B's last P V, B's next scores, A's P V.
         while (!end.at(w)) {
           const Part part(runs, p, w, end);
-          if (part.first < part.until_a) qk(0, true, part.first + 1 == part.until_a, parts_a, scores_a);
-          if (part.first < part.until_b) qk(1, true, part.first + 1 == part.until_b, parts_b, scores_b);
-          keys_done();
-          for (int u = part.first; u < part.last; ++u) {
-            if (u + 1 < part.until_a) qk(0, false, u + 2 == part.until_a, parts_a, scores_a);
-            if (u > part.first) pv_b(part, u - 1);
-            if (u + 1 < part.until_b) qk(1, false, u + 2 == part.until_b, parts_b, scores_b);
-            if (u + 1 < part.last) keys_done();
-            pv_a(part, u);
+          const int until = part.until(t);
+          for (int u = part.first; u <= part.last; ++u) {          // scores of a unit, P V of the one before
+            if (u < part.last) qk(u < until, u == part.first);
+            if (u > part.first) pv(u - 1 < until, u - 1 == part.first);
           }
-          pv_b(part, part.last - 1);
           w.unit = part.last;
           if (w.unit == w.units) runs.next_item(w);
         }
         mma_commit(&ms->drained);                                  // (nobody else is sure to wait for them once a wait has given up)
         for (uint32_t j = 0; j < DRAIN_POLLS && !mbar_test(&ms->drained, 0); ++j) {}
       }
-    } else if (warp == ROW_WARPS + 1) {
+    } else if (warp == FETCH_WARP) {
       // ================================================================ fetching
       const int per = box_rows / 8;                                // blocks of 8 keys in a box, all on one page
       auto ids_of = [&](const ChunkWalk &x) {                      // page of a unit's lane-th block
@@ -398,43 +396,12 @@ __global__ void __launch_bounds__(THREADS, 1) paged_chunk_tc_kernel(const ChunkP
           for (uint32_t j = 0; j < DRAIN_POLLS && !mbar_test(&ms->v_full[i], (vph - (i >= vs)) & 1); ++j) {}
       }
     } else {
-      // ================================================================ queries; values that not every row sees
-      const int t = warp - ROW_WARPS - 2;
-      uint32_t slot = 0, phase = 0, brought = 0;
+      // ================================================================ values that not every row sees
+      uint32_t slot = 0, phase = 0;
       int parts = 0;
       while (!end.at(w)) {
         const Part part(runs, p, w, end);
         ++parts;
-        if (part.first < part.until(t)) {
-          if (brought > 0) warp_wait(&ms->q_free[t], brought - 1, ms, p);
-          ++brought;
-          // A row is D / 8 pieces of 16 bytes; the warp brings STEP rows at a time.  The place of the next ones follows from that of the last: STEP rows are
-          // so many tokens and heads further.
-          constexpr int PIECES = D / 8, STEP = 32 / PIECES;
-          const int col = lane % PIECES, rows = part.rows_of(t), at = w.rt * R + t * TILE + lane / PIECES;
-          const bool dims = col * 8 < p.head_dim;
-          int tok = p.group_of.quot(at), head = at - tok * p.group;
-          const int step_tok = p.group_of.quot(STEP), step_head = STEP - step_tok * p.group;
-          const int64_t step = step_tok * p.q_stride + (int64_t)step_head * p.head_dim, wrap = p.q_stride - (int64_t)p.group * p.head_dim;
-          const __nv_bfloat16 *src = (const __nv_bfloat16 *)p.q + (int64_t)(w.start + tok) * p.q_stride + ((int64_t)w.head * p.group + head) * p.head_dim + col * 8;
-          uint32_t dst = sm + C::OFF_Q + t * C::Q_TILE + (col >> 3) * C::Q_BOX + (lane / PIECES) * 128;
-#pragma unroll 4
-          for (int r = lane / PIECES; r < TILE; r += STEP) {
-            const bool on = r < rows && dims;
-            cp_async16(dst + (((col & 7) ^ (r & 7)) << 4), on ? src : p.q, on);
-            dst += STEP * 128;
-            src += step;
-            head += step_head;
-            if (head >= p.group) {
-              head -= p.group;
-              src += wrap;
-            }
-          }
-          asm volatile("cp.async.wait_all;" ::: "memory");
-          fence_async_smem();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&ms->q_full[t]);
-        }
         const int edge = max(0, runs.sees(w, w.rt * R));           // keys in front of it are seen by every row
         for (; w.unit < part.last; ++w.unit) {
           warp_wait(&ms->v_full[slot], phase, ms, p);
@@ -442,22 +409,22 @@ __global__ void __launch_bounds__(THREADS, 1) paged_chunk_tc_kernel(const ChunkP
           if (key0 + KEYS > edge) {
             // Keys that some rows do not see: 0 times their values must be 0, so what is not finite is taken out here and put in again, for the
             // rows that see it, at the part's end.  Behind the sequence's end lie other sequences' rows, or nothing.
-            // A lane has 16 bytes of every fourth key of the warp's half.  A number times 0 is 0, but for what is not finite.
-            uint8_t *vp = smem + C::OFF_V + slot * C::SLOT + t * (KEYS / 2) * 128 + lane * 16;
-            const int key = key0 + t * (KEYS / 2) + (lane >> 3);
+            // A lane has 16 bytes of every fourth key.  A number times 0 is 0, but for what is not finite.
+            uint8_t *vp = smem + C::OFF_V + slot * C::SLOT + lane * 16;
+            const int key = key0 + (lane >> 3);
             bool odd = false;
 #pragma unroll
             for (int x = 0; x < C::BOXES; ++x) {
-              uint4 v[KEYS / 8];
+              uint4 v[KEYS / 4];
               __nv_bfloat162 sum = __floats2bfloat162_rn(0.f, 0.f), more = sum;
               const __nv_bfloat162 zero = sum;
 #pragma unroll
-              for (int i = 0; i < KEYS / 8; ++i) {
+              for (int i = 0; i < KEYS / 4; ++i) {
                 if (key + 4 * i >= w.len) *(uint4 *)(vp + x * C::KV_BOX + i * 512) = make_uint4(0, 0, 0, 0);
                 v[i] = *(const uint4 *)(vp + x * C::KV_BOX + i * 512);
               }
 #pragma unroll
-              for (int i = 0; i < KEYS / 8; ++i) {
+              for (int i = 0; i < KEYS / 4; ++i) {
                 sum = __hfma2(*(const __nv_bfloat162 *)&v[i].x, zero, sum);
                 more = __hfma2(*(const __nv_bfloat162 *)&v[i].y, zero, more);
                 sum = __hfma2(*(const __nv_bfloat162 *)&v[i].z, zero, sum);
@@ -466,7 +433,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_chunk_tc_kernel(const ChunkP
               sum = __hadd2(sum, more);
               if (!__any_sync(0xffffffffu, odd_pair(*(const uint32_t *)&sum))) continue;
 #pragma unroll 1
-              for (int i = 0; i < KEYS / 8; ++i) {                 // (rare)
+              for (int i = 0; i < KEYS / 4; ++i) {                 // (rare)
                 if (key + 4 * i < edge) continue;
                 uint4 *at = (uint4 *)(vp + x * C::KV_BOX + i * 512);
                 const uint4 y = *at;
@@ -498,29 +465,61 @@ __global__ void __launch_bounds__(THREADS, 1) paged_chunk_tc_kernel(const ChunkP
     const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), s_at = lanes + t * KEYS, p_at = lanes + C::P_COL + t * KEYS, o_at = lanes + C::O_COL + t * 128;
     uint32_t steps = 0, unit0 = 0;                                 // of the tile so far; of the run, in front of the part, modulo V_SLOTS
     int parts = 0;
+    // The queries of the warp's rows, 32 / PIECES rows of D / 8 pieces of 16 bytes at a time; the scores with those before are done.
+    auto bring = [&](const ChunkWalk &x, int rows) {
+      constexpr int PIECES = D / 8, STEP = 32 / PIECES;
+      const int at = x.rt * R + t * TILE + min(r, rows - 1), tok = p.group_of.quot(at), col = lane % PIECES;
+      const __nv_bfloat16 *mine = (const __nv_bfloat16 *)p.q + (int64_t)(x.start + tok) * p.q_stride + (int64_t)(x.head * p.group + at - tok * p.group) * p.head_dim;
+      const uint32_t dst = sm + C::OFF_Q + t * C::Q_TILE + (col >> 3) * C::Q_BOX + quarter * 32 * 128;
+#pragma unroll
+      for (int i = 0; i < 32; i += STEP) {
+        const int k = i + lane / PIECES;
+        const __nv_bfloat16 *src = (const __nv_bfloat16 *)__shfl_sync(0xffffffffu, (unsigned long long)mine, k);
+        const bool on = quarter * 32 + k < rows && col * 8 < p.head_dim;
+        cp_async16(dst + k * 128 + (((col & 7) ^ (k & 7)) << 4), on ? src + col * 8 : p.q, on);
+      }
+    };
+    auto brought = [&]() {
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&ms->q_full[t]);
+    };
+    if (t == 1) turn_over(1, quarter);                             // (A begins)
+    if (!end.at(w)) {
+      const Part part(runs, p, w, end);
+      if (part.first < part.until(t)) {
+        if (quarter * 32 < part.rows_of(t)) bring(w, part.rows_of(t));
+        brought();
+      }
+    }
     while (!end.at(w)) {
       const Part part(runs, p, w, end);
       ++parts;
       const int rows = part.rows_of(t), until = part.until(t), at0 = w.rt * R + t * TILE;
       const bool on = quarter * 32 < rows, mine = r < rows;        // the warp has rows; this thread has one
       const int at = at0 + (rows > 0 ? min(r, rows - 1) : 0);
+      const int together = quarter * 32 < part.rows_of(1) ? min(part.until_a, part.until_b) : 0;       // units that both tiles' warps of this quarter work on
       const int vis = runs.sees(w, at), all_see = runs.sees(w, at0);
       float m = -INFINITY, l = 0.f;
       uint32_t there_at = unit0;
-      // A unit; cut: not every row sees every key (`there`: blocks of 8 that are on pages, n: keys in front of the row's end).
-      auto unit = [&](auto cut, int u, uint32_t there, int n) {
+      auto unit = [&](int u) {
+        warp_wait(&ms->s_full[t], steps, ms, p);
+        fence_after_sync();
         float s[KEYS];
         tmem_ld32(s_at, s);
         tmem_ld32(s_at + 32, s + 32);
+        const uint32_t there = *(volatile uint32_t *)&ms->there[there_at];
+        if (++there_at == C::V_SLOTS) there_at = 0;
         tmem_ld_wait32(s);
         tmem_ld_wait32(s + 32);
         fence_before_sync();
         __syncwarp();
         if (lane == 0) mbar_arrive(&ms->s_free[t]);
-        if (decltype(cut)::value) {
+        if (there != 0xffu || u * KEYS + KEYS > all_see) {         // (uniform) not every row sees every key
 #pragma unroll
           for (int x = 0; x < KEYS; x += 32) {                     // a bit for each key that the row sees
-            const int ahead = min(max(n - x, 0), 32);
+            const int ahead = min(max(vis - u * KEYS - x, 0), 32);
             const uint32_t bits = (uint32_t)((1ull << ahead) - 1) & ((((there >> (x / 8) & 15u) * 0x00204081u) & 0x01010101u) * 0xffu);
 #pragma unroll
             for (int i = 0; i < 32; ++i) s[x + i] = bits >> i & 1 ? s[x + i] : -INFINITY;
@@ -559,11 +558,8 @@ __global__ void __launch_bounds__(THREADS, 1) paged_chunk_tc_kernel(const ChunkP
         const float base = -base_of(m);
         const u64 base2 = pair(base, base), scale2 = pair(p.scale_log2, p.scale_log2);
         u64 sum = pair(0.f, 0.f);
-        const uint32_t buf = steps & 1;
-        if (steps >= 2) {                                          // (the buffer has been read)
-          warp_wait(&ms->o_done[t][buf], (steps - 2) >> 1, ms, p);
-          fence_after_sync();
-        }
+        const uint32_t buf = steps & 1;                            // (free: the scores came behind the P V that was the last to read it)
+        if (u < together) turn_wait(t, quarter);
 #pragma unroll
         for (int x = 0; x < KEYS; x += 32) {
           uint32_t w16[16];
@@ -578,37 +574,45 @@ __global__ void __launch_bounds__(THREADS, 1) paged_chunk_tc_kernel(const ChunkP
           }
           tmem_st16(p_at + buf * (KEYS / 2) + x / 2, w16);
         }
+        if (u < together) turn_over(t, quarter);
         tmem_st_wait();
         fence_before_sync();
         __syncwarp();
         if (lane == 0) mbar_arrive(&ms->p_full[t][buf]);
+        ++steps;
         float s0, s1;
         unpair(sum, s0, s1);
         l += s0 + s1;
       };
-      for (int u = part.first; u < until; ++u, ++steps) {
-        warp_wait(&ms->s_full[t], steps, ms, p);
-        fence_after_sync();
-        const uint32_t there = *(volatile uint32_t *)&ms->there[there_at];
-        if (++there_at == C::V_SLOTS) there_at = 0;
-        if (!on) {
-          fence_before_sync();
-          __syncwarp();
+      if (on) {
+#pragma unroll 1
+        for (int u = part.first; u < until; ++u) unit(u);
+      } else {
+        for (int u = part.first; u < until; ++u, ++steps) {
+          warp_wait(&ms->s_full[t], steps, ms, p);
           if (lane == 0) {
             mbar_arrive(&ms->s_free[t]);
             mbar_arrive(&ms->p_full[t][steps & 1]);
           }
-        } else if (there == 0xffu && u * KEYS + KEYS <= all_see) {
-          unit(std::false_type{}, u, there, KEYS);
-        } else {
-          unit(std::true_type{}, u, there, vis - u * KEYS);
         }
       }
       unit0 = (unit0 + part.last - part.first) % C::V_SLOTS;
-      // ---- the part's end
+      // ---- the part's end: the next one's queries, and the outputs
+      ChunkWalk nw = w;
+      nw.unit = part.last;
+      if (nw.unit == nw.units) runs.next_item(nw);
+      const bool more = !end.at(nw);
+      if (more) {
+        const Part next(runs, p, nw, end);
+        if (next.first < next.until(t) && quarter * 32 < next.rows_of(t)) bring(nw, next.rows_of(t));
+      }
       if (until > part.first) {
         warp_wait(&ms->o_done[t][(steps - 1) & 1], (steps - 1) >> 1, ms, p);
         fence_after_sync();
+      }
+      if (more) {                                                  // (there by now, and the next scores are worked out meanwhile)
+        const Part next(runs, p, nw, end);
+        if (next.first < next.until(t)) brought();
       }
       if (on) {
         const bool whole = part.first == 0 && part.last == w.units;
@@ -660,13 +664,13 @@ __global__ void __launch_bounds__(THREADS, 1) paged_chunk_tc_kernel(const ChunkP
         }
       }
       fence_before_sync();
-      w.unit = part.last;
-      if (w.unit == w.units) runs.next_item(w);
+      w = nw;
     }
+    if (t == 0) turn_wait(0, quarter);                             // (so that nobody is left waiting for)
   }
   fence_before_sync();
   __syncthreads();
-  if (warp == ROW_WARPS) {
+  if (warp == MMA_WARP) {
     fence_after_sync();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::COLS));
   }
