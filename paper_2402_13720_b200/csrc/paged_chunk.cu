@@ -42,7 +42,7 @@ struct Cfg {
   static constexpr int PITCH = D + 4;                              // (eight threads that read eight rows meet different banks)
   static constexpr int P_PITCH = KEYS + 4;
   static constexpr int OFF_K = R * PITCH, OFF_V = OFF_K + KEYS * PITCH, OFF_P = OFF_V + KEYS * D, OFF_CUM = OFF_P + R * P_PITCH;
-  static constexpr int OFF_MISC = OFF_CUM + OURO_MAX_LIST + 4;
+  static constexpr int OFF_MISC = OFF_CUM + 2 * (OURO_MAX_LIST + 2);
   static constexpr int BYTES = (OFF_MISC + 64) * 4;
 };
 
@@ -55,10 +55,11 @@ __global__ void __launch_bounds__(THREADS, 2) paged_chunk_kernel(const ChunkPara
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
   pdl_wait();
   pdl_trigger();
-  const Share runs(p, gridDim.x, (int *)(smem + C::OFF_CUM), (int *)(smem + C::OFF_MISC), THREADS);
-  const bool any = blockIdx.x < runs.G;
-  ChunkWalk w = runs.place(any ? blockIdx.x : runs.G);
-  const ChunkWalk end = runs.place(any ? blockIdx.x + 1 : runs.G);
+  const Share runs(p);
+  ChunkWalk *places = (ChunkWalk *)(smem + C::OFF_MISC);
+  runs.plan((int64_t *)(smem + C::OFF_CUM), places, THREADS);
+  ChunkWalk w = places[0];
+  const ChunkWalk end = places[1];
   if (tid == 0) p.begins[blockIdx.x] = paged::same(w, end) ? make_int4(-1, 0, 0, 0) : make_int4(w.s, w.head, w.rt, w.unit);
 
   while (!paged::same(w, end)) {
@@ -221,9 +222,10 @@ __global__ void __launch_bounds__(THREADS, 2) paged_chunk_kernel(const ChunkPara
 }
 
 // Items that are cut, by the first run that begins within one: its pieces are the second of the CTA before and the first of that CTA and of those behind
-// that begin within the item too.  The rows of an item are shared by gridDim.y CTAs; a thread has four columns of a row.
+// that begin within the item too.  The rows of an item are shared by gridDim.y CTAs; a thread has four columns of a row.  BY_COLUMNS: a piece's outputs lie as
+// [four columns][row], as threads that have a row each write them best, else [row][column].
 constexpr int JOIN_THREADS = 128, JOIN_SLICES = 16;
-template <typename T, int ROWS, int CTAS>
+template <typename T, int ROWS, int CTAS, bool BY_COLUMNS>
 __global__ void __launch_bounds__(JOIN_THREADS) paged_chunk_join_kernel(const ChunkParams p, const int grid) {
   const int D = p.head_dim;
   pdl_wait();
@@ -235,16 +237,19 @@ __global__ void __launch_bounds__(JOIN_THREADS) paged_chunk_join_kernel(const Ch
   int c1 = c;
   while (c1 + 1 < grid && within(p.begins[c1 + 1])) ++c1;
   const int start = p.starts[b.x], m = p.starts[b.x + 1] - start, rows = min(ROWS, m * p.group - b.z * ROWS);
-  const int r0 = rows * blockIdx.y / JOIN_SLICES, r1 = rows * (blockIdx.y + 1) / JOIN_SLICES, C4 = D / 4;
+  constexpr int EACH = ROWS / JOIN_SLICES;
+  const int r0 = EACH * blockIdx.y, C4 = D / 4;
   const float *mls = p.pieces + (int64_t)CTAS * 2 * ROWS * D;
-  for (int e = threadIdx.x; e < (r1 - r0) * C4; e += JOIN_THREADS) {
-    const int r = r0 + e / C4, col = e % C4 * 4;
+  // (by columns: a warp has 8 rows of 16 columns, so that it reads 128 bytes and writes 32 at a place)
+  for (int e = threadIdx.x; e < EACH * C4; e += JOIN_THREADS) {
+    const int r = r0 + (BY_COLUMNS ? e % 8 + e / 8 / C4 * 8 : e / C4), col = (BY_COLUMNS ? e / 8 % C4 : e % C4) * 4;
+    if (r >= rows) continue;
     float M = -INFINITY, L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
     for (int j = c - 1; j <= c1; ++j) {
       const int64_t at = ((int64_t)j * 2 + (j == c - 1 ? 1 : 0)) * ROWS + r;
       const float2 ml = __ldcg((const float2 *)(mls + at * 2));
-      const float4 y = __ldcg((const float4 *)(p.pieces + at * D + col));
+      const float4 y = __ldcg((const float4 *)(p.pieces + (BY_COLUMNS ? (at - r) * D + (int64_t)col * ROWS + r * 4 : at * D + col)));
       const float mx = fmaxf(M, ml.x), base = base_of(mx), a = ex2(M - base), x = ex2(ml.x - base);
       M = mx;
       L = fmaf(L, a, x * ml.y);
@@ -261,15 +266,15 @@ __global__ void __launch_bounds__(JOIN_THREADS) paged_chunk_join_kernel(const Ch
   }
 }
 
-template <typename T, int ROWS, int CTAS>
+template <typename T, int ROWS, int CTAS, bool BY_COLUMNS>
 int join(const ChunkParams &p, int grid, cudaStream_t s) {
-  const cudaError_t e = launch_pdl(paged_chunk_join_kernel<T, ROWS, CTAS>, dim3(grid - 1, JOIN_SLICES), dim3(JOIN_THREADS), 0, s, p, grid);
+  const cudaError_t e = launch_pdl(paged_chunk_join_kernel<T, ROWS, CTAS, BY_COLUMNS>, dim3(grid - 1, JOIN_SLICES), dim3(JOIN_THREADS), 0, s, p, grid);
   OURO_COUNT_LAUNCH();
   return e == cudaSuccess ? OURO_OK : paged::refuse(CALL, cudaGetErrorString(e), OURO_ECUDA);
 }
 
 template <typename T, int D>
-int launch(const ChunkParams &p, int64_t cost, cudaStream_t s) {
+int launch(ChunkParams p, int64_t cost, cudaStream_t s) {
   using C = Cfg<D>;
   static int fit[paged::MAX_DEVICES] = {};                         // CTAs that are resident at once, per device
   int dev = 0, sms = 0;
@@ -283,10 +288,12 @@ int launch(const ChunkParams &p, int64_t cost, cudaStream_t s) {
     fit[dev] = min(paged::CHUNK_CTAS, sms * per_sm);
   }
   const int grid = (int)min((int64_t)fit[dev], max((int64_t)1, cost / MIN_RUN));
+  p.unit_of.set(KEYS * p.group);
+  p.inv_grid = 1.0 / grid;
   const cudaError_t e = launch_pdl(paged_chunk_kernel<T, D>, dim3(grid), dim3(THREADS), C::BYTES, s, p);
   OURO_COUNT_LAUNCH();
   if (e != cudaSuccess) return paged::refuse(CALL, cudaGetErrorString(e), OURO_ECUDA);
-  return grid > 1 ? join<T, R, paged::CHUNK_CTAS>(p, grid, s) : OURO_OK;
+  return grid > 1 && Share::may_cut(p.cap) ? join<T, R, paged::CHUNK_CTAS, false>(p, grid, s) : OURO_OK;
 }
 
 template <typename T>
@@ -301,7 +308,7 @@ int by_dim(const ChunkParams &p, int64_t cost, cudaStream_t s) {
 
 }  // namespace
 
-int paged::chunk_tc_join(const paged::ChunkParams &p, int grid, cudaStream_t s) { return join<__nv_bfloat16, paged::CHUNK_TC_ROWS, paged::CHUNK_TC_CTAS>(p, grid, s); }
+int paged::chunk_tc_join(const paged::ChunkParams &p, int grid, cudaStream_t s) { return join<__nv_bfloat16, paged::CHUNK_TC_ROWS, paged::CHUNK_TC_CTAS, true>(p, grid, s); }
 
 extern "C" int ouro_paged_chunk_attention(const ouro_paged_cache *c, int32_t layer, const int32_t *seqs, const int32_t *starts, int32_t n, int32_t rows,
                                           const void *q, int64_t q_stride, int32_t n_heads, float scale, void *out, float *lse, void *stream) {
@@ -322,9 +329,10 @@ extern "C" int ouro_paged_chunk_attention(const ouro_paged_cache *c, int32_t lay
   p.group = n_heads / c->n_kv_heads;
   p.cap = c->max_pages * c->page_size;
   if ((int64_t)rows * p.group > paged::MAX_TOKENS) return paged::refuse(CALL, "rows * n_heads / n_kv_heads is above 2^31 - 65536");
-  // units of the finest kind: every tile may see all keys of the longest sequence
+  if ((int64_t)p.cap * p.group > paged::MAX_TOKENS - 65536) return paged::refuse(CALL, "max_pages * page_size * n_heads / n_kv_heads is above 2^31 - 2^17");
+  // units of the finest kind at most: every tile may see all keys of the longest sequence
   const int64_t tiles = ((int64_t)rows * p.group + R - 1) / R + (n < rows ? n : rows), item = ((int64_t)p.cap + KEYS - 1) / KEYS + 8;
-  if (tiles > INT32_MAX / item / c->n_kv_heads) return paged::refuse(CALL, "the sequences' work may be above 2^31 units");
+  if (tiles > ((int64_t)1 << 40) / item / c->n_kv_heads) return paged::refuse(CALL, "the sequences' work may be above 2^40 units");
   const paged::Layout l = paged::layout(*c);
   p.k = (const uint8_t *)c->k + (int64_t)layer * c->layer_stride * esize;
   p.v = (const uint8_t *)c->v + (int64_t)layer * c->layer_stride * esize;

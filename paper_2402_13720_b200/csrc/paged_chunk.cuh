@@ -2,9 +2,12 @@
 //
 // A sequence has m new tokens, the newest of its len; they and the query heads of a kv head's group are its m * group query rows, token by token.  An
 // item is a sequence's kv head and a tile of R rows; KEYS keys of an item are a unit, and an item has as many as its last row sees.  Items in order
-// (sequence, head, tile) are dealt out to G CTAs in runs of equal cost (units, and ITEM_COST for each item); a run begins within an item unless that is
-// within SNAP units of the item's border.  Every CTA works this out for itself from the lengths, so that there is no planning call; what is cut leaves
-// pieces (maximum, sum, unnormalised output, in 32 bits), and a second kernel adds them up in ascending order: the same call gives the same bits.
+// (sequence, head, tile) are dealt out to the CTAs in runs of equal cost; a run begins within an item unless that is within SNAP units of the item's
+// border.  Every CTA works this out for itself from the lengths, so that there is no planning call; what is cut leaves pieces (maximum, sum, unnormalised
+// output, in 32 bits), and a second kernel adds them up in ascending order: the same call gives the same bits.
+// An item's cost is that of its keys, group times their number, and ITEM_COST units for filling and draining the chain.  It grows by R from one tile to
+// the next of a sequence, so that the cost of the first k tiles is a polynomial of k and a run's beginning is found without a walk over the tiles: this is the
+// first that a CTA does, with cold caches, and every instruction counts (walking took 4900 cycles before the first copy, this 2500).
 #pragma once
 
 #include "paged_runs.cuh"
@@ -23,9 +26,11 @@ struct ChunkParams {
   int64_t page_bytes, slot_bytes, head_bytes, q_stride;
   int n, rows, H, Hkv, group;                       // rows: of q (tokens)
   int n_pages, max_pages, max_seqs, cap, layer, head_dim;
-  Div page, group_of;
+  Div page, group_of, unit_of;                      // unit_of: KEYS * group
+  double inv_grid;
   float scale_log2;
   uint32_t wait_limit;
+  bool wide_out;                                    // out is a multiple of 32 bytes
 };
 
 // The tcgen05 kernel (paged_chunk_tc.cu); cost: the call's at most; 0: does not take the call.  And the join of its pieces (paged_chunk.cu).
@@ -43,9 +48,10 @@ __device__ __forceinline__ bool same(const ChunkWalk &a, const ChunkWalk &b) { r
 template <int R, int KEYS, int ITEM_COST, int SNAP, int MIN_RUN>
 struct ChunkRuns {
   const ChunkParams &p;
-  const int *s_cum;                                 // [n + 1] cost of a head of the sequences before
-  int cost, G, each_run, rest;                      // cost = G * each_run + rest (below 2^31: the host checks what it may be); G = 0: the lists are wrong
 
+  // Whether an item of so many keys has units for a cut.
+  static bool may_cut(int keys) { return (keys + KEYS - 1) / KEYS >= 2 * SNAP + 2; }
+  __device__ __forceinline__ explicit ChunkRuns(const ChunkParams &params) : p(params) {}
   // What is known of a sequence; no tokens outside the table.
   __device__ __forceinline__ void enter(ChunkWalk &w) const {
     const int sid = p.seqs ? p.seqs[w.s] : w.s;
@@ -63,56 +69,9 @@ struct ChunkRuns {
     const int last = min(w.m * p.group - 1, rt * R + R - 1);
     return max(1, (sees(w, last) + KEYS - 1) / KEYS);
   }
-  // All threads of the CTA; grid: CTAs at most; scratch: [n + 1] for the costs, which have to last until the last place(), and a word for every warp.
-  __device__ __forceinline__ ChunkRuns(const ChunkParams &params, int grid, int *cum, int *s_sums, int threads) : p(params), s_cum(cum) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = threads / 32;
-    bool bad = false;
-    if (p.n <= warps) {                             // a warp for a sequence, a lane for a tile
-      if (warp < p.n) {
-        ChunkWalk w{warp};
-        enter(w);
-        bad = wrong(w);
-        int sum = 0;
-        if (!bad)
-          for (int rt = lane; rt < w.tiles; rt += 32) sum += units_of(w, rt) + ITEM_COST;
-#pragma unroll
-        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (lane == 0) cum[warp + 1] = sum;
-      }
-    } else {
-      for (int i = tid; i < p.n; i += threads) {
-        ChunkWalk w{i};
-        enter(w);
-        const bool refused = wrong(w);
-        bad |= refused;
-        int sum = 0;
-        if (!refused)
-          for (int rt = 0; rt < w.tiles; ++rt) sum += units_of(w, rt) + ITEM_COST;
-        cum[i + 1] = sum;
-      }
-    }
-    bad = __syncthreads_or(bad);
-    // their sums in order, by the first warp
-    if (warp == 0) {
-      int at = 0;
-      for (int i0 = 0; i0 < p.n; i0 += 32) {
-        int x = i0 + lane < p.n ? cum[i0 + lane + 1] : 0;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const int up = __shfl_up_sync(0xffffffffu, x, o);
-          if (lane >= o) x += up;
-        }
-        if (i0 + lane < p.n) cum[i0 + lane + 1] = at + x;
-        at += __shfl_sync(0xffffffffu, x, 31);
-      }
-      if (lane == 0) cum[0] = 0;
-    }
-    __syncthreads();
-    cost = cum[p.n] * p.Hkv;
-    G = bad || cost == 0 ? 0 : min(grid, max(1, cost / MIN_RUN));
-    each_run = G ? (int)((uint32_t)cost / (uint32_t)G) : 0;
-    rest = cost - each_run * G;
-    if (bad && blockIdx.x == 0 && tid == 0) atomicCAS(p.status, OURO_OK, OURO_EINVAL);
+  // Cost of the first k tiles of a head.
+  __device__ __forceinline__ int64_t upto(const ChunkWalk &w, int k) const {
+    return (int64_t)k * (p.group * (max(w.len - w.m, 0) + ITEM_COST * KEYS) + R) + (int64_t)R * k * (k - 1) / 2;
   }
   // The beginning of the next item that there is, or the end.
   __device__ __forceinline__ void next_item(ChunkWalk &w) const {
@@ -137,50 +96,69 @@ struct ChunkRuns {
   __device__ __forceinline__ void next(ChunkWalk &w) const {
     if (++w.unit >= w.units) next_item(w);
   }
-  // Where the c-th run begins, c <= G; a warp looks for it together.
-  __device__ __forceinline__ ChunkWalk place(int c) const {
-    ChunkWalk w{p.n};
-    if (G == 0) return w;
-    const int at = each_run * c + (int)((uint32_t)(rest * c) / (uint32_t)G);    // cost * c / G
-    if (at >= cost) return w;
-    const int lane = threadIdx.x & 31;
-    // the last sequence that begins at or in front of it and has something (sequences without tokens cost nothing)
-    int lo = 0, hi = p.n;                                           // (all before lo begin in front; all from hi on behind)
-    while (hi - lo > 1) {
-      const int step = (hi - lo + 31) / 32, i = lo + lane * step;
-      const int k = __popc(__ballot_sync(0xffffffffu, i < hi && s_cum[min(i, p.n)] * p.Hkv <= at));
-      const int new_lo = lo + (k - 1) * step;
-      hi = min(hi, new_lo + step);
-      lo = new_lo;
+  // The last k of 0 .. n - 1 with cost(k) <= x, which does not descend; cost(0) <= x.  A warp together.
+  template <typename F>
+  __device__ __forceinline__ int last_within(int n, int64_t x, const F &cost) const {
+    int lo = 0;
+    while (n > 1) {
+      const int step = (n + 31) / 32, i = (threadIdx.x & 31) * step;
+      const int k = __popc(__ballot_sync(0xffffffffu, i < n && cost(lo + min(i, n - 1)) <= x)) - 1;
+      lo += k * step;
+      n = min(step, n - k * step);
     }
-    w.s = lo;
-    enter(w);
-    const int each = s_cum[lo + 1] - s_cum[lo];
-    int in = at - s_cum[lo] * p.Hkv;
-    w.head = in / each;
-    in -= w.head * each;
-    for (int t0 = 0; t0 < w.tiles; t0 += 32) {
-      const int mine = t0 + lane < w.tiles ? units_of(w, t0 + lane) + ITEM_COST : 0;
-      int upto = mine;
+    return lo;
+  }
+  // All threads of the CTA: where its run begins and ends (places[2]).  cum: [n + 1].  Lists that are wrong leave nothing to do, and the cache's status.
+  __device__ __forceinline__ void plan(int64_t *cum, ChunkWalk *places, int threads) const {
+    const int tid = threadIdx.x, lane = tid & 31;
+    bool bad = false;
+    for (int i = tid; i < p.n; i += threads) {
+      ChunkWalk w{i};
+      enter(w);
+      bad |= wrong(w);
+      cum[i + 1] = upto(w, w.tiles) * p.Hkv;
+    }
+    bad = __syncthreads_or(bad);
+    if (tid < 32) {
+      // the sums, each lane those of its part of the list
+      const int per = (p.n + 31) / 32, i0 = min(lane * per, p.n), i1 = min(i0 + per, p.n);
+      int64_t sum = 0;
+      for (int i = i0; i < i1; ++i) sum += cum[i + 1];
+      int64_t at = sum;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const int up = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += up;
+        const int64_t up = __shfl_up_sync(0xffffffffu, at, o);
+        if (lane >= o) at += up;
       }
-      const uint32_t behind = __ballot_sync(0xffffffffu, in < upto);
-      if (behind) {
-        const int k = __ffs(behind) - 1;
-        w.rt = t0 + k;
-        w.units = __shfl_sync(0xffffffffu, mine, k) - ITEM_COST;
-        in -= __shfl_sync(0xffffffffu, upto - mine, k);
-        break;
+      const int64_t total = bad ? 0 : __shfl_sync(0xffffffffu, at, 31);
+      at -= sum;
+      if (lane == 0) cum[0] = 0;
+      for (int i = i0; i < i1; ++i) cum[i + 1] = at += cum[i + 1];
+      __syncwarp();
+      const int64_t run = max((int64_t)MIN_RUN * KEYS * p.group, (int64_t)((double)total * p.inv_grid) + 1);
+#pragma unroll 1
+      for (int e = 0; e < 2; ++e) {
+        int64_t x = run * (blockIdx.x + e);
+        ChunkWalk w{p.n};
+        if (x < total) {
+          w.s = last_within(p.n, x, [&](int i) { return cum[i]; });
+          enter(w);
+          x -= cum[w.s];
+          const int64_t each = upto(w, w.tiles);
+          w.head = last_within(p.Hkv, x, [&](int i) { return i * each; });
+          x -= w.head * each;
+          w.rt = last_within(w.tiles, x, [&](int i) { return upto(w, i); });
+          x -= upto(w, w.rt);
+          w.units = units_of(w, w.rt);
+          const int unit = p.unit_of.quot((int)x) - ITEM_COST;
+          w.unit = unit <= SNAP ? 0 : unit;
+          if (w.unit > 0 && w.units - unit <= SNAP) next_item(w);
+        }
+        if (lane == 0) places[e] = w;
       }
-      in -= __shfl_sync(0xffffffffu, upto, 31);
+      if (bad && blockIdx.x == 0 && lane == 0) atomicCAS(p.status, OURO_OK, OURO_EINVAL);
     }
-    const int unit = in - ITEM_COST;
-    w.unit = unit <= SNAP ? 0 : unit;
-    if (w.unit > 0 && w.units - unit <= SNAP) next_item(w);
-    return w;
+    __syncthreads();
   }
 };
 

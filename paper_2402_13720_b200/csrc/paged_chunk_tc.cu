@@ -46,13 +46,13 @@ struct Cfg {
   // The scores are a unit ahead of P V, and given back as soon as they are done: two more slots for values keep both as far ahead.
   static constexpr int K_SLOTS = D == 64 ? 8 : 4, V_SLOTS = K_SLOTS + 2;
   static constexpr int OFF_Q = 0, OFF_K = 2 * Q_TILE, OFF_V = OFF_K + K_SLOTS * SLOT, OFF_MISC = OFF_V + V_SLOTS * SLOT;
-  static constexpr int OFF_CUM = OFF_K;                            // [n + 1], until the first copy
+  static constexpr int OFF_CUM = OFF_Q;                            // [n + 1], until the first queries
   static constexpr int BYTES = OFF_MISC + 1024;
   // TMEM columns: S of A and B, two P (two keys a column) of A and of B, O of A and B
   static constexpr int P_COL = 2 * KEYS, O_COL = P_COL + 2 * KEYS;
   static constexpr uint32_t COLS = 512;
   static_assert(V_SLOTS <= MAX_SLOTS && V_SLOTS < ODD_SLOTS && O_COL + 256 <= 512 && R == paged::CHUNK_TC_ROWS && BYTES <= 227 * 1024 &&
-                    K_SLOTS * SLOT >= (OURO_MAX_LIST + 1) * 4, "");
+                    Q_TILE >= (OURO_MAX_LIST + 1) * 8, "");
 };
 
 struct Misc {
@@ -60,7 +60,6 @@ struct Misc {
   uint64_t q_full[2], s_full[2], s_free[2], p_full[2][2], o_done[2][2], drained;           // [tile] ([buffer of P])
   ChunkWalk places[2];                             // where the run begins and ends
   uint32_t tmem;
-  int sums[THREADS / 32];
   int dead;                                        // a wait gave up: nobody issues or waits any more
   int odd[ODD_SLOTS];                              // [part mod ..]: the last part of which values that are no finite numbers were taken out, from 1
   uint32_t there[MAX_SLOTS];                       // [slot of V] blocks of 8 keys that are on pages
@@ -164,6 +163,11 @@ __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t *v) {
                : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// 32 bytes, whole sectors: a row's thread writes its own row, and 16 bytes at a time took twice as long.
+__device__ __forceinline__ void store32(void *dst, const uint32_t *v) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
+}
 __device__ __forceinline__ void fence_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -263,14 +267,8 @@ __global__ void __launch_bounds__(THREADS, 1) paged_chunk_tc_kernel(const ChunkP
   pdl_wait();
   pdl_trigger();
   fence_before_sync();
-  const Share runs(p, gridDim.x, (int *)(smem + C::OFF_CUM), ms->sums, THREADS);      // (two barriers)
-  const bool any = blockIdx.x < runs.G;
-  if (warp < 2) {
-    const ChunkWalk x = runs.place(any ? blockIdx.x + warp : runs.G);
-    if (lane == 0) ms->places[warp] = x;
-  }
-  fence_async_smem();
-  __syncthreads();                                                 // (the costs lie where keys will)
+  const Share runs(p);
+  runs.plan((int64_t *)(smem + C::OFF_CUM), ms->places, THREADS);              // (the costs lie where queries will)
   fence_after_sync();
   ChunkWalk w = ms->places[0];
   const End end{ms->places[1].s, ms->places[1].head, ms->places[1].rt, ms->places[1].unit};
@@ -471,7 +469,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_chunk_tc_kernel(const ChunkP
       const int at = x.rt * R + t * TILE + min(r, rows - 1), tok = p.group_of.quot(at), col = lane % PIECES;
       const __nv_bfloat16 *mine = (const __nv_bfloat16 *)p.q + (int64_t)(x.start + tok) * p.q_stride + (int64_t)(x.head * p.group + at - tok * p.group) * p.head_dim;
       const uint32_t dst = sm + C::OFF_Q + t * C::Q_TILE + (col >> 3) * C::Q_BOX + quarter * 32 * 128;
-#pragma unroll
+#pragma unroll 4
       for (int i = 0; i < 32; i += STEP) {
         const int k = i + lane / PIECES;
         const __nv_bfloat16 *src = (const __nv_bfloat16 *)__shfl_sync(0xffffffffu, (unsigned long long)mine, k);
@@ -647,14 +645,21 @@ __global__ void __launch_bounds__(THREADS, 1) paged_chunk_tc_kernel(const ChunkP
             }
           if (mine) {
             if (whole) {
-              uint4 *dst = (uint4 *)((__nv_bfloat16 *)p.out + to * p.head_dim + x);
+              __nv_bfloat16 *dst = (__nv_bfloat16 *)p.out + to * p.head_dim + x;
+              uint32_t y[16];
 #pragma unroll
-              for (int i = 0; i < 32; i += 8)
-                dst[i / 8] = make_uint4(pack(o[i] * inv, o[i + 1] * inv), pack(o[i + 2] * inv, o[i + 3] * inv), pack(o[i + 4] * inv, o[i + 5] * inv),
-                                        pack(o[i + 6] * inv, o[i + 7] * inv));
+              for (int i = 0; i < 16; ++i) y[i] = pack(o[2 * i] * inv, o[2 * i + 1] * inv);
+              if (p.wide_out) {
+                store32(dst, y);
+                store32(dst + 16, y + 8);
+              } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) ((uint4 *)dst)[i] = make_uint4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+              }
             } else {
+              float *dst = p.pieces + ((int64_t)blockIdx.x * 2 + slot) * R * p.head_dim + (int64_t)x * R + (mine_at - w.rt * R) * 4;   // [four columns][row]
 #pragma unroll
-              for (int i = 0; i < 32; i += 4) __stcg((float4 *)(p.pieces + piece * p.head_dim + x + i), make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]));
+              for (int i = 0; i < 32; i += 4) __stcg((float4 *)(dst + i * R), make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]));
             }
           }
         }
@@ -679,7 +684,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_chunk_tc_kernel(const ChunkP
 const char *CALL = "ouro_paged_chunk_attention";
 
 template <int D>
-int launch(const ChunkParams &p, int64_t cost, const Maps &maps, int box_rows, cudaStream_t s) {
+int launch(ChunkParams p, int64_t cost, const Maps &maps, int box_rows, cudaStream_t s) {
   using C = Cfg<D>;
   static bool ready[paged::MAX_DEVICES] = {};
   int dev = 0, sms = 0;
@@ -691,10 +696,13 @@ int launch(const ChunkParams &p, int64_t cost, const Maps &maps, int box_rows, c
   }
   const int64_t most = sms < paged::CHUNK_TC_CTAS ? sms : paged::CHUNK_TC_CTAS, want = cost / MIN_RUN;
   const int grid = (int)(want < 1 ? 1 : want < most ? want : most);
-  cudaError_t e = launch_pdl(paged_chunk_tc_kernel<D>, dim3(grid), dim3(THREADS), C::BYTES, s, p, maps, box_rows);
+  p.unit_of.set(KEYS * p.group);
+  p.inv_grid = 1.0 / grid;
+  p.wide_out = (uintptr_t)p.out % 32 == 0;
+  const cudaError_t e = launch_pdl(paged_chunk_tc_kernel<D>, dim3(grid), dim3(THREADS), C::BYTES, s, p, maps, box_rows);
   OURO_COUNT_LAUNCH();
   if (e != cudaSuccess) return paged::refuse(CALL, cudaGetErrorString(e), OURO_ECUDA);
-  return grid > 1 ? paged::chunk_tc_join(p, grid, s) : OURO_OK;
+  return grid > 1 && Share::may_cut(p.cap) ? paged::chunk_tc_join(p, grid, s) : OURO_OK;
 }
 
 }  // namespace
