@@ -42,7 +42,7 @@ struct Cfg {
   static constexpr int PITCH = D + 4;                              // (eight threads that read eight rows meet different banks)
   static constexpr int P_PITCH = KEYS + 4;
   static constexpr int OFF_K = R * PITCH, OFF_V = OFF_K + KEYS * PITCH, OFF_P = OFF_V + KEYS * D, OFF_CUM = OFF_P + R * P_PITCH;
-  static constexpr int OFF_MISC = OFF_CUM + 2 * (OURO_MAX_LIST + 2);
+  static constexpr int OFF_MISC = OFF_CUM + 5 * OURO_MAX_LIST;
   static constexpr int BYTES = (OFF_MISC + 64) * 4;
 };
 
@@ -53,11 +53,12 @@ __global__ void __launch_bounds__(THREADS, 2) paged_chunk_kernel(const ChunkPara
   extern __shared__ __align__(16) float smem[];
   float *qs = smem, *ks = smem + C::OFF_K, *vs = smem + C::OFF_V, *ps = smem + C::OFF_P;
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+  const Share runs(p);
+  runs.touch();
   pdl_wait();
   pdl_trigger();
-  const Share runs(p);
   ChunkWalk *places = (ChunkWalk *)(smem + C::OFF_MISC);
-  runs.plan((int64_t *)(smem + C::OFF_CUM), places, THREADS);
+  runs.plan((int *)(smem + C::OFF_CUM), (Share::Known *)(smem + C::OFF_CUM + OURO_MAX_LIST), places, THREADS);
   ChunkWalk w = places[0];
   const ChunkWalk end = places[1];
   if (tid == 0) p.begins[blockIdx.x] = paged::same(w, end) ? make_int4(-1, 0, 0, 0) : make_int4(w.s, w.head, w.rt, w.unit);
@@ -221,42 +222,76 @@ __global__ void __launch_bounds__(THREADS, 2) paged_chunk_kernel(const ChunkPara
   }
 }
 
-// Items that are cut, by the first run that begins within one: its pieces are the second of the CTA before and the first of that CTA and of those behind
-// that begin within the item too.  The rows of an item are shared by gridDim.y CTAs; a thread has four columns of a row.  BY_COLUMNS: a piece's outputs lie as
-// [four columns][row], as threads that have a row each write them best, else [row][column].
-constexpr int JOIN_THREADS = 128, JOIN_SLICES = 16;
+// Items that are cut: the pieces of one are the second of the CTA before the first run that begins within it, the first of that run's CTA and of those behind
+// that begin within it too.  gridDim.x: cut items at most, by rank; gridDim.y CTAs share the rows of one, four columns of a row for a thread, which asks for
+// BATCH pieces at once.  BY_COLUMNS: a piece's outputs lie as [four columns][row], as threads that have a row each write them best, else [row][column].
+constexpr int JOIN_THREADS = 256, BATCH = 4, JOIN_CTAS = 8 * 148;
 template <typename T, int ROWS, int CTAS, bool BY_COLUMNS>
 __global__ void __launch_bounds__(JOIN_THREADS) paged_chunk_join_kernel(const ChunkParams p, const int grid) {
-  const int D = p.head_dim;
+  constexpr int WORDS = (CTAS + 31) / 32;
+  __shared__ uint32_t s_first[WORDS], s_more[WORDS];               // a bit for each CTA: the first that begins within its item; one of those behind
+  const int D = p.head_dim, tid = threadIdx.x;
   pdl_wait();
   pdl_trigger();
-  const int c = blockIdx.x + 1;
-  const int4 b = p.begins[c], before = p.begins[c - 1];
-  auto within = [&](const int4 &x) { return x.x == b.x && x.y == b.y && x.z == b.z && x.w > 0; };
-  if (b.x < 0 || b.w == 0 || within(before)) return;
+  for (int i = tid; i < WORDS * 32; i += JOIN_THREADS) {
+    const int4 x = i < grid ? p.begins[i] : make_int4(-1, 0, 0, 0), y = i > 0 && i < grid ? p.begins[i - 1] : x;
+    const bool within = x.x >= 0 && x.w > 0, more = within && i > 0 && y.w > 0 && y.x == x.x && y.y == x.y && y.z == x.z;
+    const uint32_t a = __ballot_sync(0xffffffffu, within && !more), b = __ballot_sync(0xffffffffu, more);
+    if ((tid & 31) == 0) s_first[i / 32] = a, s_more[i / 32] = b;
+  }
+  __syncthreads();
+  int word = 0, rank = blockIdx.x;
+  while (word < WORDS && rank >= __popc(s_first[word])) rank -= __popc(s_first[word++]);
+  if (word == WORDS) return;
+  uint32_t bits = s_first[word];
+  for (; rank > 0; --rank) bits &= bits - 1;
+  const int c = word * 32 + __ffs(bits) - 1;
   int c1 = c;
-  while (c1 + 1 < grid && within(p.begins[c1 + 1])) ++c1;
-  const int start = p.starts[b.x], m = p.starts[b.x + 1] - start, rows = min(ROWS, m * p.group - b.z * ROWS);
-  constexpr int EACH = ROWS / JOIN_SLICES;
-  const int r0 = EACH * blockIdx.y, C4 = D / 4;
+  for (int i = c + 1; i < grid; i = (i / 32 + 1) * 32) {           // ones in a row
+    const uint32_t other = ~(s_more[i / 32] >> (i & 31));
+    const int run = min(other ? __ffs(other) - 1 : 32, 32 - (i & 31));
+    c1 += run;
+    if (run < 32 - (i & 31)) break;
+  }
+  const int4 b = p.begins[c];
+  const int start = p.starts[b.x], m = p.starts[b.x + 1] - start, rows = min(ROWS, m * p.group - b.z * ROWS), C4 = D / 4;
   const float *mls = p.pieces + (int64_t)CTAS * 2 * ROWS * D;
   // (by columns: a warp has 8 rows of 16 columns, so that it reads 128 bytes and writes 32 at a place)
-  for (int e = threadIdx.x; e < EACH * C4; e += JOIN_THREADS) {
-    const int r = r0 + (BY_COLUMNS ? e % 8 + e / 8 / C4 * 8 : e / C4), col = (BY_COLUMNS ? e / 8 % C4 : e % C4) * 4;
+  const int each = ROWS / gridDim.y;
+  for (int e = tid; e < each * C4; e += JOIN_THREADS) {
+    const int q = e / (BY_COLUMNS ? 8 : 1), r = each * blockIdx.y + (BY_COLUMNS ? e % 8 + q / C4 * 8 : q / C4), col = q % C4 * 4;
     if (r >= rows) continue;
     float M = -INFINITY, L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int j = c - 1; j <= c1; ++j) {
-      const int64_t at = ((int64_t)j * 2 + (j == c - 1 ? 1 : 0)) * ROWS + r;
-      const float2 ml = __ldcg((const float2 *)(mls + at * 2));
-      const float4 y = __ldcg((const float4 *)(p.pieces + (BY_COLUMNS ? (at - r) * D + (int64_t)col * ROWS + r * 4 : at * D + col)));
-      const float mx = fmaxf(M, ml.x), base = base_of(mx), a = ex2(M - base), x = ex2(ml.x - base);
+    for (int j0 = c - 1; j0 <= c1; j0 += BATCH) {
+      float2 ml[BATCH];
+      float4 y[BATCH];
+#pragma unroll
+      for (int k = 0; k < BATCH; ++k) {
+        const int j = j0 + k;
+        const int64_t at = ((int64_t)j * 2 + (j == c - 1 ? 1 : 0)) * ROWS;
+        ml[k] = make_float2(-INFINITY, 0.f);
+        y[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (j > c1) continue;
+        ml[k] = __ldcg((const float2 *)(mls + (at + r) * 2));
+        y[k] = __ldcg((const float4 *)(p.pieces + (BY_COLUMNS ? at * D + (int64_t)col * ROWS + r * 4 : (at + r) * D + col)));
+      }
+      float mx = M;
+#pragma unroll
+      for (int k = 0; k < BATCH; ++k) mx = fmaxf(mx, ml[k].x);
+      const float base = base_of(mx), a = ex2(M - base);
       M = mx;
-      L = fmaf(L, a, x * ml.y);
-      o[0] = fmaf(o[0], a, x * y.x);
-      o[1] = fmaf(o[1], a, x * y.y);
-      o[2] = fmaf(o[2], a, x * y.z);
-      o[3] = fmaf(o[3], a, x * y.w);
+      L *= a;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] *= a;
+#pragma unroll
+      for (int k = 0; k < BATCH; ++k) {
+        const float x = ex2(ml[k].x - base);
+        L = fmaf(x, ml[k].y, L);
+        o[0] = fmaf(x, y[k].x, o[0]);
+        o[1] = fmaf(x, y[k].y, o[1]);
+        o[2] = fmaf(x, y[k].z, o[2]);
+        o[3] = fmaf(x, y[k].w, o[3]);
+      }
     }
     const int at = b.z * ROWS + r, tok = p.group_of.quot(at);
     const int64_t to = (int64_t)(start + tok) * p.H + b.y * p.group + at - tok * p.group;
@@ -268,13 +303,17 @@ __global__ void __launch_bounds__(JOIN_THREADS) paged_chunk_join_kernel(const Ch
 
 template <typename T, int ROWS, int CTAS, bool BY_COLUMNS>
 int join(const ChunkParams &p, int grid, cudaStream_t s) {
-  const cudaError_t e = launch_pdl(paged_chunk_join_kernel<T, ROWS, CTAS, BY_COLUMNS>, dim3(grid - 1, JOIN_SLICES), dim3(JOIN_THREADS), 0, s, p, grid);
+  const int64_t items = (((int64_t)p.rows * p.group + ROWS - 1) / ROWS + (p.n < p.rows ? p.n : p.rows)) * p.Hkv;      // at most
+  // As many CTAs as are resident at once, with eight rows each at least.
+  dim3 ctas((unsigned)min((int64_t)grid - 1, items), 1);
+  while (ctas.y < ROWS / 8 && ctas.x * ctas.y * 2 <= JOIN_CTAS) ctas.y *= 2;
+  const cudaError_t e = launch_pdl(paged_chunk_join_kernel<T, ROWS, CTAS, BY_COLUMNS>, ctas, dim3(JOIN_THREADS), 0, s, p, grid);
   OURO_COUNT_LAUNCH();
   return e == cudaSuccess ? OURO_OK : paged::refuse(CALL, cudaGetErrorString(e), OURO_ECUDA);
 }
 
 template <typename T, int D>
-int launch(ChunkParams p, int64_t cost, cudaStream_t s) {
+int launch(ChunkParams p, int64_t cost, int64_t tiles, cudaStream_t s) {
   using C = Cfg<D>;
   static int fit[paged::MAX_DEVICES] = {};                         // CTAs that are resident at once, per device
   int dev = 0, sms = 0;
@@ -288,8 +327,7 @@ int launch(ChunkParams p, int64_t cost, cudaStream_t s) {
     fit[dev] = min(paged::CHUNK_CTAS, sms * per_sm);
   }
   const int grid = (int)min((int64_t)fit[dev], max((int64_t)1, cost / MIN_RUN));
-  p.unit_of.set(KEYS * p.group);
-  p.inv_grid = 1.0 / grid;
+  Share::set(p, grid, tiles);
   const cudaError_t e = launch_pdl(paged_chunk_kernel<T, D>, dim3(grid), dim3(THREADS), C::BYTES, s, p);
   OURO_COUNT_LAUNCH();
   if (e != cudaSuccess) return paged::refuse(CALL, cudaGetErrorString(e), OURO_ECUDA);
@@ -297,12 +335,12 @@ int launch(ChunkParams p, int64_t cost, cudaStream_t s) {
 }
 
 template <typename T>
-int by_dim(const ChunkParams &p, int64_t cost, cudaStream_t s) {
+int by_dim(const ChunkParams &p, int64_t cost, int64_t tiles, cudaStream_t s) {
   switch (p.head_dim) {
-    case 32: return launch<T, 32>(p, cost, s);
-    case 64: return launch<T, 64>(p, cost, s);
-    case 96: return launch<T, 96>(p, cost, s);
-    default: return launch<T, 128>(p, cost, s);
+    case 32: return launch<T, 32>(p, cost, tiles, s);
+    case 64: return launch<T, 64>(p, cost, tiles, s);
+    case 96: return launch<T, 96>(p, cost, tiles, s);
+    default: return launch<T, 128>(p, cost, tiles, s);
   }
 }
 
@@ -348,6 +386,6 @@ extern "C" int ouro_paged_chunk_attention(const ouro_paged_cache *c, int32_t lay
   p.wait_limit = paged::wait_limit.load(std::memory_order_relaxed);
   const int64_t cost = tiles * item * c->n_kv_heads;
   int status = OURO_OK;
-  if (paged::chunk_tc(c, p, cost, (cudaStream_t)stream, &status)) return status;
-  return c->dtype == OURO_F32 ? by_dim<float>(p, cost, (cudaStream_t)stream) : by_dim<__nv_bfloat16>(p, cost, (cudaStream_t)stream);
+  if (paged::chunk_tc(c, p, cost, tiles, (cudaStream_t)stream, &status)) return status;
+  return c->dtype == OURO_F32 ? by_dim<float>(p, cost, tiles, (cudaStream_t)stream) : by_dim<__nv_bfloat16>(p, cost, tiles, (cudaStream_t)stream);
 }

@@ -7,7 +7,7 @@
 // output, in 32 bits), and a second kernel adds them up in ascending order: the same call gives the same bits.
 // An item's cost is that of its keys, group times their number, and ITEM_COST units for filling and draining the chain.  It grows by R from one tile to
 // the next of a sequence, so that the cost of the first k tiles is a polynomial of k and a run's beginning is found without a walk over the tiles: this is the
-// first that a CTA does, with cold caches, and every instruction counts (walking took 4900 cycles before the first copy, this 2500).
+// first that a CTA does, a chain of dependent instructions that nothing hides.
 #pragma once
 
 #include "paged_runs.cuh"
@@ -26,15 +26,15 @@ struct ChunkParams {
   int64_t page_bytes, slot_bytes, head_bytes, q_stride;
   int n, rows, H, Hkv, group;                       // rows: of q (tokens)
   int n_pages, max_pages, max_seqs, cap, layer, head_dim;
-  Div page, group_of, unit_of;                      // unit_of: KEYS * group
-  double inv_grid;
+  Div page, group_of, unit_of, grid_of;             // unit_of: KEYS * group
+  int shift;                                        // costs are counted in 2^shift
   float scale_log2;
   uint32_t wait_limit;
   bool wide_out;                                    // out is a multiple of 32 bytes
 };
 
-// The tcgen05 kernel (paged_chunk_tc.cu); cost: the call's at most; 0: does not take the call.  And the join of its pieces (paged_chunk.cu).
-int chunk_tc(const ouro_paged_cache *c, const ChunkParams &p, int64_t cost, cudaStream_t s, int *status);
+// The tcgen05 kernel (paged_chunk_tc.cu); cost, tiles: units and row tiles of the call at most; 0: does not take the call.  And the join of its pieces (paged_chunk.cu).
+int chunk_tc(const ouro_paged_cache *c, const ChunkParams &p, int64_t cost, int64_t tiles, cudaStream_t s, int *status);
 int chunk_tc_join(const ChunkParams &p, int grid, cudaStream_t s);
 
 // A place in the list of units.
@@ -53,14 +53,20 @@ struct ChunkRuns {
   static bool may_cut(int keys) { return (keys + KEYS - 1) / KEYS >= 2 * SNAP + 2; }
   __device__ __forceinline__ explicit ChunkRuns(const ChunkParams &params) : p(params) {}
   // What is known of a sequence; no tokens outside the table.
-  __device__ __forceinline__ void enter(ChunkWalk &w) const {
-    const int sid = p.seqs ? p.seqs[w.s] : w.s;
+  __device__ __forceinline__ int enter(ChunkWalk &w) const {       // (its row of the table)
+    int sid = p.seqs ? p.seqs[w.s] : w.s;
     const bool known = sid >= 0 && sid < p.max_seqs;
+    if (!known) sid = 0;
     w.len = known ? min(max(p.lens[sid], 0), p.cap) : 0;
-    w.row = p.table + (int64_t)(known ? sid : 0) * p.max_pages;
+    w.row = p.table + (int64_t)sid * p.max_pages;
     w.start = p.starts[w.s];
     w.m = p.starts[w.s + 1] - w.start;
     w.tiles = (w.m * p.group + R - 1) / R;
+    return sid;
+  }
+  // Brings what every CTA reads of the parameters near, before it waits for the kernel in front.
+  __device__ __forceinline__ void touch() const {
+    asm volatile("" ::"l"(p.table), "l"(p.lens), "l"(p.seqs), "l"(p.starts), "l"(p.q), "r"(p.n), "r"(p.group), "r"(p.cap), "r"(p.unit_of.mul), "r"(p.shift), "r"(p.wait_limit));
   }
   __device__ __forceinline__ bool wrong(const ChunkWalk &w) const { return w.start < 0 || w.m < 0 || w.start > p.rows - w.m; }
   // Keys that row r (of the sequence's m * group) sees; below 1: none.
@@ -70,8 +76,16 @@ struct ChunkRuns {
     return max(1, (sees(w, last) + KEYS - 1) / KEYS);
   }
   // Cost of the first k tiles of a head.
-  __device__ __forceinline__ int64_t upto(const ChunkWalk &w, int k) const {
-    return (int64_t)k * (p.group * (max(w.len - w.m, 0) + ITEM_COST * KEYS) + R) + (int64_t)R * k * (k - 1) / 2;
+  __device__ __forceinline__ int upto(const ChunkWalk &w, int k) const {
+    const uint32_t first = p.group * (max(w.len - w.m, 0) + ITEM_COST * KEYS) + R;
+    return (int)(((uint64_t)(uint32_t)k * first + (uint64_t)(uint32_t)k * (uint32_t)(k - 1) * (R / 2)) >> p.shift);
+  }
+  // What the host sets for a launch; tiles: of all sequences at most.
+  static void set(ChunkParams &p, int grid, int64_t tiles) {
+    p.unit_of.set(KEYS * p.group);
+    p.grid_of.set(grid);
+    const int64_t most = tiles * p.Hkv * ((int64_t)p.group * (p.cap + ITEM_COST * KEYS) + 2 * R);
+    for (p.shift = 0; most >> p.shift >= (int64_t)1 << 30;) ++p.shift;
   }
   // The beginning of the next item that there is, or the end.
   __device__ __forceinline__ void next_item(ChunkWalk &w) const {
@@ -96,67 +110,81 @@ struct ChunkRuns {
   __device__ __forceinline__ void next(ChunkWalk &w) const {
     if (++w.unit >= w.units) next_item(w);
   }
-  // The last k of 0 .. n - 1 with cost(k) <= x, which does not descend; cost(0) <= x.  A warp together.
-  template <typename F>
-  __device__ __forceinline__ int last_within(int n, int64_t x, const F &cost) const {
-    int lo = 0;
-    while (n > 1) {
-      const int step = (n + 31) / 32, i = (threadIdx.x & 31) * step;
-      const int k = __popc(__ballot_sync(0xffffffffu, i < n && cost(lo + min(i, n - 1)) <= x)) - 1;
-      lo += k * step;
-      n = min(step, n - k * step);
-    }
-    return lo;
-  }
-  // All threads of the CTA: where its run begins and ends (places[2]).  cum: [n + 1].  Lists that are wrong leave nothing to do, and the cache's status.
-  __device__ __forceinline__ void plan(int64_t *cum, ChunkWalk *places, int threads) const {
+  // All threads of the CTA: where its run begins and ends (places[2]), by a warp each.  cost, known: [n].  Lists that are wrong leave nothing to do, and the
+  // cache's status.
+  struct Known {
+    int sid, len, start, m;
+  };
+  __device__ __forceinline__ void plan(int *cost, Known *known, ChunkWalk *places, int threads) const {
     const int tid = threadIdx.x, lane = tid & 31;
     bool bad = false;
     for (int i = tid; i < p.n; i += threads) {
       ChunkWalk w{i};
-      enter(w);
+      const int sid = enter(w);
       bad |= wrong(w);
-      cum[i + 1] = upto(w, w.tiles) * p.Hkv;
+      cost[i] = upto(w, w.tiles) * p.Hkv;
+      known[i] = Known{sid, w.len, w.start, w.m};
     }
     bad = __syncthreads_or(bad);
-    if (tid < 32) {
+    if (tid < 64) {
       // the sums, each lane those of its part of the list
-      const int per = (p.n + 31) / 32, i0 = min(lane * per, p.n), i1 = min(i0 + per, p.n);
-      int64_t sum = 0;
-      for (int i = i0; i < i1; ++i) sum += cum[i + 1];
-      int64_t at = sum;
+      auto scan = [&](int x) {
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int64_t up = __shfl_up_sync(0xffffffffu, at, o);
-        if (lane >= o) at += up;
-      }
-      const int64_t total = bad ? 0 : __shfl_sync(0xffffffffu, at, 31);
-      at -= sum;
-      if (lane == 0) cum[0] = 0;
-      for (int i = i0; i < i1; ++i) cum[i + 1] = at += cum[i + 1];
-      __syncwarp();
-      const int64_t run = max((int64_t)MIN_RUN * KEYS * p.group, (int64_t)((double)total * p.inv_grid) + 1);
-#pragma unroll 1
-      for (int e = 0; e < 2; ++e) {
-        int64_t x = run * (blockIdx.x + e);
-        ChunkWalk w{p.n};
-        if (x < total) {
-          w.s = last_within(p.n, x, [&](int i) { return cum[i]; });
-          enter(w);
-          x -= cum[w.s];
-          const int64_t each = upto(w, w.tiles);
-          w.head = last_within(p.Hkv, x, [&](int i) { return i * each; });
-          x -= w.head * each;
-          w.rt = last_within(w.tiles, x, [&](int i) { return upto(w, i); });
-          x -= upto(w, w.rt);
-          w.units = units_of(w, w.rt);
-          const int unit = p.unit_of.quot((int)x) - ITEM_COST;
-          w.unit = unit <= SNAP ? 0 : unit;
-          if (w.unit > 0 && w.units - unit <= SNAP) next_item(w);
+        for (int o = 1; o < 32; o <<= 1) {
+          const int up = __shfl_up_sync(0xffffffffu, x, o);
+          if (lane >= o) x += up;
         }
-        if (lane == 0) places[e] = w;
+        return x;
+      };
+      const int per = (p.n + 31) / 32, i0 = lane * per;
+      int sum = 0;
+      for (int i = i0; i < min(i0 + per, p.n); ++i) sum += cost[i];
+      const int upto_here = scan(sum), total = bad ? 0 : __shfl_sync(0xffffffffu, upto_here, 31);
+      const int run = max(((MIN_RUN * KEYS * p.group) >> p.shift) + 1, p.grid_of.quot(total) + 1);
+      int x = run * (int)(blockIdx.x + (tid >> 5));
+      ChunkWalk w{p.n};
+      if (x < total) {
+        // the last of what begins at or in front of it
+        const int part = __popc(__ballot_sync(0xffffffffu, i0 < p.n && upto_here - sum <= x)) - 1;
+        x -= __shfl_sync(0xffffffffu, upto_here - sum, part);
+        w.s = part * per;
+        if (per > 1) {
+          const int mine = lane < per && w.s + lane < p.n ? cost[w.s + lane] : 0, to = scan(mine);
+          const int k = __popc(__ballot_sync(0xffffffffu, lane < per && w.s + lane < p.n && to - mine <= x)) - 1;
+          x -= __shfl_sync(0xffffffffu, to - mine, k);
+          w.s += k;
+        }
+        const Known seq = known[w.s];
+        w.row = p.table + (int64_t)seq.sid * p.max_pages;
+        w.len = seq.len;
+        w.start = seq.start;
+        w.m = seq.m;
+        w.tiles = (w.m * p.group + R - 1) / R;
+        const int each = upto(w, w.tiles);
+        w.head = min((int)((float)x / (float)each), p.Hkv - 1);    // (off by one at most)
+        x -= w.head * each;
+        if (x < 0) {
+          --w.head;
+          x += each;
+        } else if (x >= each) {
+          ++w.head;
+          x -= each;
+        }
+        int n = w.tiles;
+        while (n > 1) {                                            // 32 places at a time
+          const int step = (n + 31) / 32, i = lane * step;
+          const int k = __popc(__ballot_sync(0xffffffffu, i < n && upto(w, w.rt + i) <= x)) - 1;
+          w.rt += k * step;
+          n = min(step, n - k * step);
+        }
+        x -= upto(w, w.rt);
+        w.units = units_of(w, w.rt);
+        const int unit = p.unit_of.quot(x << p.shift) - ITEM_COST;
+        w.unit = unit <= SNAP ? 0 : unit;
+        if (w.unit > 0 && w.units - unit <= SNAP) next_item(w);
       }
-      if (bad && blockIdx.x == 0 && lane == 0) atomicCAS(p.status, OURO_OK, OURO_EINVAL);
+      if (lane == 0) places[tid >> 5] = w;
+      if (bad && blockIdx.x == 0 && tid == 0) atomicCAS(p.status, OURO_OK, OURO_EINVAL);
     }
     __syncthreads();
   }

@@ -46,13 +46,12 @@ struct Cfg {
   // The scores are a unit ahead of P V, and given back as soon as they are done: two more slots for values keep both as far ahead.
   static constexpr int K_SLOTS = D == 64 ? 8 : 4, V_SLOTS = K_SLOTS + 2;
   static constexpr int OFF_Q = 0, OFF_K = 2 * Q_TILE, OFF_V = OFF_K + K_SLOTS * SLOT, OFF_MISC = OFF_V + V_SLOTS * SLOT;
-  static constexpr int OFF_CUM = OFF_Q;                            // [n + 1], until the first queries
   static constexpr int BYTES = OFF_MISC + 1024;
   // TMEM columns: S of A and B, two P (two keys a column) of A and of B, O of A and B
   static constexpr int P_COL = 2 * KEYS, O_COL = P_COL + 2 * KEYS;
   static constexpr uint32_t COLS = 512;
   static_assert(V_SLOTS <= MAX_SLOTS && V_SLOTS < ODD_SLOTS && O_COL + 256 <= 512 && R == paged::CHUNK_TC_ROWS && BYTES <= 227 * 1024 &&
-                    Q_TILE >= (OURO_MAX_LIST + 1) * 8, "");
+                    2 * Q_TILE >= OURO_MAX_LIST * 32, "");
 };
 
 struct Misc {
@@ -264,11 +263,12 @@ __global__ void __launch_bounds__(THREADS, 1) paged_chunk_tc_kernel(const ChunkP
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ms->tmem)), "r"(C::COLS) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  const Share runs(p);
+  runs.touch();
   pdl_wait();
   pdl_trigger();
   fence_before_sync();
-  const Share runs(p);
-  runs.plan((int64_t *)(smem + C::OFF_CUM), ms->places, THREADS);              // (the costs lie where queries will)
+  runs.plan((int *)(smem + C::OFF_Q), (Share::Known *)(smem + C::OFF_Q) + OURO_MAX_LIST, ms->places, THREADS);         // (where the queries will be)
   fence_after_sync();
   ChunkWalk w = ms->places[0];
   const End end{ms->places[1].s, ms->places[1].head, ms->places[1].rt, ms->places[1].unit};
@@ -684,7 +684,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_chunk_tc_kernel(const ChunkP
 const char *CALL = "ouro_paged_chunk_attention";
 
 template <int D>
-int launch(ChunkParams p, int64_t cost, const Maps &maps, int box_rows, cudaStream_t s) {
+int launch(ChunkParams p, int64_t cost, int64_t tiles, const Maps &maps, int box_rows, cudaStream_t s) {
   using C = Cfg<D>;
   static bool ready[paged::MAX_DEVICES] = {};
   int dev = 0, sms = 0;
@@ -696,8 +696,7 @@ int launch(ChunkParams p, int64_t cost, const Maps &maps, int box_rows, cudaStre
   }
   const int64_t most = sms < paged::CHUNK_TC_CTAS ? sms : paged::CHUNK_TC_CTAS, want = cost / MIN_RUN;
   const int grid = (int)(want < 1 ? 1 : want < most ? want : most);
-  p.unit_of.set(KEYS * p.group);
-  p.inv_grid = 1.0 / grid;
+  Share::set(p, grid, tiles);
   p.wide_out = (uintptr_t)p.out % 32 == 0;
   const cudaError_t e = launch_pdl(paged_chunk_tc_kernel<D>, dim3(grid), dim3(THREADS), C::BYTES, s, p, maps, box_rows);
   OURO_COUNT_LAUNCH();
@@ -708,12 +707,12 @@ int launch(ChunkParams p, int64_t cost, const Maps &maps, int box_rows, cudaStre
 }  // namespace
 
 // 0: does not take the call (pages that no box fits).
-int paged::chunk_tc(const ouro_paged_cache *c, const paged::ChunkParams &p, int64_t cost, cudaStream_t s, int *status) {
+int paged::chunk_tc(const ouro_paged_cache *c, const paged::ChunkParams &p, int64_t cost, int64_t tiles, cudaStream_t s, int *status) {
   if (c->dtype != OURO_BF16 || c->page_size % 8) return 0;
   int box_rows = 8;
   while (box_rows < KEYS && c->page_size % (2 * box_rows) == 0) box_rows *= 2;
   Maps maps;
   if (!make_map(&maps.k, c, c->k, box_rows) || !make_map(&maps.v, c, c->v, box_rows)) return 0;
-  *status = c->head_dim <= 64 ? launch<64>(p, cost, maps, box_rows, s) : launch<128>(p, cost, maps, box_rows, s);
+  *status = c->head_dim <= 64 ? launch<64>(p, cost, tiles, maps, box_rows, s) : launch<128>(p, cost, tiles, maps, box_rows, s);
   return 1;
 }
