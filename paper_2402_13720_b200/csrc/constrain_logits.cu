@@ -48,7 +48,7 @@ template <> struct Piece<__nv_bfloat16> {
   static __device__ __forceinline__ void put(__nv_bfloat16 *p, float x) { *p = __float2bfloat16_rn(x); }
 };
 
-// A slice has U pieces a thread.  Pieces begin where the row's addresses are multiples of 16 bytes: the row's first may begin in front of it, its last
+// A slice has U pieces a thread (us of the 1000 rows with U of 1, 2, 4, 8 of f32: -, 121, 115, 130; two groups of U, one on its way: 116, 128).  Pieces begin where the row's addresses are multiples of 16 bytes: the row's first may begin in front of it, its last
 // may end behind it; those two go element by element, and all do where the output's row is aligned differently.
 template <typename T, int U, bool COUNTS>
 __global__ void __launch_bounds__(THREADS) constrain_kernel(const ConstrainParams p) {
@@ -76,10 +76,19 @@ __global__ void __launch_bounds__(THREADS) constrain_kernel(const ConstrainParam
     __syncthreads();
     const int len = p.lens ? min(max(p.lens[row], 0), p.width) : p.width;
     const int32_t *told = p.tokens + row * p.token_stride;
-    for (int i = tid; i < len; i += THREADS) {
-      const int t = told[i];
-      if (t >= 0 && t < p.vocab && (uint32_t)(t - base) < (uint32_t)SLICE) atomicAdd(&s_count[t - base], 1u);
+    const int lo = max(base, 0), here = max(min(base + SLICE, p.vocab) - lo, 0);        // tokens of the slice
+    auto count = [&](int t) {
+      if ((uint32_t)(t - lo) < (uint32_t)here) atomicAdd(&s_count[t - base], 1u);
+    };
+    const int head = min(len, (int)((16 - (uintptr_t)told % 16) % 16 / 4)), fours = (len - head) / 4;
+    const int4 *told4 = (const int4 *)(told + head);
+    for (int i = tid; i < fours; i += 2 * THREADS) {               // eight tokens under way at once
+      const int4 a = told4[i], b = i + THREADS < fours ? told4[i + THREADS] : make_int4(-1, -1, -1, -1);
+      count(a.x); count(a.y); count(a.z); count(a.w);
+      count(b.x); count(b.y); count(b.z); count(b.w);
     }
+    if (tid < head) count(told[tid]);
+    if (tid < len - head - 4 * fours) count(told[head + 4 * fours + tid]);
     if (p.repetition) rep = p.repetition[row];
     if (p.presence) pres = p.presence[row];
     if (p.frequency) freq = p.frequency[row];
@@ -87,7 +96,13 @@ __global__ void __launch_bounds__(THREADS) constrain_kernel(const ConstrainParam
   }
   const float *bias = p.bias ? p.bias + row * p.bias_stride : nullptr;
   const uint32_t *allowed = p.allowed ? p.allowed + row * p.allowed_stride : nullptr;
-  auto told_of = [&](float x, uint32_t c) { return (x > 0.f ? x / rep : x * rep) - fmaf(freq, (float)c, pres); };
+  // x * 1 - 0 where nobody has told the token.  A product with the reciprocal is 2^-23 of the quotient off at most.  (Where histories are long, nearly every
+  // 128 logits of a warp have somebody's token: 1000 rows of 64000 took 173 us with divisions behind branches.)
+  const float inv = 1.f / rep;
+  auto told_of = [&](float x, uint32_t c) {
+    const float n = __uint_as_float(c | 0x4b000000u) - 8388608.f;   // c below 2^23, without the slow conversion
+    return x * (c ? x > 0.f ? inv : rep : 1.f) - (c ? fmaf(freq, n, pres) : 0.f);
+  };
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int local = (u * THREADS + tid) * N, e0 = base + local;
@@ -100,10 +115,10 @@ __global__ void __launch_bounds__(THREADS) constrain_kernel(const ConstrainParam
         for (int i = 0; i < N; i += 4) {
           const uint4 c = *(const uint4 *)(s_count + local + i);
           if (c.x | c.y | c.z | c.w) {
-            if (c.x) x[i] = told_of(x[i], c.x);
-            if (c.y) x[i + 1] = told_of(x[i + 1], c.y);
-            if (c.z) x[i + 2] = told_of(x[i + 2], c.z);
-            if (c.w) x[i + 3] = told_of(x[i + 3], c.w);
+            x[i] = told_of(x[i], c.x);
+            x[i + 1] = told_of(x[i + 1], c.y);
+            x[i + 2] = told_of(x[i + 2], c.z);
+            x[i + 3] = told_of(x[i + 3], c.w);
           }
         }
       }
@@ -111,7 +126,7 @@ __global__ void __launch_bounds__(THREADS) constrain_kernel(const ConstrainParam
         if (((uintptr_t)(bias + e0) & 15) == 0) {
 #pragma unroll
           for (int i = 0; i < N; i += 4) {
-            const float4 b = *(const float4 *)(bias + e0 + i);
+            const float4 b = __ldg((const float4 *)(bias + e0 + i));
             x[i] += b.x; x[i + 1] += b.y; x[i + 2] += b.z; x[i + 3] += b.w;
           }
         } else {
@@ -120,7 +135,7 @@ __global__ void __launch_bounds__(THREADS) constrain_kernel(const ConstrainParam
         }
       }
       if (allowed) {
-        const uint32_t bits = __funnelshift_r(allowed[e0 >> 5], allowed[(e0 + N - 1) >> 5], e0 & 31);
+        const uint32_t bits = __funnelshift_r(__ldg(allowed + (e0 >> 5)), __ldg(allowed + ((e0 + N - 1) >> 5)), e0 & 31);
 #pragma unroll
         for (int i = 0; i < N; ++i)
           if (!(bits >> i & 1)) x[i] = -INFINITY;
@@ -150,7 +165,7 @@ cudaError_t launch(ConstrainParams p, cudaStream_t s) {
 template <typename T>
 cudaError_t by_size(const ConstrainParams &p, int sms, cudaStream_t s) {
   const int64_t pieces = (int64_t)p.rows * (p.vocab / Piece<T>::N + 1);
-  return pieces < (int64_t)sms * THREADS * 8 ? launch<T, 1>(p, s) : launch<T, sizeof(T) == 4 ? 8 : 4>(p, s);
+  return pieces < (int64_t)sms * THREADS * 8 ? launch<T, 1>(p, s) : launch<T, sizeof(T) == 4 ? 4 : 2>(p, s);
 }
 
 }  // namespace
@@ -171,7 +186,7 @@ extern "C" int ouro_constrain_logits(const void *logits, int32_t dtype, int64_t 
   if (rows > 1 && (row_stride < vocab || out_stride < vocab)) return paged::refuse(call, "row_stride or out_stride is below vocab");
   if (logits == out && rows > 1 && row_stride != out_stride) return paged::refuse(call, "out is logits, with other rows");
   if (tokens) {
-    if (width < 0 || (rows > 1 && token_stride < width && token_stride != 0)) return paged::refuse(call, "width is below 0, or token_stride below width");
+    if (width < 0 || width >= 1 << 23 || (rows > 1 && token_stride < width && token_stride != 0)) return paged::refuse(call, "width is below 0 or above 2^23 - 1, or token_stride below width");
   } else if (lens || repetition || presence || frequency) {
     return paged::refuse(call, "lens and penalties come with tokens");
   }
