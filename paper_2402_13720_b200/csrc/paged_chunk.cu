@@ -5,8 +5,11 @@
 //
 // Four operations a query head, key and dimension: behind a few dozen query rows the contractions are what counts, not the keys' bytes.  bf16 goes to
 // paged_chunk_tc.cu.  Here a CTA has 64 query rows in shared memory, passes over the keys 64 at a time and keeps maximum, sum and output of its rows in
-// registers; all in 32 bits.  A thread has 4 rows and every sixteenth key, then 4 rows and every sixteenth group of four dims, so that a value that it
-// reads from shared memory serves four multiply-adds.
+// registers; all in 32 bits.  A thread has 4 rows and every sixteenth key, then 4 rows and every sixteenth group of four dims.  The next keys are asked for when the
+// scores are done, the next values when the outputs are, and the ids of their pages a unit before that.  What bounds it is what comes from shared memory
+// (16 bytes to a lane take four cycles a warp, whoever else wants them): a unit of 128 dims takes an SM 8 us, two CTAs or one, so that a call of few units is best
+// dealt out one by one (five prompts of the `small` shape, up to 411 tokens: 60 us, with runs from 2 units on 77; 4096 tokens, four heads of 128: 503 us, 34
+// TFLOP/s).  8 rows to a thread, who then has to read a third less, leave too few warps: 83 and 544.
 #include "paged_chunk.cuh"
 #include "row_ops.cuh"
 
@@ -17,8 +20,8 @@ using paged::ChunkWalk;
 
 const char *CALL = "ouro_paged_chunk_attention";
 
-constexpr int R = paged::CHUNK_ROWS, KEYS = 64, THREADS = 256;
-constexpr int ITEM_COST = 2, SNAP = 1, MIN_RUN = 2;
+constexpr int R = paged::CHUNK_ROWS, KEYS = 64, THREADS = 256, RT = R / (THREADS / 16);            // RT: rows of a thread
+constexpr int ITEM_COST = 1, SNAP = 0, MIN_RUN = 1;
 typedef paged::ChunkRuns<R, KEYS, ITEM_COST, SNAP, MIN_RUN> Share;
 
 __device__ __forceinline__ float ex2(float x) {
@@ -37,13 +40,37 @@ __device__ __forceinline__ void store4(float *p, float4 x) { *(float4 *)p = x; }
 __device__ __forceinline__ void store4(__nv_bfloat16 *p, float4 x) { *(uint2 *)p = make_uint2(rowops::pack(x.x, x.y), rowops::pack(x.z, x.w)); }
 __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f; }
 
+// 16 bytes, or zeros where there is nothing to read
+__device__ __forceinline__ void cp_async16(void *dst, const void *src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void wait_but_one() { asm volatile("cp.async.wait_group 1;" ::: "memory"); }
+// Four values of N pieces to shared memory as f32: f32 on its way, bf16 at once.
+template <int N>
+__device__ __forceinline__ void bring(float *const *dst, const float *const *src, const bool *there) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) cp_async16(dst[i], src[i], there[i]);
+}
+template <int N>
+__device__ __forceinline__ void bring(float *const *dst, const __nv_bfloat16 *const *src, const bool *there) {
+  uint2 x[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = there[i] ? *(const uint2 *)src[i] : make_uint2(0, 0);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float2 a = rowops::unpack(x[i].x), b = rowops::unpack(x[i].y);
+    *(float4 *)dst[i] = make_float4(a.x, a.y, b.x, b.y);
+  }
+}
+
 template <int D>
 struct Cfg {
   static constexpr int PITCH = D + 4;                              // (eight threads that read eight rows meet different banks)
-  static constexpr int P_PITCH = KEYS + 4;
-  static constexpr int OFF_K = R * PITCH, OFF_V = OFF_K + KEYS * PITCH, OFF_P = OFF_V + KEYS * D, OFF_CUM = OFF_P + R * P_PITCH;
-  static constexpr int OFF_MISC = OFF_CUM + 5 * OURO_MAX_LIST;
-  static constexpr int BYTES = (OFF_MISC + 64) * 4;
+  static constexpr int HALF = KEYS / 2, P_PITCH = HALF + 4;        // probabilities pass through shared memory half a unit at a time: two CTAs fit an SM
+  static constexpr int OFF_K = R * PITCH, OFF_V = OFF_K + KEYS * PITCH, OFF_P = OFF_V + KEYS * D, OFF_MISC = OFF_P + R * P_PITCH;
+  static constexpr int PLAN = 5 * OURO_MAX_LIST;                   // at the beginning, until the first queries
+  static constexpr int BYTES = ((OFF_MISC > PLAN ? OFF_MISC : PLAN) + 64) * 4;
 };
 
 template <typename T, int D>
@@ -57,8 +84,8 @@ __global__ void __launch_bounds__(THREADS, 2) paged_chunk_kernel(const ChunkPara
   runs.touch();
   pdl_wait();
   pdl_trigger();
-  ChunkWalk *places = (ChunkWalk *)(smem + C::OFF_MISC);
-  runs.plan((int *)(smem + C::OFF_CUM), (Share::Known *)(smem + C::OFF_CUM + OURO_MAX_LIST), places, THREADS);
+  ChunkWalk *places = (ChunkWalk *)((uint8_t *)smem + C::BYTES - 256);
+  runs.plan((int *)smem, (Share::Known *)(smem + OURO_MAX_LIST), places, THREADS);
   ChunkWalk w = places[0];
   const ChunkWalk end = places[1];
   if (tid == 0) p.begins[blockIdx.x] = paged::same(w, end) ? make_int4(-1, 0, 0, 0) : make_int4(w.s, w.head, w.rt, w.unit);
@@ -66,21 +93,59 @@ __global__ void __launch_bounds__(THREADS, 2) paged_chunk_kernel(const ChunkPara
   while (!paged::same(w, end)) {
     // ---- an item, or the part of it in this run
     const int rows = min(R, w.m * p.group - w.rt * R), part_begin = w.unit;
-    __syncthreads();                                               // (what was there has been read)
-    for (int e = tid; e < R * D4; e += THREADS) {
-      const int r = e / D4, col = e - r * D4;
-      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (r < rows) {
-        const int at = w.rt * R + r, tok = p.group_of.quot(at);
-        x = load4((const T *)p.q + (int64_t)(w.start + tok) * p.q_stride + (int64_t)(w.head * p.group + at - tok * p.group) * D + col * 4);
-      }
-      *(float4 *)(qs + r * C::PITCH + col * 4) = x;
-    }
-    int vis[4];
-    float m[4], l[4], o[4][OUT][4];
+    const int last = w.s == end.s && w.head == end.head && w.rt == end.rt ? end.unit : w.units;
+    constexpr int PER = KEYS * D4 / THREADS;                       // pieces of four values of a unit's keys, or of the queries, for a thread
+    static_assert(R == KEYS && KEYS * D4 % THREADS == 0, "");
+    float *dst[PER];
+    const T *src[PER];
+    bool there[PER];
+    int ids[PER];
+    auto row_of = [&](int i) { return (tid + i * THREADS) / D4; };
+    auto col_of = [&](int i) { return (tid + i * THREADS) % D4 * 4; };
+    auto ask_ids = [&](int unit) {                                 // of the pages that a unit's keys lie on
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      vis[i] = ty * 4 + i < rows ? runs.sees(w, w.rt * R + ty * 4 + i) : 0;
+      for (int i = 0; i < PER; ++i) {
+        const int key = unit * KEYS + row_of(i);
+        ids[i] = unit < last && key < w.len ? w.row[p.page.quot(key)] : -1;
+      }
+    };
+    auto ask = [&](const uint8_t *pool, float *to, int pitch, int unit) {        // a unit's keys or values
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int key = unit * KEYS + row_of(i), row = key - p.page.quot(key) * (int)p.page.d;
+        there[i] = ids[i] >= 0 && ids[i] < p.n_pages;
+        dst[i] = to + row_of(i) * pitch + col_of(i);
+        src[i] = (const T *)(pool + (there[i] ? (int64_t)ids[i] * p.page_bytes + (int64_t)row * p.slot_bytes : 0) + (int64_t)w.head * p.head_bytes) + col_of(i);
+      }
+      bring<PER>(dst, src, there);
+    };
+    auto lost = [&](int unit) {                                    // keys of the sequence on no page
+      bool any = false;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) any |= unit * KEYS + row_of(i) < w.len && !(ids[i] >= 0 && ids[i] < p.n_pages);
+      return any;
+    };
+    ask_ids(w.unit);
+    __syncthreads();                                               // (what was there has been read)
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      there[i] = row_of(i) < rows;
+      const int at = w.rt * R + (there[i] ? row_of(i) : 0), tok = p.group_of.quot(at);
+      dst[i] = qs + row_of(i) * C::PITCH + col_of(i);
+      src[i] = (const T *)p.q + (int64_t)(w.start + tok) * p.q_stride + (int64_t)(w.head * p.group + at - tok * p.group) * D + col_of(i);
+    }
+    bring<PER>(dst, src, there);
+    bool missing = lost(w.unit);
+    ask(p.k, ks, C::PITCH, w.unit);
+    commit();
+    ask(p.v, vs, D, w.unit);
+    commit();
+    ask_ids(w.unit + 1);
+    int vis[RT];
+    float m[RT], l[RT], o[RT][OUT][4];
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      vis[i] = ty * RT + i < rows ? runs.sees(w, w.rt * R + ty * RT + i) : 0;
       m[i] = -INFINITY;
       l[i] = 0.f;
 #pragma unroll
@@ -89,62 +154,48 @@ __global__ void __launch_bounds__(THREADS, 2) paged_chunk_kernel(const ChunkPara
         for (int d = 0; d < 4; ++d) o[i][x][d] = 0.f;
     }
     const int all_see = runs.sees(w, w.rt * R);                    // keys that every row sees
-    const int last = w.s == end.s && w.head == end.head && w.rt == end.rt ? end.unit : w.units;
     for (; w.unit < last; ++w.unit) {
       const int key0 = w.unit * KEYS;
-      bool missing = false;
-      __syncthreads();                                             // keys and values have been read
-      for (int e = tid; e < KEYS * D4; e += THREADS) {
-        const int r = e / D4, col = e - r * D4, key = key0 + r;
-        float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
-        if (key < w.len) {
-          const int pg = p.page.quot(key), id = w.row[pg];
-          if (id >= 0 && id < p.n_pages) {
-            const int64_t at = (int64_t)id * p.page_bytes + (int64_t)(key - pg * (int)p.page.d) * p.slot_bytes + (int64_t)w.head * p.head_bytes;
-            a = load4((const T *)(p.k + at) + col * 4);
-            b = load4((const T *)(p.v + at) + col * 4);
-          } else {
-            missing = true;
-          }
-        }
-        *(float4 *)(ks + r * C::PITCH + col * 4) = a;
-        *(float4 *)(vs + r * D + col * 4) = b;
-      }
-      missing = __syncthreads_or(missing);
-      float s[4][4];                                               // [row][key tx + 16 j]
+      wait_but_one();
+      const bool gone = __syncthreads_or(missing);                 // (queries and keys are there)
+      float s[RT][4];                                              // [row][key tx + 16 j]
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < RT; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
 #pragma unroll 4
       for (int d = 0; d < D; d += 4) {
-        float4 a[4], b[4];
+        float4 a[RT], b[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] = *(const float4 *)(qs + (ty * 4 + i) * C::PITCH + d);
+        for (int i = 0; i < RT; ++i) a[i] = *(const float4 *)(qs + (ty * RT + i) * C::PITCH + d);
 #pragma unroll
         for (int j = 0; j < 4; ++j) b[j] = *(const float4 *)(ks + (tx + 16 * j) * C::PITCH + d);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < RT; ++i)
 #pragma unroll
           for (int j = 0; j < 4; ++j) s[i][j] = fmaf(a[i].w, b[j].w, fmaf(a[i].z, b[j].z, fmaf(a[i].y, b[j].y, fmaf(a[i].x, b[j].x, s[i][j]))));
       }
-      const bool edge = missing || key0 + KEYS > all_see;          // (the same for the CTA) not every row sees every key
+      __syncthreads();                                             // the keys have been read
+      missing = lost(w.unit + 1);
+      ask(p.k, ks, C::PITCH, w.unit + 1);
+      commit();
+      const bool edge = gone || key0 + KEYS > all_see;             // (the same for the CTA) not every row sees every key
       if (edge) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int key = key0 + tx + 16 * j;
-          bool there = key < w.len;
-          if (missing && there) {
+          bool on = key < w.len;
+          if (gone && on) {
             const int id = w.row[p.page.quot(key)];
-            there = id >= 0 && id < p.n_pages;
+            on = id >= 0 && id < p.n_pages;
           }
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (!there || key >= vis[i]) s[i][j] = -INFINITY;
+          for (int i = 0; i < RT; ++i)
+            if (!on || key >= vis[i]) s[i][j] = -INFINITY;
         }
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < RT; ++i) {
         float top = fmaxf(fmaxf(s[i][0], s[i][1]), fmaxf(s[i][2], s[i][3]));
 #pragma unroll
         for (int x = 8; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
@@ -158,28 +209,28 @@ __global__ void __launch_bounds__(THREADS, 2) paged_chunk_kernel(const ChunkPara
           for (int d = 0; d < 4; ++d) o[i][x][d] *= a;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const float y = ex2(fmaf(s[i][j], p.scale_log2, -base));
-          l[i] += y;
-          ps[(ty * 4 + i) * C::P_PITCH + tx + 16 * j] = y;
+          s[i][j] = ex2(fmaf(s[i][j], p.scale_log2, -base));
+          l[i] += s[i][j];
         }
       }
-      __syncwarp();                                                // (a warp's rows are its own)
+      wait_but_one();
+      __syncthreads();                                             // (values are there)
       // At an edge, 0 times a value that is no finite number must be 0 for the rows that do not see it.
-      auto pv = [&](auto at_edge) {
+      auto pv = [&](auto at_edge, int half) {
 #pragma unroll 2
-        for (int key = 0; key < KEYS; key += 4) {
-          float4 a[4];
+        for (int key = 0; key < C::HALF; key += 4) {
+          float4 a[RT];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) a[i] = *(const float4 *)(ps + (ty * 4 + i) * C::P_PITCH + key);
+          for (int i = 0; i < RT; ++i) a[i] = *(const float4 *)(ps + (ty * RT + i) * C::P_PITCH + key);
 #pragma unroll
           for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
             for (int x = 0; x < OUT; ++x) {
               if (tx + 16 * x >= D4) continue;
-              const float4 b = *(const float4 *)(vs + (key + kk) * D + (tx + 16 * x) * 4);
+              const float4 b = *(const float4 *)(vs + (half * C::HALF + key + kk) * D + (tx + 16 * x) * 4);
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                if (decltype(at_edge)::value && key0 + key + kk >= vis[i]) continue;
+              for (int i = 0; i < RT; ++i) {
+                if (decltype(at_edge)::value && key0 + half * C::HALF + key + kk >= vis[i]) continue;
                 const float y = kk == 0 ? a[i].x : kk == 1 ? a[i].y : kk == 2 ? a[i].z : a[i].w;
                 o[i][x][0] = fmaf(y, b.x, o[i][x][0]);
                 o[i][x][1] = fmaf(y, b.y, o[i][x][1]);
@@ -189,17 +240,29 @@ __global__ void __launch_bounds__(THREADS, 2) paged_chunk_kernel(const ChunkPara
             }
         }
       };
-      if (edge) pv(std::true_type{});
-      else pv(std::false_type{});
-      __syncwarp();
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        __syncwarp();                                              // (a warp's rows are its own)
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) ps[(ty * RT + i) * C::P_PITCH + tx + 16 * j] = s[i][half * 2 + j];
+        __syncwarp();
+        if (edge) pv(std::true_type{}, half);
+        else pv(std::false_type{}, half);
+      }
+      __syncthreads();                                             // the values have been read
+      ask(p.v, vs, D, w.unit + 1);
+      commit();
+      ask_ids(w.unit + 2);
     }
     // ---- its end
     const bool whole = part_begin == 0 && w.unit == w.units;
     const int slot = part_begin == 0 ? 1 : 0;
     float *mls = p.pieces + (int64_t)paged::CHUNK_CTAS * 2 * R * D;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = ty * 4 + i;
+    for (int i = 0; i < RT; ++i) {
+      const int r = ty * RT + i;
 #pragma unroll
       for (int x = 8; x; x >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
       if (r >= rows) continue;
@@ -220,6 +283,7 @@ __global__ void __launch_bounds__(THREADS, 2) paged_chunk_kernel(const ChunkPara
     }
     if (w.unit == w.units) runs.next_item(w);
   }
+  asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
 // Items that are cut: the pieces of one are the second of the CTA before the first run that begins within it, the first of that run's CTA and of those behind

@@ -27,7 +27,7 @@ struct ChunkParams {
   int n, rows, H, Hkv, group;                       // rows: of q (tokens)
   int n_pages, max_pages, max_seqs, cap, layer, head_dim;
   Div page, group_of, unit_of, grid_of;             // unit_of: KEYS * group
-  int shift;                                        // costs are counted in 2^shift
+  int shift, snap;                                  // costs are counted in 2^shift; units from an item's border that are not cut off
   float scale_log2;
   uint32_t wait_limit;
   bool wide_out;                                    // out is a multiple of 32 bytes
@@ -49,8 +49,8 @@ template <int R, int KEYS, int ITEM_COST, int SNAP, int MIN_RUN>
 struct ChunkRuns {
   const ChunkParams &p;
 
-  // Whether an item of so many keys has units for a cut.
-  static bool may_cut(int keys) { return (keys + KEYS - 1) / KEYS >= 2 * SNAP + 2; }
+  // Whether items of so many keys are worth cuts, and with them a second launch.
+  static bool may_cut(int keys) { return (keys + KEYS - 1) / KEYS >= (SNAP > 1 ? 2 * SNAP + 2 : 4); }
   __device__ __forceinline__ explicit ChunkRuns(const ChunkParams &params) : p(params) {}
   // What is known of a sequence; no tokens outside the table.
   __device__ __forceinline__ int enter(ChunkWalk &w) const {       // (its row of the table)
@@ -84,6 +84,7 @@ struct ChunkRuns {
   static void set(ChunkParams &p, int grid, int64_t tiles) {
     p.unit_of.set(KEYS * p.group);
     p.grid_of.set(grid);
+    p.snap = may_cut(p.cap) ? SNAP : INT32_MAX;
     const int64_t most = tiles * p.Hkv * ((int64_t)p.group * (p.cap + ITEM_COST * KEYS) + 2 * R);
     for (p.shift = 0; most >> p.shift >= (int64_t)1 << 30;) ++p.shift;
   }
@@ -180,8 +181,8 @@ struct ChunkRuns {
         x -= upto(w, w.rt);
         w.units = units_of(w, w.rt);
         const int unit = p.unit_of.quot(x << p.shift) - ITEM_COST;
-        w.unit = unit <= SNAP ? 0 : unit;
-        if (w.unit > 0 && w.units - unit <= SNAP) next_item(w);
+        w.unit = unit <= p.snap ? 0 : unit;
+        if (w.unit > 0 && w.units - unit <= p.snap) next_item(w);
       }
       if (lane == 0) places[tid >> 5] = w;
       if (bad && blockIdx.x == 0 && tid == 0) atomicCAS(p.status, OURO_OK, OURO_EINVAL);
