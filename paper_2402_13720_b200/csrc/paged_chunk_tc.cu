@@ -27,9 +27,14 @@ constexpr int TILE = 128, R = 2 * TILE;            // query rows of a tile, of a
 constexpr int KEYS = 64;                           // of a unit
 constexpr int ROW_WARPS = 8, MMA_WARP = ROW_WARPS, FETCH_WARP = MMA_WARP + 2, VALUE_WARP = FETCH_WARP + 1,
               THREADS = 32 * (VALUE_WARP + 1);
-constexpr int ITEM_COST = 4, SNAP = 2, MIN_RUN = 4;
+// us with an item's cost of 2, 4, 5, 6, 8 units: 1.1B shape, mixed batch 27.7, 30.0, 28.1, 29.4, 29.3; 7B shape, 2048 tokens 67.4, 59.5, 59.5, 71.0, 67.9; 70B shape, five
+// prompts 914, 780, 780, 903, 918 (5 and 4 on a later kernel than the others, which had 887 with 4).
+constexpr int ITEM_COST = 5, SNAP = 2, MIN_RUN = 4;
 typedef paged::ChunkRuns<R, KEYS, ITEM_COST, SNAP, MIN_RUN> Share;
 constexpr float GROWTH = 8.f;                      // (log2) a maximum may grow by this before sums and outputs are rescaled
+// Of 32 exponentials, those that go to the special function unit, which takes 8 cycles for a warp's; the others go to the multiply-adds that wait
+// meanwhile.  us with 32, 28, 24, 20, 16: 70B shape, five prompts 814, 795, 781, 792, 828; 34B shape, 61 behind 24000 62.2, 60.4, 58.3, 58.3, 61.0.
+constexpr int EX2_OF_32 = 24;
 constexpr uint32_t DRAIN_POLLS = 1u << 20;         // for copies and contractions under way when their warp is done: they end by themselves
 constexpr int MAX_SLOTS = 12, ODD_SLOTS = 16;      // (whoever sees to the values is a ring ahead of the rows at most)
 
@@ -200,10 +205,24 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
   return y;
 }
-// The warps of A and B that share a scheduler take turns at the exponentials, A first: both at once they would be twice as slow, and then both leave the
-// unit for exponentials idle while they wait for scores and look for maxima.  (A wait of the other warp for its scores is bounded, and so is this one.)
-__device__ __forceinline__ void turn_wait(int t, int quarter) { asm volatile("barrier.cta.sync %0, 64;" ::"r"(1 + t * 4 + quarter) : "memory"); }
-__device__ __forceinline__ void turn_over(int t, int quarter) { asm volatile("barrier.cta.arrive %0, 64;" ::"r"(1 + (t ^ 1) * 4 + quarter) : "memory"); }
+__device__ __forceinline__ u64 mul2(u64 a, u64 b) {
+  u64 y;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b));
+  return y;
+}
+// 2^a and 2^b by multiply-adds: the whole part n of x comes off by rounding to it, 2^f for f in -1/2 .. 1/2 is 1 + f (c1 + f (c2 + f (c3 + f c4))), fitted here for the
+// least largest relative error (2^-18.4; P keeps 8 bits of it, and a row's sum averages it), and 2^n is made of its exponent, which is that of 0 at -127 and below.
+__device__ __forceinline__ u64 ex2_pair(float a, float b) {
+  const u64 x = pair(fmaxf(a, -127.f), fmaxf(b, -127.f)), round = pair(12582912.f, 12582912.f), n = add2(x, round);    // (1.5 2^23)
+  const u64 f = fma2(add2(n, pair(-12582912.f, -12582912.f)), pair(-1.f, -1.f), x), one = pair(1.f, 1.f);
+  u64 y = fma2(f, pair(0.009582852944731712f, 0.009582852944731712f), pair(0.055906426161527634f, 0.055906426161527634f));
+  y = fma2(y, f, pair(0.24024099111557007f, 0.24024099111557007f));
+  y = fma2(y, f, pair(0.6931241750717163f, 0.6931241750717163f));
+  y = fma2(y, f, one);
+  float na, nb;
+  unpair(n, na, nb);
+  return mul2(y, pair(__uint_as_float((__float_as_uint(na) << 23) + 0x3f800000u), __uint_as_float((__float_as_uint(nb) << 23) + 0x3f800000u)));
+}
 __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
 __device__ __forceinline__ bool odd_pair(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }   // not finite
 
@@ -483,7 +502,6 @@ __global__ void __launch_bounds__(THREADS, 1) paged_chunk_tc_kernel(const ChunkP
       __syncwarp();
       if (lane == 0) mbar_arrive(&ms->q_full[t]);
     };
-    if (t == 1) turn_over(1, quarter);                             // (A begins)
     if (!end.at(w)) {
       const Part part(runs, p, w, end);
       if (part.first < part.until(t)) {
@@ -497,7 +515,6 @@ __global__ void __launch_bounds__(THREADS, 1) paged_chunk_tc_kernel(const ChunkP
       const int rows = part.rows_of(t), until = part.until(t), at0 = w.rt * R + t * TILE;
       const bool on = quarter * 32 < rows, mine = r < rows;        // the warp has rows; this thread has one
       const int at = at0 + (rows > 0 ? min(r, rows - 1) : 0);
-      const int together = quarter * 32 < part.rows_of(1) ? min(part.until_a, part.until_b) : 0;       // units that both tiles' warps of this quarter work on
       const int vis = runs.sees(w, at), all_see = runs.sees(w, at0);
       float m = -INFINITY, l = 0.f;
       uint32_t there_at = unit0;
@@ -557,7 +574,6 @@ __global__ void __launch_bounds__(THREADS, 1) paged_chunk_tc_kernel(const ChunkP
         const u64 base2 = pair(base, base), scale2 = pair(p.scale_log2, p.scale_log2);
         u64 sum = pair(0.f, 0.f);
         const uint32_t buf = steps & 1;                            // (free: the scores came behind the P V that was the last to read it)
-        if (u < together) turn_wait(t, quarter);
 #pragma unroll
         for (int x = 0; x < KEYS; x += 32) {
           uint32_t w16[16];
@@ -565,14 +581,18 @@ __global__ void __launch_bounds__(THREADS, 1) paged_chunk_tc_kernel(const ChunkP
           for (int i = 0; i < 32; i += 2) {
             float a, b;
             unpair(fma2(pair(s[x + i], s[x + i + 1]), scale2, base2), a, b);
-            a = ex2(a);
-            b = ex2(b);
-            sum = add2(sum, pair(a, b));
+            u64 e;
+            if (i < EX2_OF_32) {
+              e = pair(ex2(a), ex2(b));
+            } else {
+              e = ex2_pair(a, b);
+            }
+            sum = add2(sum, e);
+            unpair(e, a, b);
             w16[i / 2] = pack(a, b);
           }
           tmem_st16(p_at + buf * (KEYS / 2) + x / 2, w16);
         }
-        if (u < together) turn_over(t, quarter);
         tmem_st_wait();
         fence_before_sync();
         __syncwarp();
@@ -596,22 +616,21 @@ __global__ void __launch_bounds__(THREADS, 1) paged_chunk_tc_kernel(const ChunkP
       }
       unit0 = (unit0 + part.last - part.first) % C::V_SLOTS;
       // ---- the part's end: the next one's queries, and the outputs
+      // (Asked for when the last scores with these are there, they cost the 70B shape's prompts 4 %.)
       ChunkWalk nw = w;
       nw.unit = part.last;
       if (nw.unit == nw.units) runs.next_item(nw);
-      const bool more = !end.at(nw);
-      if (more) {
+      bool next_on = false;
+      if (!end.at(nw)) {
         const Part next(runs, p, nw, end);
-        if (next.first < next.until(t) && quarter * 32 < next.rows_of(t)) bring(nw, next.rows_of(t));
+        next_on = next.first < next.until(t);
+        if (next_on && quarter * 32 < next.rows_of(t)) bring(nw, next.rows_of(t));
       }
       if (until > part.first) {
         warp_wait(&ms->o_done[t][(steps - 1) & 1], (steps - 1) >> 1, ms, p);
         fence_after_sync();
       }
-      if (more) {                                                  // (there by now, and the next scores are worked out meanwhile)
-        const Part next(runs, p, nw, end);
-        if (next.first < next.until(t)) brought();
-      }
+      if (next_on) brought();                                      // (there by now, and the next scores are worked out meanwhile)
       if (on) {
         const bool whole = part.first == 0 && part.last == w.units;
         const int slot = part.first == 0 ? 1 : 0;                  // pieces of a CTA: of an item it begins, of one it goes on with
@@ -671,7 +690,6 @@ __global__ void __launch_bounds__(THREADS, 1) paged_chunk_tc_kernel(const ChunkP
       fence_before_sync();
       w = nw;
     }
-    if (t == 0) turn_wait(0, quarter);                             // (so that nobody is left waiting for)
   }
   fence_before_sync();
   __syncthreads();

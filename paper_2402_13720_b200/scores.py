@@ -44,6 +44,21 @@ def allowed_words(mask: torch.Tensor) -> torch.Tensor:
     return torch.where(words >= 1 << 31, words - (1 << 32), words).int()
 
 
+def _of_rows(t, name, dtype, rows, width, dev):
+    """Distance between the rows of an argument [rows, width], 0 for one row for all [width]."""
+    if t.dtype is not dtype or t.device != dev or t.shape[-1] != width or not (t.dim() == 1 or t.dim() == 2 and t.shape[0] == rows) or (width > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{name}: [rows, {width}] of {dtype} on {dev}, with dense rows, is needed (or one row for all, where that is allowed)")
+    return t.stride(0) if t.dim() == 2 else 0
+
+
+def _of_row(t, name, dtype, rows, dev):
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.device != dev or t.dim() != 1 or t.shape[0] != rows or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous tensor of {rows} elements of {dtype} on {dev} is needed")
+    return t.data_ptr()
+
+
 def constrain_logits(logits: torch.Tensor, *, tokens: torch.Tensor | None = None, lens: torch.Tensor | None = None, repetition: torch.Tensor | None = None,
                      presence: torch.Tensor | None = None, frequency: torch.Tensor | None = None, bias: torch.Tensor | None = None,
                      allowed: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
@@ -56,38 +71,29 @@ def constrain_logits(logits: torch.Tensor, *, tokens: torch.Tensor | None = None
     rows, vocab = logits.shape
     dev = logits.device
     if out is None:
-        out = torch.empty_strided((rows, vocab), (vocab, 1), dtype=logits.dtype, device=dev)
+        out = torch.empty_like(logits) if logits.is_contiguous() else torch.empty((rows, vocab), dtype=logits.dtype, device=dev)
     elif out.shape != logits.shape or out.dtype is not logits.dtype or out.device != dev or (vocab > 1 and out.stride(1) != 1):
         raise ValueError("out has to be like logits")
-
-    def of_rows(t, name, dtype, width, shared):
-        """Distance between the rows of an argument (0: one for all) and its address."""
-        if t is None:
-            return 0, None
-        if t.dtype is not dtype or t.device != dev or t.shape[-1] != width or not (t.dim() == 2 and t.shape[0] == rows or shared and t.dim() == 1) or \
-                (width > 1 and t.stride(-1) != 1):
-            raise ValueError(f"{name}: [rows, {width}]{f' or [{width}]' if shared else ''} of {dtype} on {dev}, with dense rows, is needed")
-        return (t.stride(0) if t.dim() == 2 else 0), t.data_ptr()
-
-    def of_row(t, name, dtype):
-        if t is None:
-            return None
-        if t.dtype is not dtype or t.device != dev or t.dim() != 1 or t.shape[0] != rows or not t.is_contiguous():
-            raise ValueError(f"{name}: a contiguous tensor of {rows} elements of {dtype} on {dev} is needed")
-        return t.data_ptr()
-
-    width = 0 if tokens is None else tokens.shape[-1]
-    token_stride, token_p = of_rows(tokens, "tokens", torch.int32, width, False)
-    bias_stride, bias_p = of_rows(bias, "bias", torch.float32, vocab, True)
-    allowed_stride, allowed_p = of_rows(allowed, "allowed", torch.int32, (vocab + 31) // 32, True)
-    if width == 0:
-        token_p = None                                             # nothing has been said
-    per_row = [of_row(t, name, dtype) for t, name, dtype in ((lens, "lens", torch.int32), (repetition, "repetition", torch.float32),
-                                                             (presence, "presence", torch.float32), (frequency, "frequency", torch.float32))]
-    if tokens is None and any(x is not None for x in (lens, repetition, presence, frequency)):
+    bias_p = allowed_p = token_p = None
+    bias_stride = allowed_stride = token_stride = width = 0
+    if bias is not None:
+        bias_stride, bias_p = _of_rows(bias, "bias", torch.float32, rows, vocab, dev), bias.data_ptr()
+    if allowed is not None:
+        allowed_stride, allowed_p = _of_rows(allowed, "allowed", torch.int32, rows, (vocab + 31) // 32, dev), allowed.data_ptr()
+    per_row = (None, None, None, None)
+    if tokens is not None:
+        if tokens.dim() != 2:
+            raise ValueError("tokens: [rows, width] of torch.int32 is needed")
+        width = tokens.shape[1]
+        token_stride = _of_rows(tokens, "tokens", torch.int32, rows, width, dev)
+        per_row = (_of_row(lens, "lens", torch.int32, rows, dev), _of_row(repetition, "repetition", torch.float32, rows, dev),
+                   _of_row(presence, "presence", torch.float32, rows, dev), _of_row(frequency, "frequency", torch.float32, rows, dev))
+        if width > 0:                                              # (else nothing has been said)
+            token_p = tokens.data_ptr()
+        else:
+            per_row = (None, None, None, None)
+    elif lens is not None or repetition is not None or presence is not None or frequency is not None:
         raise ValueError("lens, repetition, presence and frequency come with tokens")
-    if token_p is None:
-        per_row = [None] * 4
     _check(lib().ouro_constrain_logits(logits.data_ptr(), _DTYPES[logits.dtype], logits.stride(0), rows, vocab, token_p, token_stride, width, *per_row, bias_p,
                                        bias_stride, allowed_p, allowed_stride, out.data_ptr(), out.stride(0), current_stream(dev.index)))
     return out
