@@ -22,85 +22,93 @@ struct RotaryParams {
   int rows, H, Hkv, D, rotary, page, n_pages;
   float magnitude;
 };
-constexpr int THREADS = 256;
+constexpr int THREADS = 128;
 
-__device__ __forceinline__ void load(const float *p, float *x) { const float4 t = *(const float4 *)p; x[0] = t.x; x[1] = t.y; x[2] = t.z; x[3] = t.w; }
-__device__ __forceinline__ void load(const __nv_bfloat16 *p, float *x) {
-  const uint4 t = *(const uint4 *)p;
+__device__ __forceinline__ void unpack(uint4 t, float *x, float) {
+  x[0] = __uint_as_float(t.x); x[1] = __uint_as_float(t.y); x[2] = __uint_as_float(t.z); x[3] = __uint_as_float(t.w);
+}
+__device__ __forceinline__ void unpack(uint4 t, float *x, __nv_bfloat16) {
   const uint32_t w[4] = {t.x, t.y, t.z, t.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) { const float2 f = rowops::unpack(w[i]); x[2 * i] = f.x; x[2 * i + 1] = f.y; }
 }
-__device__ __forceinline__ void store(float *p, const float *x) { *(float4 *)p = make_float4(x[0], x[1], x[2], x[3]); }
-__device__ __forceinline__ void store(__nv_bfloat16 *p, const float *x) {
-  *(uint4 *)p = make_uint4(rowops::pack(x[0], x[1]), rowops::pack(x[2], x[3]), rowops::pack(x[4], x[5]), rowops::pack(x[6], x[7]));
+__device__ __forceinline__ uint4 pack(const float *x, float) {
+  return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+}
+__device__ __forceinline__ uint4 pack(const float *x, __nv_bfloat16) {
+  return make_uint4(rowops::pack(x[0], x[1]), rowops::pack(x[2], x[3]), rowops::pack(x[4], x[5]), rowops::pack(x[6], x[7]));
 }
 
 // A CTA has a row.  A thread has two pieces of 16 bytes of every so manieth head: those of the pairs' two halves, or two side by side; queries first,
-// then keys, then values (which are only moved).
+// then keys, then values (which are only moved).  The first AHEAD heads' pieces are on their way while the angles are worked out (70B shape, 4100 rows: 32.0 us
+// without that and with 256 threads, which 2, 3, 5 ahead left at 31.9, 32.5, 36.3; 128 threads with 2, 4, 6 31.0, 30.5, 31.9; 64 34.8; 25.3 at the copy peak).
+constexpr int AHEAD = 4;
 template <typename T, bool INTERLEAVED>
 __global__ void __launch_bounds__(THREADS) append_rotary_kernel(const RotaryParams p) {
   constexpr int VEC = 16 / sizeof(T);
   __shared__ float s_cos[paged::TEXT_DIM / 2], s_sin[paged::TEXT_DIM / 2];
   const int tid = threadIdx.x, chunks = p.D / (2 * VEC), turned = p.rotary / (2 * VEC), par = THREADS / chunks;   // heads at a time
-  const int ch = tid % chunks, h0 = tid / chunks, row = blockIdx.x;
-  pdl_wait();
-  pdl_trigger();
-  const int pos = p.positions[row], slot = p.slots[row];
-  const bool known = pos >= 0;
-  const int pg = slot / p.page;
-  const bool there = known && slot >= 0 && pg < p.n_pages;
-  if (known && tid < p.rotary / 2) {
-    const double t = pos * p.turns[tid], q = rint(4.0 * t);
-    float s, c;
-    sincospif(2.f * (float)fma(q, -0.25, t), &s, &c);
-    const int quarter = (int)((long long)q & 3);                   // (cos, sin) of q quarter turns more
-    const float x = quarter & 1 ? -s : c, y = quarter & 1 ? c : s;
-    s_cos[tid] = p.magnitude * (quarter & 2 ? -x : x);
-    s_sin[tid] = p.magnitude * (quarter & 2 ? -y : y);
-  }
-  __syncthreads();
-  if (h0 >= par) return;
+  const int ch = tid % chunks, h0 = tid / chunks, row = blockIdx.x, heads = h0 < par ? p.H + 2 * p.Hkv : 0;
   const bool rotates = ch < turned;
   // the two pieces, in elements of the head, and the first pair
   const int first = INTERLEAVED || !rotates ? ch * 2 * VEC : ch * VEC, second = INTERLEAVED || !rotates ? first + VEC : first + p.rotary / 2;
   const int pair = ch * VEC;
-  const int64_t at = there ? (int64_t)pg * p.page_bytes + (int64_t)(slot - pg * p.page) * p.slot_bytes : 0;
-  for (int h = h0; h < p.H + 2 * p.Hkv; h += par) {
-    const int kv = h - p.H, vh = kv - p.Hkv;
-    const T *src;
-    T *dst;
-    if (kv < 0) {
-      src = (const T *)p.q + row * p.q_stride + (int64_t)h * p.D;
-      dst = (T *)p.q_out + ((int64_t)row * p.H + h) * p.D;
-    } else {
-      if (!there) break;                           // (only keys and values follow)
-      src = (const T *)(vh < 0 ? p.k_new : p.v_new) + row * p.kv_stride + (int64_t)(vh < 0 ? kv : vh) * p.D;
-      dst = (T *)((vh < 0 ? p.k : p.v) + at + (int64_t)(vh < 0 ? kv : vh) * p.head_bytes);
-    }
-    if (vh >= 0 || (!rotates && known)) {
-      const uint4 a = *(const uint4 *)(src + first), b = *(const uint4 *)(src + second);
-      *(uint4 *)(dst + first) = a;
-      *(uint4 *)(dst + second) = b;
-      continue;
-    }
-    if (!known) {
-      *(uint4 *)(dst + first) = make_uint4(0, 0, 0, 0);
-      *(uint4 *)(dst + second) = make_uint4(0, 0, 0, 0);
-      continue;
-    }
-    float x[2 * VEC], y[2 * VEC];
-    load(src + first, x);
-    load(src + second, x + VEC);
+  const T *q = (const T *)p.q + row * p.q_stride, *k = (const T *)p.k_new + row * p.kv_stride, *v = (const T *)p.v_new + row * p.kv_stride;
+  auto source = [&](int h) { return h < p.H ? q + (int64_t)h * p.D : h < p.H + p.Hkv ? k + (int64_t)(h - p.H) * p.D : v + (int64_t)(h - p.H - p.Hkv) * p.D; };
+  pdl_wait();
+  pdl_trigger();
+  const int pos = p.positions[row], slot = p.slots[row];
+  uint4 ahead[AHEAD][2];
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-      const int a = INTERLEAVED ? 2 * i : i, b = INTERLEAVED ? 2 * i + 1 : i + VEC;
-      const float c = s_cos[pair + i], s = s_sin[pair + i];
-      y[a] = rowops::rotate(x[a], x[b], c, -s);
-      y[b] = rowops::rotate(x[b], x[a], c, s);
+  for (int i = 0; i < AHEAD; ++i)
+    if (h0 + i * par < heads) {
+      const T *src = source(h0 + i * par);
+      ahead[i][0] = __ldcs((const uint4 *)(src + first));
+      ahead[i][1] = __ldcs((const uint4 *)(src + second));
     }
-    store(dst + first, y);
-    store(dst + second, y + VEC);
+  const bool known = pos >= 0;
+  if (known && tid < p.rotary / 2) {
+    const double t = pos * p.turns[tid], n = rint(4.0 * t);
+    float s, c;
+    sincospif(2.f * (float)fma(n, -0.25, t), &s, &c);
+    const int quarter = (int)((long long)n & 3);                   // (cos, sin) of n quarter turns more
+    const float x = quarter & 1 ? -s : c, y = quarter & 1 ? c : s;
+    s_cos[tid] = p.magnitude * (quarter & 2 ? -x : x);
+    s_sin[tid] = p.magnitude * (quarter & 2 ? -y : y);
+  }
+  const int pg = slot / p.page;
+  const bool there = known && slot >= 0 && pg < p.n_pages;
+  const int64_t at = there ? (int64_t)pg * p.page_bytes + (int64_t)(slot - pg * p.page) * p.slot_bytes : 0;
+  __syncthreads();
+  auto head = [&](int h, uint4 a, uint4 b) {
+    const int kv = h - p.H, vh = kv - p.Hkv;
+    if (kv >= 0 && !there) return;
+    T *dst = kv < 0 ? (T *)p.q_out + ((int64_t)row * p.H + h) * p.D : (T *)((vh < 0 ? p.k : p.v) + at + (int64_t)(vh < 0 ? kv : vh) * p.head_bytes);
+    if (!known) {
+      a = b = make_uint4(0, 0, 0, 0);
+    } else if (vh < 0 && rotates) {
+      float x[2 * VEC], y[2 * VEC];
+      unpack(a, x, T{});
+      unpack(b, x + VEC, T{});
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const int m = INTERLEAVED ? 2 * i : i, n = INTERLEAVED ? 2 * i + 1 : i + VEC;
+        const float c = s_cos[pair + i], s = s_sin[pair + i];
+        y[m] = rowops::rotate(x[m], x[n], c, -s);
+        y[n] = rowops::rotate(x[n], x[m], c, s);
+      }
+      a = pack(y, T{});
+      b = pack(y + VEC, T{});
+    }
+    *(uint4 *)(dst + first) = a;
+    *(uint4 *)(dst + second) = b;
+  };
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i)
+    if (h0 + i * par < heads) head(h0 + i * par, ahead[i][0], ahead[i][1]);
+  for (int h = h0 + AHEAD * par; h < heads; h += par) {
+    const T *src = source(h);
+    head(h, *(const uint4 *)(src + first), *(const uint4 *)(src + second));
   }
 }
 
