@@ -351,9 +351,9 @@ int ouro_paged_attention(const ouro_paged_cache *cache, int32_t layer, const int
  * rows starts_dev[i] .. starts_dev[i+1]-1 (starts_dev [n+1], not descending, within 0 .. rows; none is allowed).  Of m new tokens the t-th sees the keys
  * 0 .. lens - m + t.  out [rows, n_heads, head_dim], lse_dev [rows, n_heads] (may be NULL): rows of no sequence are left as they are.  Tokens that see no
  * key, missing pages and sequences outside the table as above; starts that descend or leave 0 .. rows make the call do nothing (OURO_EINVAL in the cache's
- * status).  seqs_dev may name a sequence twice.  Two launches; a page_size that is a multiple of 8 is faster in bf16.  Sums and maxima are held in 32 bits; in
+ * status).  seqs_dev may name a sequence twice.  Two launches (one where no sequence can have 256 keys, bf16: 384); a page_size that is a multiple of 8 is faster in bf16.  Sums and maxima are held in 32 bits; in
  * bf16 a probability may go into the second product rounded to bf16, so that an output is off by up to 2^-8 of its probabilities' weighted |values| besides
- * its own rounding.  rows * n_heads / n_kv_heads is at most 2^31 - 65536. */
+ * its own rounding.  rows * n_heads / n_kv_heads and (max_pages * page_size + 1024) * n_heads / n_kv_heads are at most 2^31 - 65536, n_heads / n_kv_heads 65536. */
 int ouro_paged_chunk_attention(const ouro_paged_cache *cache, int32_t layer, const int32_t *seqs_dev, const int32_t *starts_dev, int32_t n, int32_t rows,
                                const void *q_dev, int64_t q_stride, int32_t n_heads, float scale, void *out_dev, float *lse_dev, void *cuda_stream);
 
@@ -387,10 +387,10 @@ int ouro_token_logprobs(const void *logits_dev, int32_t dtype, int64_t row_strid
 /* Rules on which tokens may come, on rows of logits [rows, vocab] (OURO_F32 or OURO_BF16), rows row_stride elements apart, into out (rows out_stride apart; may
  * be logits itself with the same stride).  In this order, in 32 bits, rounded once:
  *   a token that is c > 0 times among the first lens_dev[row] (NULL: width) of the row's tokens_dev [rows, width] (rows token_stride apart; ids outside the
- *   vocabulary count for nothing):  y = y > 0 ? y / repetition[row] : y * repetition[row], then y -= frequency[row] * c + presence[row];
+ *   vocabulary count for nothing):  y = y > 0 ? y / repetition[row] (a product with the rounded reciprocal) : y * repetition[row], then y -= frequency[row] * c + presence[row];
  *   y += bias[row, token] (rows bias_stride apart, 0: one row for all);
  *   y = -inf, whatever it was, where bit token % 32 of word token / 32 of the row's allowed_dev (rows allowed_stride apart, 0: one row for all) is 0.
- * repetition, presence, frequency [rows] f32.  Every array but logits and out may be NULL (repetition 1, the others 0 or allowed); lens and penalties come with tokens. */
+ * repetition, presence, frequency [rows] f32; width is at most 2^23 - 1.  Every array but logits and out may be NULL (repetition 1, the others 0 or allowed); lens and penalties come with tokens. */
 int ouro_constrain_logits(const void *logits_dev, int32_t dtype, int64_t row_stride, int32_t rows, int32_t vocab, const int32_t *tokens_dev,
                           int64_t token_stride, int32_t width, const int32_t *lens_dev, const float *repetition_dev, const float *presence_dev,
                           const float *frequency_dev, const float *bias_dev, int64_t bias_stride, const uint32_t *allowed_dev, int64_t allowed_stride,

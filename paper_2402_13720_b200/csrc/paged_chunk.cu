@@ -431,7 +431,8 @@ extern "C" int ouro_paged_chunk_attention(const ouro_paged_cache *c, int32_t lay
   p.group = n_heads / c->n_kv_heads;
   p.cap = c->max_pages * c->page_size;
   if ((int64_t)rows * p.group > paged::MAX_TOKENS) return paged::refuse(CALL, "rows * n_heads / n_kv_heads is above 2^31 - 65536");
-  if ((int64_t)p.cap * p.group > paged::MAX_TOKENS - 65536) return paged::refuse(CALL, "max_pages * page_size * n_heads / n_kv_heads is above 2^31 - 2^17");
+  if (p.group > 65536) return paged::refuse(CALL, "n_heads / n_kv_heads is above 65536");
+  if (((int64_t)p.cap + 1024) * p.group > paged::MAX_TOKENS) return paged::refuse(CALL, "(max_pages * page_size + 1024) * n_heads / n_kv_heads is above 2^31 - 65536");
   // units of the finest kind at most: every tile may see all keys of the longest sequence
   const int64_t tiles = ((int64_t)rows * p.group + R - 1) / R + (n < rows ? n : rows), item = ((int64_t)p.cap + KEYS - 1) / KEYS + 8;
   if (tiles > ((int64_t)1 << 40) / item / c->n_kv_heads) return paged::refuse(CALL, "the sequences' work may be above 2^40 units");

@@ -142,7 +142,7 @@ struct ChunkRuns {
       for (int i = i0; i < min(i0 + per, p.n); ++i) sum += cost[i];
       const int upto_here = scan(sum), total = bad ? 0 : __shfl_sync(0xffffffffu, upto_here, 31);
       const int run = max(((MIN_RUN * KEYS * p.group) >> p.shift) + 1, p.grid_of.quot(total) + 1);
-      int x = run * (int)(blockIdx.x + (tid >> 5));
+      int x = (int)min((int64_t)run * (blockIdx.x + (tid >> 5)), (int64_t)total);
       ChunkWalk w{p.n};
       if (x < total) {
         // the last of what begins at or in front of it

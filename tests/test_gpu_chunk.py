@@ -343,6 +343,130 @@ def test_chunk_pages_beyond_32_bit_offsets(dtype):
     c.check(out, lse, c.expected(), most=float(v[:, -70:].float().abs().max()))
 
 
+@gpu
+@pytest.mark.parametrize("page", [16, 8])
+def test_chunk_waits_that_run_out(page):
+    """Waits of no or few polls give up: the call returns, the status says so, and the next call is right again."""
+    c = Call([(900, 700), (3000, 20), (5, 5)], 8, 2, 128, page, BF16)
+    want, lse = c.run(want_lse=True)
+    c.cache.check()
+    try:
+        for limit in (0, 0, 1, 2, 5, 20):
+            paged.set_wait_limit(limit)
+            for _ in range(3):
+                c.run()
+            if limit == 0:
+                with pytest.raises(binding.OuroError) as e:
+                    c.cache.check()
+                assert e.value.status == binding.OURO_ETIMEOUT
+            paged.set_wait_limit(-1)
+            got, got_lse = c.run(want_lse=True)
+            if limit == 0:
+                c.cache.check()
+            else:                                          # (so few polls may or may not do)
+                try:
+                    c.cache.check()
+                except binding.OuroError as err:
+                    assert err.status == binding.OURO_ETIMEOUT
+            assert torch.equal(got, want) and torch.equal(got_lse, lse)
+    finally:
+        paged.set_wait_limit(-1)
+    c.cache.check()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("page", [16, 20])
+def test_chunk_hidden_values_as_large_as_they_get(dtype, page):
+    """0 times the type's largest value is 0: tokens that come later, and rows of a page behind the end."""
+    c = Call([(300, 150)], 4, 2, 64, page, dtype)
+    clean = c.run()
+    j, pg, row = c.slots(0)
+    big = torch.finfo(dtype).max
+    for at in range(200, 300):
+        c.v[0, pg[at], row[at]] = big if at % 2 else -big
+    out = c.run()
+    assert torch.equal(out[:50], clean[:50])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_chunk_keys_that_are_no_numbers_show_where_they_are_seen(dtype):
+    """Every place of a unit: a NaN among the keys that a token sees leaves it no distribution, and no other token notices."""
+    c = Call([(260, 130)], 2, 1, 64, 16, dtype)
+    clean = c.run()
+    j, pg, row = c.slots(0)
+    starts = i32(c.starts)
+    for at in list(range(60, 130)) + [131, 200, 259]:
+        keep = c.k[0, pg[at], row[at]].clone()
+        c.k[0, pg[at], row[at], :, 3] = float("nan")
+        out = c.cache.attend_chunk(0, c.q, starts)
+        first = max(0, at - 130)
+        assert bool(torch.isnan(out[first:]).all()) and torch.equal(out[:first], clean[:first]), at
+        c.k[0, pg[at], row[at]] = keep
+    assert torch.equal(c.run(), clean)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("H,Hkv,D", [(160, 1, 64), (256, 2, 32), (66, 3, 128)])
+def test_chunk_more_heads_than_a_tile_has_rows(H, Hkv, D, dtype):
+    c = Call([(70, 33), (200, 1), (12, 12)], H, Hkv, D, 16, dtype)
+    out, lse = c.run(want_lse=True)
+    c.check(out, lse, c.expected())
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_chunk_as_many_sequences_as_there_may_be(dtype):
+    r = np.random.default_rng(5)
+    chunks = [(int(a + b), int(b)) for a, b in zip(r.integers(0, 60, 1024), r.integers(0, 4, 1024))]
+    c = Call(chunks, 2, 1, 32, 8, dtype)
+    out, lse = c.run(want_lse=True)
+    c.check(out, lse, c.expected())
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_chunk_lengths_outside_the_table(dtype):
+    c = Call([(64, 10), (64, 10), (30, 10)], 2, 2, 64, 16, dtype, max_pages=4)
+    c.cache.lens.copy_(i32([10 ** 6, -5, 30]))
+    out, lse = c.run(want_lse=True)
+    c.chunks = [(64, 10), (0, 10), (30, 10)]
+    c.check(out, lse, c.expected())
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_chunk_two_caches_at_once(dtype):
+    """Calls on two caches, which have a workspace each, on two streams; and two graphs of one cache, one after the other."""
+    a, b = (Call([(700, 400), (900, 30)], 8, 2, 128, 16, dtype, seed=s) for s in (1, 2))
+    want = [x.run() for x in (a, b)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for _ in range(10):
+        for k, x in enumerate((a, b)):
+            with torch.cuda.stream(streams[k]):
+                got[k].append(x.run())
+    torch.cuda.synchronize()
+    for k in range(2):
+        assert all(torch.equal(x, want[k]) for x in got[k])
+    starts, short = i32(a.starts), i32([0, 100, 103])
+    outs = [torch.zeros_like(a.q) for _ in range(2)]
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    for g, s, o in zip(graphs, (starts, short), outs):
+        with torch.cuda.graph(g):
+            a.cache.attend_chunk(0, a.q, s, out=o)
+    for _ in range(3):
+        for g in graphs:
+            g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], want[0])
+    a.starts = np.array([0, 100, 103])
+    a.check(outs[1], None, a.expected(), torch.zeros_like(a.q))
+
+
 # ---------------------------------------------------------------------------------------------- refusals, on the host
 def fake(dtype=binding.OURO_BF16, **kw):
     """A description whose pointers nothing reads: every call below is refused before it launches anything."""
@@ -360,7 +484,8 @@ def chunk_call(c, layer=0, seqs=None, starts=4096, n=2, rows=8, q=4096, stride=2
 
 @pytest.mark.parametrize("kw", [dict(layer=2), dict(layer=-1), dict(n=-1), dict(n=1025), dict(n=5), dict(rows=-1), dict(heads=0), dict(heads=3), dict(scale=0.0),
                                 dict(scale=float("nan")), dict(scale=float("inf")), dict(q=None), dict(out=None), dict(starts=None), dict(starts=4098), dict(seqs=4097),
-                                dict(lse=4098), dict(q=4104), dict(out=4104), dict(stride=252), dict(stride=192), dict(rows=2 ** 31 - 1)])
+                                dict(lse=4098), dict(q=4104), dict(out=4104), dict(stride=252), dict(stride=192), dict(rows=2 ** 31 - 1),
+                                dict(heads=2 * 65537, stride=2 ** 24)])
 def test_chunk_refuses(kw):
     assert chunk_call(fake(), **kw) == binding.OURO_EINVAL
     assert b"ouro_paged_chunk_attention" in binding.lib().ouro_last_error(None)
