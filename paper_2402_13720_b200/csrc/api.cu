@@ -250,6 +250,15 @@ extern "C" int ouro_create(const ouro_model_desc *t, const ouro_model_mem *tm, c
   if ((e = cudaGetDevice(&dev)) != cudaSuccess || (e = cudaDeviceGetAttribute(&n->sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess ||
       (e = cudaMemsetAsync(n->met_dev, 0, 2 * sizeof(uint32_t), n->stream)) != cudaSuccess)
     return bail(OURO_ECUDA, std::string("device set-up: ") + cudaGetErrorString(e));
+  // Blocks are padded to more rows than they hold, and a forward whose wait gave up leaves its choices unwritten: what stands there
+  // is used as positions, ranges and tokens all the same, so it starts out as some that are valid.
+  if ((e = cudaMemsetAsync(n->a.argmax, 0, OURO_MAX_ROWS * sizeof(int32_t), n->stream)) != cudaSuccess)
+    return bail(OURO_ECUDA, std::string("clearing the choices: ") + cudaGetErrorString(e));
+  for (auto &m : n->m)
+    if (m.present)
+      for (int32_t *words : {m.blk.tok, m.blk.pos, m.blk.group, m.blk.lin_end, m.blk.seg_start, m.blk.seg_len})
+        if ((e = cudaMemsetAsync(words, 0, OURO_TEXT_ROWS * sizeof(int32_t), n->stream)) != cudaSuccess)
+          return bail(OURO_ECUDA, std::string("clearing the blocks: ") + cudaGetErrorString(e));
   launch_pool_clear(n->pool, n->st, n->stream);
   launch_set_state(n->st, n->seq_dev, 1, 0, 1, Leftovers(), n->stream);
   int rc = ouro_fast_setup(n);
@@ -506,7 +515,7 @@ static int forward(ouro_ctx *c, int which, int32_t *argmax_dev, float *logits_de
   }
   if (ouro_fast_embed(c, which, rows) == OURO_ESTATE) {
     ProfScope ps(c, OURO_PROF_EMBED);
-    launch_embed(dt, M.embed, M.blk.tok, rows, d.d_model, a.x, s);
+    launch_embed(dt, M.embed, M.blk.tok, d.vocab, rows, d.d_model, a.x, s);
   }
   for (int l = 0; l < d.n_layers; ++l) {
     const bool kv_only = !argmax_dev && l + 1 == d.n_layers;

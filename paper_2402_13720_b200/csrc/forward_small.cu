@@ -213,7 +213,7 @@ __global__ void __launch_bounds__(THREADS, 1) forward_small_kernel(const __grid_
     constexpr int V = Vec<T>::N;
     if (embedded) {
       Vec<T> e;
-      e.load((const T *)p.embed + (size_t)p.b.tok[r0 + i] * d + k);
+      e.load((const T *)p.embed + rowops::row_of(p.b.tok[r0 + i], p.V) * d + k);
 #pragma unroll
       for (int j = 0; j < V; ++j) xv[j] = e.get(j);
     } else {
@@ -367,7 +367,7 @@ __global__ void __launch_bounds__(THREADS, 1) forward_small_kernel(const __grid_
           const T *const ws[1] = {(const T *)weight + (size_t)n_col * K};
           float old = 0.f;
           if (lane < n)
-            old = embedded ? to_f<T>(((const T *)p.embed)[(size_t)p.b.tok[r0 + lane] * d + n_col]) : __ldcg(p.x + (size_t)(r0 + lane) * d + n_col);
+            old = embedded ? to_f<T>(((const T *)p.embed)[rowops::row_of(p.b.tok[r0 + lane], p.V) * d + n_col]) : __ldcg(p.x + (size_t)(r0 + lane) * d + n_col);
           float acc[1][RT];
           contract<T, 1, RT>(stored(src + (size_t)r0 * K, K), (const T *)nullptr, 0.f, ws, n, K, acc);
           if (lane < n) __stcg(p.x + (size_t)(r0 + lane) * d + n_col, old + of_row<RT>(acc[0], lane));

@@ -1374,6 +1374,7 @@ int ouro_fast_embed(ouro_ctx *c, int which, int rows) {
   e.rows_dev = c->cur_rows_dev;
   e.rows = rows;
   e.d = M.d.d_model;
+  e.vocab = M.d.vocab;
   e.ss_pitch = OURO_TEXT_ROWS;
   if (text_rows(rows)) launch_text_embed(own, c->sms, c->stream);
   return OURO_OK;
@@ -1650,7 +1651,7 @@ struct Tidy {
   float *slots = nullptr;      // [n_slots][128][128]; a call of `rows` rows has used the first rows x 128 words of each
   int n_slots = 0;
 };
-__global__ void argmax_tiles_kernel(const float *tile_max, const int *tile_arg, int tiles, int32_t *out, const Tidy tidy) {
+__global__ void argmax_tiles_kernel(const float *tile_max, const int *tile_arg, int tiles, int vocab, int32_t *out, const Tidy tidy) {
   pdl_trigger();
   pdl_wait();
   const int t = blockIdx.x;
@@ -1678,7 +1679,8 @@ __global__ void argmax_tiles_kernel(const float *tile_max, const int *tile_arg, 
   if (threadIdx.x == 0) {
     for (int w = 1; w < (int)(blockDim.x >> 5); ++w)
       if (sv[w] > bv || (sv[w] == bv && si[w] < bi)) { bv = sv[w]; bi = si[w]; }
-    out[t] = bi == INT_MAX ? 0 : bi;
+    // (a tile whose wait gave up has left its words as they were: what they hold need not be an id)
+    out[t] = (uint32_t)bi < (uint32_t)vocab ? bi : 0;
   }
 }
 
@@ -1704,7 +1706,7 @@ int ouro_fast_head(ouro_ctx *c, int which, int rows, float *logits, int32_t *arg
     const rows_gemm::Plan &pl = fm.rm.plan[G_HEAD];
     const int entries = rows_launch(fm, rows) ? (pl.units + pl.up - 1) / pl.up : (d.vocab + TILE_N - 1) / TILE_N;
     launch_pdl(argmax_tiles_kernel, rows, 128, 0, c->stream, (const float *)c->fast->s.tile_max, (const int *)c->fast->s.tile_arg,
-               entries, argmax_dev, Tidy());
+               entries, (int)d.vocab, argmax_dev, Tidy());
   }
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) {
@@ -1868,7 +1870,7 @@ extern "C" int ouro_lm_head_static(const void *x_dev, const void *lm_head_dev, i
   Tidy tidy;
   tidy.slots = p.scratch;
   tidy.n_slots = 2 * cut_by;
-  argmax_tiles_kernel<<<rows, 128, 0, s>>>(p.tile_max, p.tile_arg, tiles, argmax_dev, tidy);
+  argmax_tiles_kernel<<<rows, 128, 0, s>>>(p.tile_max, p.tile_arg, tiles, vocab, argmax_dev, tidy);
   int status = 0;
   if ((e = cudaGetLastError()) != cudaSuccess ||
       (e = cudaMemcpyAsync(&status, p.status, sizeof(int), cudaMemcpyDeviceToHost, s)) != cudaSuccess ||

@@ -9,6 +9,7 @@
 // library (the paper observes small differences "caused by floating point error", Appendix A).
 #include "ouro_internal.h"
 #include "generic.cuh"
+#include "row_ops.cuh"
 
 // ------------------------------------------------------------------------------ rotary table
 // cos/sin of pos * theta^(-2i/h), evaluated in double once at set-up.
@@ -28,17 +29,17 @@ void launch_rope_table(float *cos_t, float *sin_t, int max_seq, int head_dim, fl
 
 // --------------------------------------------------------------------------------- embedding
 template <typename T>
-__global__ void embed_kernel(const T *E, const int32_t *tok, int d, float *x) {
+__global__ void embed_kernel(const T *E, const int32_t *tok, int vocab, int d, float *x) {
   pdl_trigger();
   pdl_wait();
-  const T *src = E + (size_t)tok[blockIdx.x] * d;
+  const T *src = E + rowops::row_of(tok[blockIdx.x], vocab) * d;
   float *dst = x + (size_t)blockIdx.x * d;
   for (int i = threadIdx.x; i < d; i += blockDim.x) dst[i] = to_f<T>(src[i]);
 }
-void launch_embed(int dtype, const void *E, const int32_t *tok, int rows, int d, float *x, cudaStream_t s) {
+void launch_embed(int dtype, const void *E, const int32_t *tok, int vocab, int rows, int d, float *x, cudaStream_t s) {
   OURO_COUNT_LAUNCH();
-  if (dtype == OURO_BF16) launch_pdl(embed_kernel<__nv_bfloat16>, rows, 256, 0, s, (const __nv_bfloat16 *)E, tok, d, x);
-  else launch_pdl(embed_kernel<float>, rows, 256, 0, s, (const float *)E, tok, d, x);
+  if (dtype == OURO_BF16) launch_pdl(embed_kernel<__nv_bfloat16>, rows, 256, 0, s, (const __nv_bfloat16 *)E, tok, vocab, d, x);
+  else launch_pdl(embed_kernel<float>, rows, 256, 0, s, (const float *)E, tok, vocab, d, x);
 }
 
 // ----------------------------------------------------------------------------------- RMSNorm

@@ -220,7 +220,7 @@ struct GemmSegs {  // up to three weight matrices [n_i, K] stacked along the out
 };
 enum { EPI_STORE = 0, EPI_RESIDUAL = 1 };
 void launch_rope_table(float *cos_t, float *sin_t, int max_seq, int head_dim, float theta, cudaStream_t s);
-void launch_embed(int dtype, const void *E, const int32_t *tok, int rows, int d, float *x, cudaStream_t s);
+void launch_embed(int dtype, const void *E, const int32_t *tok, int vocab, int rows, int d, float *x, cudaStream_t s);
 void launch_rmsnorm(int dtype, const float *x, const void *g, int rows, int d, float eps, void *out, cudaStream_t s);
 void launch_gemm_simple(int dtype, const void *X, const GemmSegs &W, int rows, int K, float *Y, int ldy, int epi,
                         cudaStream_t s);

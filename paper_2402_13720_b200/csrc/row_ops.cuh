@@ -57,7 +57,11 @@ struct Embed {
   float *ss;                    // [d / 128][ss_pitch] sums of squares per 128-column tile
   const int *rows_dev;
   int rows, d, ss_pitch;
+  int vocab;                    // rows of the table
 };
+// The table's row of a token.  A forward whose wait gave up leaves its greedy choices unwritten, and what stands in their place is
+// taken for tokens by the launches queued behind it: they gather some row of the table then, never one outside it.
+__device__ __forceinline__ size_t row_of(int32_t token, int vocab) { return min((uint32_t)token, (uint32_t)vocab - 1); }
 // One warp per (row, tile): four columns per lane.  Items first, first + step, ..
 __device__ __forceinline__ void embed(const Embed &e, int first, int step, int lane) {
   const int rows = e.rows_dev ? min(e.rows, __ldg(e.rows_dev)) : e.rows, tiles = (e.d + 127) / 128;
@@ -65,7 +69,7 @@ __device__ __forceinline__ void embed(const Embed &e, int first, int step, int l
     const int r = it / tiles, col = (it - r * tiles) * 128 + 4 * lane;
     float sq = 0.f;
     if (col < e.d) {                                            // d is a multiple of 64: four columns are in or out together
-      const uint2 raw = __ldg(reinterpret_cast<const uint2 *>(e.table + (size_t)__ldg(e.tok + r) * e.d + col));
+      const uint2 raw = __ldg(reinterpret_cast<const uint2 *>(e.table + row_of(__ldg(e.tok + r), e.vocab) * e.d + col));
       const uint2 graw = __ldg(reinterpret_cast<const uint2 *>(e.gain + col));
       const float2 a = unpack(raw.x), b = unpack(raw.y), ga = unpack(graw.x), gb = unpack(graw.y);
       *reinterpret_cast<float4 *>(e.x + (size_t)r * e.d + col) = make_float4(a.x, a.y, b.x, b.y);
@@ -84,7 +88,7 @@ __device__ __forceinline__ void embed_packets(const Embed &e, int first, int ste
   for (int it = first; it < (e.d + 127) / 128; it += step) {
     const int col = it * 128 + 4 * lane;
     if (col >= e.d) continue;
-    const uint2 raw = __ldg(reinterpret_cast<const uint2 *>(e.table + (size_t)__ldg(e.tok) * e.d + col));
+    const uint2 raw = __ldg(reinterpret_cast<const uint2 *>(e.table + row_of(__ldg(e.tok), e.vocab) * e.d + col));
     const uint2 graw = __ldg(reinterpret_cast<const uint2 *>(e.gain + col));
     const float2 a = unpack(raw.x), b = unpack(raw.y), ga = unpack(graw.x), gb = unpack(graw.y);
     *reinterpret_cast<float4 *>(e.x + col) = make_float4(a.x, a.y, b.x, b.y);
