@@ -1,6 +1,6 @@
 """Several continuations of one prompt at once: beam search over a paged cache.
 
-    python -m paper_2402_13720_b200.beams [--config C1] [--beams 4] [--new 32] [--layers N] [--chunk 512] [--repetition 1.0]
+    python -m paper_2402_13720_b200.beams [--config C1] [--beams 4] [--new 32] [--layers N] [--chunk 16] [--repetition 1.0]
 
 One step of the search: the scores of every beam's best tokens (``token_logprobs``), the best beams among them, the pages of their parents
 (``PagedCache.fork``), room for a token (``extend``, which copies an unfinished page that several beams share), and a forward pass whose layers
@@ -119,8 +119,8 @@ class BeamDecoder:
     def search(self, prompt, max_new: int, *, repetition: float | None = None, presence: float | None = None, frequency: float | None = None,
                bias: torch.Tensor | None = None, allowed=None):
         """The ``beams`` best continuations of max_new tokens that a beam search finds: tokens [beams, max_new], sums of log probabilities
-        [beams], best first.  Rules as in ``constrain_logits``, penalties for what the prompt and the continuation have; ``allowed``: the words of
-        a mask, or a function of the texts [rows, length] int32 (prompt first) that gives the words [rows, ceil(vocab / 32)] of theirs."""
+        [beams], best first.  Rules as in ``constrain_logits``, penalties for what the prompt and the continuation have, ``bias`` [vocab]; ``allowed``: the words of
+        one mask for all, or a function of the texts [rows, length] int32 (prompt first) that gives the words [rows, ceil(vocab / 32)] of theirs."""
         prompt, _ = self._text(prompt, new=max_new)
         m, B, c = self.m, self.beams, self.cache
         rules = dict(repetition=repetition, presence=presence, frequency=frequency, bias=bias, allowed=allowed)

@@ -30,12 +30,6 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
-__device__ __forceinline__ float4 load4(const float *p) { return *(const float4 *)p; }
-__device__ __forceinline__ float4 load4(const __nv_bfloat16 *p) {
-  const uint2 t = *(const uint2 *)p;
-  const float2 a = rowops::unpack(t.x), b = rowops::unpack(t.y);
-  return make_float4(a.x, a.y, b.x, b.y);
-}
 __device__ __forceinline__ void store4(float *p, float4 x) { *(float4 *)p = x; }
 __device__ __forceinline__ void store4(__nv_bfloat16 *p, float4 x) { *(uint2 *)p = make_uint2(rowops::pack(x.x, x.y), rowops::pack(x.z, x.w)); }
 __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f; }
