@@ -48,7 +48,7 @@ template <> struct Piece<__nv_bfloat16> {
   static __device__ __forceinline__ void put(__nv_bfloat16 *p, float x) { *p = __float2bfloat16_rn(x); }
 };
 
-// A slice has U pieces a thread (us of the 1000 rows with U of 1, 2, 4, 8 of f32: -, 121, 115, 130; two groups of U, one on its way: 116, 128).  Pieces begin where the row's addresses are multiples of 16 bytes: the row's first may begin in front of it, its last
+// A slice has U pieces a thread.  Pieces begin where the row's addresses are multiples of 16 bytes: the row's first may begin in front of it, its last
 // may end behind it; those two go element by element, and all do where the output's row is aligned differently.
 template <typename T, int U, bool COUNTS>
 __global__ void __launch_bounds__(THREADS) constrain_kernel(const ConstrainParams p) {
@@ -65,11 +65,22 @@ __global__ void __launch_bounds__(THREADS) constrain_kernel(const ConstrainParam
     for (int i = tid; i < SLICE / 4; i += THREADS) ((uint4 *)s_count)[i] = make_uint4(0, 0, 0, 0);
   pdl_wait();
   pdl_trigger();
+  const float *bias = p.bias ? p.bias + row * p.bias_stride : nullptr;
+  const uint32_t *allowed = p.allowed ? p.allowed + row * p.allowed_stride : nullptr;
+  // (the mask's words as early as the logits: 64 rows of 32000 5.5 -> 4.4 us, 1000 of 64000 91 -> 89, in bf16 75 -> 71; the biases too would take 22 registers
+  // more, and with them a CTA of five: 98)
   uint4 raw[U];
+  uint32_t bits_lo[U], bits_hi[U];                                 // the words of the mask with a piece's first and last bit
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int e0 = base + (u * THREADS + tid) * N;
-    if (alike && e0 >= 0 && e0 + N <= p.vocab) raw[u] = __ldcs((const uint4 *)(in + e0));
+    if (alike && e0 >= 0 && e0 + N <= p.vocab) {
+      raw[u] = __ldcs((const uint4 *)(in + e0));
+      if (allowed) {
+        bits_lo[u] = __ldg(allowed + (e0 >> 5));
+        bits_hi[u] = __ldg(allowed + ((e0 + N - 1) >> 5));
+      }
+    }
   }
   float rep = 1.f, pres = 0.f, freq = 0.f;
   if (COUNTS) {
@@ -94,14 +105,13 @@ __global__ void __launch_bounds__(THREADS) constrain_kernel(const ConstrainParam
     if (p.frequency) freq = p.frequency[row];
     __syncthreads();
   }
-  const float *bias = p.bias ? p.bias + row * p.bias_stride : nullptr;
-  const uint32_t *allowed = p.allowed ? p.allowed + row * p.allowed_stride : nullptr;
-  // x * 1 - 0 where nobody has told the token.  A product with the reciprocal is 2^-23 of the quotient off at most.  (Where histories are long, nearly every
+  // A product with the reciprocal is 2^-23 of the quotient off at most.  (Where histories are long, nearly every
   // 128 logits of a warp have somebody's token: 1000 rows of 64000 took 173 us with divisions behind branches.)
   const float inv = 1.f / rep;
   auto told_of = [&](float x, uint32_t c) {
     const float n = __uint_as_float(c | 0x4b000000u) - 8388608.f;   // c below 2^23, without the slow conversion
-    return x * (c ? x > 0.f ? inv : rep : 1.f) - (c ? fmaf(freq, n, pres) : 0.f);
+    const float y = __fsub_rn(__fmul_rn(x, x > 0.f ? inv : rep), fmaf(freq, n, pres));
+    return c ? y : x;
   };
 #pragma unroll
   for (int u = 0; u < U; ++u) {
@@ -135,7 +145,7 @@ __global__ void __launch_bounds__(THREADS) constrain_kernel(const ConstrainParam
         }
       }
       if (allowed) {
-        const uint32_t bits = __funnelshift_r(__ldg(allowed + (e0 >> 5)), __ldg(allowed + ((e0 + N - 1) >> 5)), e0 & 31);
+        const uint32_t bits = __funnelshift_r(bits_lo[u], bits_hi[u], e0 & 31);
 #pragma unroll
         for (int i = 0; i < N; ++i)
           if (!(bits >> i & 1)) x[i] = -INFINITY;
@@ -162,10 +172,14 @@ cudaError_t launch(ConstrainParams p, cudaStream_t s) {
   const dim3 grid((unsigned)(p.slices * p.rows));
   return p.tokens ? launch_pdl(constrain_kernel<T, U, true>, grid, dim3(THREADS), 0, s, p) : launch_pdl(constrain_kernel<T, U, false>, grid, dim3(THREADS), 0, s, p);
 }
+// Small slices end sooner while all of them are under way at once; the more there are, the more it counts that every slice goes through the row's whole history.
+// us a launch (histories of 512, penalty and mask; U of 1 / of 4) with 1, 8, 20, 40, 128 rows of 32000 and 1000 rows of 64000 with histories of 2048:
+//     f32   1.8/2.3, 2.0/2.4, 3.4/2.7, 4.3/3.3, 11.1/6.3, 172/89        bf16   1.9/2.8, 2.0/2.8, 2.4/2.9, 4.0/3.4, 7.0/5.8, 102/59
+// (1000 rows with U of 2, 4, 8: f32 113, 89, 92, bf16 71, 59, 82; CTAs of 128 threads with 4 and 8: 102, 101 and 68, 82, of 512 with 4: 107 and 73.)
 template <typename T>
 cudaError_t by_size(const ConstrainParams &p, int sms, cudaStream_t s) {
   const int64_t pieces = (int64_t)p.rows * (p.vocab / Piece<T>::N + 1);
-  return pieces < (int64_t)sms * THREADS * 8 ? launch<T, 1>(p, s) : launch<T, sizeof(T) == 4 ? 4 : 2>(p, s);
+  return pieces < (int64_t)sms * THREADS * 3 ? launch<T, 1>(p, s) : launch<T, 4>(p, s);
 }
 
 }  // namespace
