@@ -351,7 +351,8 @@ int ouro_paged_attention(const ouro_paged_cache *cache, int32_t layer, const int
  * rows starts_dev[i] .. starts_dev[i+1]-1 (starts_dev [n+1], not descending, within 0 .. rows; none is allowed).  Of m new tokens the t-th sees the keys
  * 0 .. lens - m + t.  out [rows, n_heads, head_dim], lse_dev [rows, n_heads] (may be NULL): rows of no sequence are left as they are.  Tokens that see no
  * key, missing pages and sequences outside the table as above; starts that descend or leave 0 .. rows make the call do nothing (OURO_EINVAL in the cache's
- * status).  seqs_dev may name a sequence twice.  Two launches (one where no sequence can have 256 keys, bf16: 384); a page_size that is a multiple of 8 is faster in bf16.  Sums and maxima are held in 32 bits; in
+ * status).  seqs_dev may name a sequence twice.  Two launches (one where no sequence can have 256 keys, bf16: 384); a page_size that is a multiple of 8 is faster in bf16.  Sums and maxima are held in 32 bits; f32
+ * products are made of parts with 11 bits each, to 2^-21; an infinity among the queries, keys and values that a token sees gives infinities or NaN; in
  * bf16 a probability may go into the second product rounded to bf16, so that an output is off by up to 2^-8 of its probabilities' weighted |values| besides
  * its own rounding.  rows * n_heads / n_kv_heads and (max_pages * page_size + 1024) * n_heads / n_kv_heads are at most 2^31 - 65536, n_heads / n_kv_heads 65536. */
 int ouro_paged_chunk_attention(const ouro_paged_cache *cache, int32_t layer, const int32_t *seqs_dev, const int32_t *starts_dev, int32_t n, int32_t rows,

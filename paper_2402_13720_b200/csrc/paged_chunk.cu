@@ -4,12 +4,17 @@
 //     o_i = sum_j e^(s_ij) v_j / sum_j e^(s_ij),   s_ij = scale q_i . k_j,   j = 0 .. len - m + i for the i-th of a sequence's m new tokens
 //
 // Four operations a query head, key and dimension: behind a few dozen query rows the contractions are what counts, not the keys' bytes.  bf16 goes to
-// paged_chunk_tc.cu.  Here a CTA has 64 query rows in shared memory, passes over the keys 64 at a time and keeps maximum, sum and output of its rows in
-// registers; all in 32 bits.  A thread has 4 rows and every sixteenth key, then 4 rows and every sixteenth group of four dims.  The next keys are asked for when the
-// scores are done, the next values when the outputs are, and the ids of their pages a unit before that.  What bounds it is what comes from shared memory
-// (16 bytes to a lane take four cycles a warp, whoever else wants them): a unit of 128 dims takes an SM 8 us, two CTAs or one, so that a call of few units is best
-// dealt out one by one (five prompts of the `small` shape, up to 411 tokens: 60 us, with runs from 2 units on 77; 4096 tokens, four heads of 128: 503 us, 34
-// TFLOP/s).  8 rows to a thread, who then has to read a third less, leave too few warps: 83 and 544.
+// paged_chunk_tc.cu.  Here a CTA has 64 query rows in shared memory, 16 to a warp, passes over the keys 64 at a time and keeps maximum, sum and output of its
+// rows in registers.  The next keys are asked for when the scores are done, the next values when the outputs are, and the ids of their pages a unit before that.
+// Products of f32 are three contractions (mma.sync, 8 deep, 11 bits an operand): x y = X Y + X y' + x' Y with the upper and the lower 11 bits of each, and x' y'
+// (2^-22 of the product at most, of either sign) left out.  The tensor cores round their sums towards 0, which counts in long chains (one for a score,
+// one for an output: 2.5e-6 of the norm off, 44 us for 46 below): the small products and every 32 dims, or 64 keys, of the large ones have sums of their own, which are added up in
+// 32 bits.  Outputs are as near to 64 bits as those of 32-bit multiply-adds (5.7e-7 of their norm for 7.9e-7).  4096 tokens, four heads of 128: 372 us, 46
+// TFLOP/s; multiply-adds by four rows and four keys a thread 503, bound by what came from shared memory; the contractions alone would take 180.  Two CTAs an SM
+// are eight warps, too few to hide one another's chains of loads, parts and contractions.  A call of few units is best dealt out one by one (five prompts of the
+// `small` shape, up to 411 tokens: 46 us).
+#include <cfloat>
+
 #include "paged_chunk.cuh"
 #include "row_ops.cuh"
 
@@ -20,7 +25,7 @@ using paged::ChunkWalk;
 
 const char *CALL = "ouro_paged_chunk_attention";
 
-constexpr int R = paged::CHUNK_ROWS, KEYS = 64, THREADS = 256, RT = R / (THREADS / 16);            // RT: rows of a thread
+constexpr int R = paged::CHUNK_ROWS, KEYS = 64, THREADS = 128;
 constexpr int ITEM_COST = 1, SNAP = 0, MIN_RUN = 1;
 typedef paged::ChunkRuns<R, KEYS, ITEM_COST, SNAP, MIN_RUN> Share;
 
@@ -60,20 +65,44 @@ __device__ __forceinline__ void bring(float *const *dst, const __nv_bfloat16 *co
 
 template <int D>
 struct Cfg {
-  static constexpr int PITCH = D + 4;                              // (eight threads that read eight rows meet different banks)
-  static constexpr int HALF = KEYS / 2, P_PITCH = HALF + 4;        // probabilities pass through shared memory half a unit at a time: two CTAs fit an SM
-  static constexpr int OFF_K = R * PITCH, OFF_V = OFF_K + KEYS * PITCH, OFF_P = OFF_V + KEYS * D, OFF_MISC = OFF_P + R * P_PITCH;
+  static constexpr int PITCH = D + 16, V_PITCH = D + 4;            // (fragments of 16 bytes a lane meet every bank once in eight lanes)
+  static constexpr int OFF_K = R * PITCH, OFF_V = OFF_K + KEYS * PITCH, OFF_AT = OFF_V + KEYS * V_PITCH, OFF_MISC = OFF_AT + 2 * KEYS;
   static constexpr int PLAN = 5 * OURO_MAX_LIST;                   // at the beginning, until the first queries
   static constexpr int BYTES = ((OFF_MISC > PLAN ? OFF_MISC : PLAN) + 64) * 4;
 };
 
+// x = big + small, both with the 11 bits that a contraction takes (of the small part it takes the upper ones).  NEAR: big is the nearest, so that the
+// products of two small parts, which are left out, are no bias; else the next towards 0, which the type's largest value has too.
+template <bool NEAR>
+__device__ __forceinline__ void split(float x, uint32_t &big, uint32_t &small) {
+  big = (__float_as_uint(x) + (NEAR ? 0x1000u : 0u)) & 0xffffe000u;
+  small = __float_as_uint(x - __uint_as_float(big));
+}
+template <bool NEAR, bool EXACT>                                   // EXACT: no more than 8 bits to begin with
+__device__ __forceinline__ void split4(const float4 &x, uint32_t *big, uint32_t *small) {
+  const float y[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (EXACT) big[i] = __float_as_uint(y[i]);
+    else split<NEAR>(y[i], big[i], small[i]);
+}
+__device__ __forceinline__ void contract(float *c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ bool finite4(const float4 &x) {
+  return fabsf(x.x) <= FLT_MAX && fabsf(x.y) <= FLT_MAX && fabsf(x.z) <= FLT_MAX && fabsf(x.w) <= FLT_MAX;
+}
+
 template <typename T, int D>
 __global__ void __launch_bounds__(THREADS, 2) paged_chunk_kernel(const ChunkParams p) {
   using C = Cfg<D>;
-  constexpr int D4 = D / 4, OUT = (D4 + 15) / 16;                  // groups of four dims; those of a thread
+  constexpr int D4 = D / 4, Q32 = D / 32;                          // groups of four dims, of 32
+  constexpr bool EXACT = sizeof(T) == 2;
   extern __shared__ __align__(16) float smem[];
-  float *qs = smem, *ks = smem + C::OFF_K, *vs = smem + C::OFF_V, *ps = smem + C::OFF_P;
-  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+  float *qs = smem, *ks = smem + C::OFF_K, *vs = smem + C::OFF_V;
+  int64_t *ats = (int64_t *)(smem + C::OFF_AT);                    // where a unit's keys lie in their pool; -1: on no page
+  const int tid = threadIdx.x, lane = tid & 31, g = lane >> 2, t = lane & 3, r0 = tid / 32 * 16 + g;       // the thread's rows: r0, r0 + 8
   const Share runs(p);
   runs.touch();
   pdl_wait();
@@ -88,189 +117,257 @@ __global__ void __launch_bounds__(THREADS, 2) paged_chunk_kernel(const ChunkPara
     // ---- an item, or the part of it in this run
     const int rows = min(R, w.m * p.group - w.rt * R), part_begin = w.unit;
     const int last = w.s == end.s && w.head == end.head && w.rt == end.rt ? end.unit : w.units;
-    constexpr int PER = KEYS * D4 / THREADS;                       // pieces of four values of a unit's keys, or of the queries, for a thread
-    static_assert(R == KEYS && KEYS * D4 % THREADS == 0, "");
-    float *dst[PER];
-    const T *src[PER];
-    bool there[PER];
-    int ids[PER];
+    constexpr int PER = KEYS * D4 / THREADS, BATCH = PER < 8 ? PER : PER / 2;    // pieces of four values of a unit's keys, or of the queries, for a thread
+    static_assert(R == KEYS && KEYS <= THREADS && KEYS * D4 % THREADS == 0 && PER % BATCH == 0, "");
     auto row_of = [&](int i) { return (tid + i * THREADS) / D4; };
     auto col_of = [&](int i) { return (tid + i * THREADS) % D4 * 4; };
-    auto ask_ids = [&](int unit) {                                 // of the pages that a unit's keys lie on
+    int id = -1;                                                   // of the page of a thread's key
+    auto ask_id = [&](int unit) {
+      const int key = unit * KEYS + tid;
+      id = tid < KEYS && unit < last && key < w.len ? w.row[p.page.quot(key)] : -1;
+    };
+    auto place = [&](int unit) {                                   // the unit's keys, once their pages are known; true: one of the sequence's is on none
+      if (tid >= KEYS) return false;
+      const int key = unit * KEYS + tid;
+      const bool there = id >= 0 && id < p.n_pages;
+      ats[tid] = there ? (int64_t)id * p.page_bytes + (int64_t)(key - p.page.quot(key) * (int)p.page.d) * p.slot_bytes : -1;
+      return unit < last && key < w.len && !there;
+    };
+    auto ask = [&](const uint8_t *pool, float *to, int pitch) {    // a unit's keys or values
+      const uint8_t *of_head = pool + (int64_t)w.head * p.head_bytes;
 #pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        const int key = unit * KEYS + row_of(i);
-        ids[i] = unit < last && key < w.len ? w.row[p.page.quot(key)] : -1;
+      for (int i0 = 0; i0 < PER; i0 += BATCH) {
+        float *dst[BATCH];
+        const T *src[BATCH];
+        bool there[BATCH];
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+          const int64_t at = ats[row_of(i0 + i)];
+          there[i] = at >= 0;
+          dst[i] = to + row_of(i0 + i) * pitch + col_of(i0 + i);
+          src[i] = (const T *)(of_head + (there[i] ? at : 0)) + col_of(i0 + i);
+        }
+        bring<BATCH>(dst, src, there);
       }
     };
-    auto ask = [&](const uint8_t *pool, float *to, int pitch, int unit) {        // a unit's keys or values
-#pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        const int key = unit * KEYS + row_of(i), row = key - p.page.quot(key) * (int)p.page.d;
-        there[i] = ids[i] >= 0 && ids[i] < p.n_pages;
-        dst[i] = to + row_of(i) * pitch + col_of(i);
-        src[i] = (const T *)(pool + (there[i] ? (int64_t)ids[i] * p.page_bytes + (int64_t)row * p.slot_bytes : 0) + (int64_t)w.head * p.head_bytes) + col_of(i);
-      }
-      bring<PER>(dst, src, there);
-    };
-    auto lost = [&](int unit) {                                    // keys of the sequence on no page
-      bool any = false;
-#pragma unroll
-      for (int i = 0; i < PER; ++i) any |= unit * KEYS + row_of(i) < w.len && !(ids[i] >= 0 && ids[i] < p.n_pages);
-      return any;
-    };
-    ask_ids(w.unit);
+    ask_id(w.unit);
     __syncthreads();                                               // (what was there has been read)
+    bool missing = place(w.unit);
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      there[i] = row_of(i) < rows;
-      const int at = w.rt * R + (there[i] ? row_of(i) : 0), tok = p.group_of.quot(at);
-      dst[i] = qs + row_of(i) * C::PITCH + col_of(i);
-      src[i] = (const T *)p.q + (int64_t)(w.start + tok) * p.q_stride + (int64_t)(w.head * p.group + at - tok * p.group) * D + col_of(i);
+    for (int i0 = 0; i0 < PER; i0 += BATCH) {
+      float *dst[BATCH];
+      const T *src[BATCH];
+      bool there[BATCH];
+#pragma unroll
+      for (int i = 0; i < BATCH; ++i) {
+        const int r = row_of(i0 + i);
+        there[i] = r < rows;
+        const int at = w.rt * R + (there[i] ? r : 0), tok = p.group_of.quot(at);
+        dst[i] = qs + r * C::PITCH + col_of(i0 + i);
+        src[i] = (const T *)p.q + (int64_t)(w.start + tok) * p.q_stride + (int64_t)(w.head * p.group + at - tok * p.group) * D + col_of(i0 + i);
+      }
+      bring<BATCH>(dst, src, there);
     }
-    bring<PER>(dst, src, there);
-    bool missing = lost(w.unit);
-    ask(p.k, ks, C::PITCH, w.unit);
+    ask_id(w.unit + 1);
+    __syncthreads();
+    ask(p.k, ks, C::PITCH);
     commit();
-    ask(p.v, vs, D, w.unit);
+    ask(p.v, vs, C::V_PITCH);
     commit();
-    ask_ids(w.unit + 1);
-    int vis[RT];
-    float m[RT], l[RT], o[RT][OUT][4];
+    int vis[2];
+    float m[2], l[2], o[Q32][4][4];                                // o[q][i]: dims 32 q + 8 t + i and + 4 of the first row, then of the second
 #pragma unroll
-    for (int i = 0; i < RT; ++i) {
-      vis[i] = ty * RT + i < rows ? runs.sees(w, w.rt * R + ty * RT + i) : 0;
+    for (int i = 0; i < 2; ++i) {
+      vis[i] = r0 + 8 * i < rows ? runs.sees(w, w.rt * R + r0 + 8 * i) : 0;
       m[i] = -INFINITY;
       l[i] = 0.f;
-#pragma unroll
-      for (int x = 0; x < OUT; ++x)
-#pragma unroll
-        for (int d = 0; d < 4; ++d) o[i][x][d] = 0.f;
     }
+#pragma unroll
+    for (int q = 0; q < Q32; ++q)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[q][i][c] = 0.f;
     const int all_see = runs.sees(w, w.rt * R);                    // keys that every row sees
     for (; w.unit < last; ++w.unit) {
       const int key0 = w.unit * KEYS;
       wait_but_one();
       const bool gone = __syncthreads_or(missing);                 // (queries and keys are there)
-      float s[RT][4];                                              // [row][key tx + 16 j]
+      float s[8][4];                                               // s[n]: keys 8 n + 2 t and the next of the first row, then of the second
+      // Dims in any order, the same for both: a lane's 16 bytes are two steps of eight.  Contractions round their sums towards 0: products with small parts
+      // are summed up by themselves, those of big parts 32 dims at a time.
 #pragma unroll
-      for (int i = 0; i < RT; ++i)
+      for (int n0 = 0; n0 < 8; n0 += 4) {
+        float fine[4][4] = {};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
-#pragma unroll 4
-      for (int d = 0; d < D; d += 4) {
-        float4 a[RT], b[4];
+        for (int n = 0; n < 4; ++n)
 #pragma unroll
-        for (int i = 0; i < RT; ++i) a[i] = *(const float4 *)(qs + (ty * RT + i) * C::PITCH + d);
+          for (int c = 0; c < 4; ++c) s[n0 + n][c] = 0.f;
+#pragma unroll 1
+        for (int d0 = 0; d0 < D; d0 += 32) {
+          float sum[4][4] = {};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) b[j] = *(const float4 *)(ks + (tx + 16 * j) * C::PITCH + d);
+          for (int d = 0; d < 32; d += 16) {
+            uint32_t ab[2][4], as[2][4], bb[4][4], bs[4][4];
 #pragma unroll
-        for (int i = 0; i < RT; ++i)
+            for (int i = 0; i < 2; ++i) split4<true, EXACT>(*(const float4 *)(qs + (r0 + 8 * i) * C::PITCH + d0 + d + 4 * t), ab[i], as[i]);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) s[i][j] = fmaf(a[i].w, b[j].w, fmaf(a[i].z, b[j].z, fmaf(a[i].y, b[j].y, fmaf(a[i].x, b[j].x, s[i][j]))));
+            for (int n = 0; n < 4; ++n) split4<false, EXACT>(*(const float4 *)(ks + (8 * (n0 + n) + g) * C::PITCH + d0 + d + 4 * t), bb[n], bs[n]);
+#pragma unroll
+            for (int h = 0; h < 4; h += 2) {
+              if (!EXACT) {
+#pragma unroll
+                for (int n = 0; n < 4; ++n) contract(fine[n], as[0][h], as[1][h], as[0][h + 1], as[1][h + 1], bb[n][h], bb[n][h + 1]);
+#pragma unroll
+                for (int n = 0; n < 4; ++n) contract(fine[n], ab[0][h], ab[1][h], ab[0][h + 1], ab[1][h + 1], bs[n][h], bs[n][h + 1]);
+              }
+#pragma unroll
+              for (int n = 0; n < 4; ++n) contract(sum[n], ab[0][h], ab[1][h], ab[0][h + 1], ab[1][h + 1], bb[n][h], bb[n][h + 1]);
+            }
+          }
+#pragma unroll
+          for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) s[n0 + n][c] += sum[n][c];
+        }
+        if (!EXACT)
+#pragma unroll
+          for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) s[n0 + n][c] += fine[n][c];
       }
+      missing = place(w.unit + 1);
       __syncthreads();                                             // the keys have been read
-      missing = lost(w.unit + 1);
-      ask(p.k, ks, C::PITCH, w.unit + 1);
+      if (w.unit + 1 < last) ask(p.k, ks, C::PITCH);               // (behind the last unit the next item's follow)
       commit();
+      ask_id(w.unit + 2);
       const bool edge = gone || key0 + KEYS > all_see;             // (the same for the CTA) not every row sees every key
       if (edge) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int key = key0 + tx + 16 * j;
-          bool on = key < w.len;
-          if (gone && on) {
-            const int id = w.row[p.page.quot(key)];
-            on = id >= 0 && id < p.n_pages;
+        for (int n = 0; n < 8; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int key = key0 + 8 * n + 2 * t + e;
+            bool on = key < w.len;
+            if (gone && on) {
+              const int of = w.row[p.page.quot(key)];
+              on = of >= 0 && of < p.n_pages;
+            }
+            if (!on || key >= vis[0]) s[n][e] = -INFINITY;
+            if (!on || key >= vis[1]) s[n][2 + e] = -INFINITY;
           }
-#pragma unroll
-          for (int i = 0; i < RT; ++i)
-            if (!on || key >= vis[i]) s[i][j] = -INFINITY;
-        }
       }
+      float grown[2];
 #pragma unroll
-      for (int i = 0; i < RT; ++i) {
-        float top = fmaxf(fmaxf(s[i][0], s[i][1]), fmaxf(s[i][2], s[i][3]));
+      for (int i = 0; i < 2; ++i) {
+        float top = fmaxf(s[0][2 * i], s[0][2 * i + 1]);
 #pragma unroll
-        for (int x = 8; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+        for (int n = 1; n < 8; ++n) top = fmaxf(top, fmaxf(s[n][2 * i], s[n][2 * i + 1]));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
         top = fmaxf(m[i], top * p.scale_log2);
-        const float base = base_of(top), a = ex2(m[i] - base);
+        const float base = base_of(top);
+        grown[i] = ex2(m[i] - base);
         m[i] = top;
-        l[i] *= a;
+        l[i] *= grown[i];
 #pragma unroll
-        for (int x = 0; x < OUT; ++x)
+        for (int n = 0; n < 8; ++n)
 #pragma unroll
-          for (int d = 0; d < 4; ++d) o[i][x][d] *= a;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          s[i][j] = ex2(fmaf(s[i][j], p.scale_log2, -base));
-          l[i] += s[i][j];
-        }
+          for (int e = 0; e < 2; ++e) {
+            float &x = s[n][2 * i + e];
+            x = ex2(fmaf(x, p.scale_log2, -base));
+            l[i] += x;
+          }
       }
       wait_but_one();
       __syncthreads();                                             // (values are there)
-      // At an edge, 0 times a value that is no finite number must be 0 for the rows that do not see it.
-      auto pv = [&](auto at_edge, int half) {
-#pragma unroll 2
-        for (int key = 0; key < C::HALF; key += 4) {
-          float4 a[RT];
+      if (edge) {
+        // 0 times a value that is no finite number must be 0 for the rows that do not see it: such values are taken out, and added for those that do (rare).
+        bool odd = false;
 #pragma unroll
-          for (int i = 0; i < RT; ++i) a[i] = *(const float4 *)(ps + (ty * RT + i) * C::P_PITCH + key);
+        for (int i = 0; i < PER; ++i) odd |= !finite4(*(const float4 *)(vs + row_of(i) * C::V_PITCH + col_of(i)));
+        if (__syncthreads_or(odd)) {
+          for (int i = 0; i < 2; ++i) grown[i] = fmaxf(grown[i], FLT_MIN);         // (an infinity times 0 would be none)
+#pragma unroll 1
+          for (int key = 0; key < KEYS; ++key) {
+            float x[2] = {0.f, 0.f};
 #pragma unroll
-          for (int kk = 0; kk < 4; ++kk)
-#pragma unroll
-            for (int x = 0; x < OUT; ++x) {
-              if (tx + 16 * x >= D4) continue;
-              const float4 b = *(const float4 *)(vs + (half * C::HALF + key + kk) * D + (tx + 16 * x) * 4);
-#pragma unroll
-              for (int i = 0; i < RT; ++i) {
-                if (decltype(at_edge)::value && key0 + half * C::HALF + key + kk >= vis[i]) continue;
-                const float y = kk == 0 ? a[i].x : kk == 1 ? a[i].y : kk == 2 ? a[i].z : a[i].w;
-                o[i][x][0] = fmaf(y, b.x, o[i][x][0]);
-                o[i][x][1] = fmaf(y, b.y, o[i][x][1]);
-                o[i][x][2] = fmaf(y, b.z, o[i][x][2]);
-                o[i][x][3] = fmaf(y, b.w, o[i][x][3]);
+            for (int n = 0; n < 8; ++n)
+              if (n == key / 8) {
+                x[0] = key & 1 ? s[n][1] : s[n][0];
+                x[1] = key & 1 ? s[n][3] : s[n][2];
               }
-            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) x[i] = __shfl_sync(0xffffffffu, x[i], (lane & ~3) | (key % 8 / 2));
+#pragma unroll
+            for (int q = 0; q < Q32; ++q)
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                  const float v = vs[key * C::V_PITCH + 32 * q + 8 * t + 4 * (c & 1) + i];
+                  if (!(fabsf(v) <= FLT_MAX) && key0 + key < vis[c / 2]) o[q][i][c] = fmaf(x[c / 2], v, o[q][i][c]);
+                }
+          }
+          __syncthreads();
+#pragma unroll
+          for (int i = 0; i < PER; ++i) {
+            float *at = vs + row_of(i) * C::V_PITCH + col_of(i);
+            for (int c = 0; c < 4; ++c)
+              if (!(fabsf(at[c]) <= FLT_MAX)) at[c] = 0.f;
+          }
+          __syncthreads();
         }
-      };
+      }
+      // Keys in an order in which a row's probabilities are where the contraction wants them: 2 t and 2 t + 1 of eight are its t and t + 4.
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        __syncwarp();                                              // (a warp's rows are its own)
+      for (int q = 0; q < Q32; ++q) {
+        float sum[4][4] = {}, fine[4][4] = {};
 #pragma unroll
-        for (int i = 0; i < RT; ++i)
+        for (int n = 0; n < 8; ++n) {
+          uint32_t ab[4], as[4], bb[2][4], bs[2][4];
+          split4<true, false>(make_float4(s[n][0], s[n][2], s[n][1], s[n][3]), ab, as);
 #pragma unroll
-          for (int j = 0; j < 2; ++j) ps[(ty * RT + i) * C::P_PITCH + tx + 16 * j] = s[i][half * 2 + j];
-        __syncwarp();
-        if (edge) pv(std::true_type{}, half);
-        else pv(std::false_type{}, half);
+          for (int e = 0; e < 2; ++e) split4<false, EXACT>(*(const float4 *)(vs + (8 * n + 2 * t + e) * C::V_PITCH + 32 * q + 4 * g), bb[e], bs[e]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) contract(fine[i], as[0], as[1], as[2], as[3], bb[0][i], bb[1][i]);
+          if (!EXACT)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) contract(fine[i], ab[0], ab[1], ab[2], ab[3], bs[0][i], bs[1][i]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) contract(sum[i], ab[0], ab[1], ab[2], ab[3], bb[0][i], bb[1][i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) o[q][i][c] = fmaf(o[q][i][c], grown[c / 2], sum[i][c] + fine[i][c]);
       }
       __syncthreads();                                             // the values have been read
-      ask(p.v, vs, D, w.unit + 1);
+      if (w.unit + 1 < last) ask(p.v, vs, C::V_PITCH);
       commit();
-      ask_ids(w.unit + 2);
     }
     // ---- its end
     const bool whole = part_begin == 0 && w.unit == w.units;
     const int slot = part_begin == 0 ? 1 : 0;
     float *mls = p.pieces + (int64_t)paged::CHUNK_CTAS * 2 * R * D;
 #pragma unroll
-    for (int i = 0; i < RT; ++i) {
-      const int r = ty * RT + i;
-#pragma unroll
-      for (int x = 8; x; x >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
+    for (int i = 0; i < 2; ++i) {
+      const int r = r0 + 8 * i;
+      l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
+      l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
       if (r >= rows) continue;
       const int at = w.rt * R + r, tok = p.group_of.quot(at);
       const int64_t to = (int64_t)(w.start + tok) * p.H + w.head * p.group + at - tok * p.group, piece = ((int64_t)blockIdx.x * 2 + slot) * R + r;
       const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
 #pragma unroll
-      for (int x = 0; x < OUT; ++x) {
-        const int col = (tx + 16 * x) * 4;
-        if (col >= D) continue;
-        if (whole) store4((T *)p.out + to * D + col, make_float4(o[i][x][0] * inv, o[i][x][1] * inv, o[i][x][2] * inv, o[i][x][3] * inv));
-        else __stcg((float4 *)(p.pieces + piece * D + col), make_float4(o[i][x][0], o[i][x][1], o[i][x][2], o[i][x][3]));
-      }
-      if (tx == 0) {
+      for (int q = 0; q < Q32; ++q)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int col = 32 * q + 8 * t + 4 * c, x = 2 * i + c;
+          if (whole) store4((T *)p.out + to * D + col, make_float4(o[q][0][x] * inv, o[q][1][x] * inv, o[q][2][x] * inv, o[q][3][x] * inv));
+          else __stcg((float4 *)(p.pieces + piece * D + col), make_float4(o[q][0][x], o[q][1][x], o[q][2][x], o[q][3][x]));
+        }
+      if (t == 0) {
         if (!whole) __stcg((float2 *)(mls + piece * 2), make_float2(m[i], l[i]));
         else if (p.lse) p.lse[to] = lse_of(m[i], l[i]);
       }
