@@ -44,18 +44,21 @@ def allowed_words(mask: torch.Tensor) -> torch.Tensor:
     return torch.where(words >= 1 << 31, words - (1 << 32), words).int()
 
 
-def _of_rows(t, name, dtype, rows, width, dev):
+def _of_rows(t, name, dtype, rows, width, index):
     """Distance between the rows of an argument [rows, width], 0 for one row for all [width]."""
-    if t.dtype is not dtype or t.device != dev or t.shape[-1] != width or not (t.dim() == 1 or t.dim() == 2 and t.shape[0] == rows) or (width > 1 and t.stride(-1) != 1):
-        raise ValueError(f"{name}: [rows, {width}] of {dtype} on {dev}, with dense rows, is needed (or one row for all, where that is allowed)")
+    shape = t.shape
+    if len(shape) == 1:
+        shape = (rows, *shape)
+    if t.dtype is not dtype or t.get_device() != index or shape != (rows, width) or (width > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{name}: [rows, {width}] of {dtype} on cuda:{index}, with dense rows, is needed (or one row for all, where that is allowed)")
     return t.stride(0) if t.dim() == 2 else 0
 
 
-def _of_row(t, name, dtype, rows, dev):
+def _of_row(t, name, dtype, rows, index):
     if t is None:
         return None
-    if t.dtype is not dtype or t.device != dev or t.dim() != 1 or t.shape[0] != rows or not t.is_contiguous():
-        raise ValueError(f"{name}: a contiguous tensor of {rows} elements of {dtype} on {dev} is needed")
+    if t.dtype is not dtype or t.get_device() != index or t.dim() != 1 or t.numel() != rows or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous tensor of {rows} elements of {dtype} on cuda:{index} is needed")
     return t.data_ptr()
 
 
@@ -66,34 +69,43 @@ def constrain_logits(logits: torch.Tensor, *, tokens: torch.Tensor | None = None
     [rows, width] int32 is divided (above 0) or multiplied by ``repetition`` and lowered by ``frequency`` * c + ``presence`` ([rows] f32 each); ``bias`` [vocab] or
     [rows, vocab] f32 is added; what ``allowed`` ([words] or [rows, words] int32, see ``allowed_words``) does not allow becomes -inf.  ``out`` may be logits.
     Enqueued on torch's current stream."""
-    if logits.dim() != 2 or logits.dtype not in _DTYPES or not logits.is_cuda or (logits.shape[1] > 1 and logits.stride(1) != 1):
-        raise ValueError("logits: a CUDA tensor [rows, vocab], f32 or bf16, with dense rows is needed (this library has no CPU path)")
+    dtype, index = _DTYPES.get(logits.dtype), logits.get_device()
+    if logits.dim() != 2 or dtype is None or index < 0:
+        raise ValueError("logits: a CUDA tensor [rows, vocab], f32 or bf16, is needed (this library has no CPU path)")
     rows, vocab = logits.shape
-    dev = logits.device
+    stride = out_stride = vocab
+    contiguous = logits.is_contiguous()
+    if not contiguous:
+        stride, step = logits.stride()
+        if vocab > 1 and step != 1:
+            raise ValueError("logits: dense rows are needed")
     if out is None:
-        out = torch.empty_like(logits) if logits.is_contiguous() else torch.empty((rows, vocab), dtype=logits.dtype, device=dev)
-    elif out.shape != logits.shape or out.dtype is not logits.dtype or out.device != dev or (vocab > 1 and out.stride(1) != 1):
-        raise ValueError("out has to be like logits")
-    bias_p = allowed_p = token_p = None
+        out = torch.empty_like(logits) if contiguous else torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
+    elif out is logits:
+        out_stride = stride
+    else:
+        if out.shape != logits.shape or out.dtype is not logits.dtype or out.get_device() != index or (vocab > 1 and out.stride(1) != 1):
+            raise ValueError("out has to be like logits")
+        out_stride = out.stride(0)
+    bias_p = allowed_p = token_p = lens_p = repetition_p = presence_p = frequency_p = None
     bias_stride = allowed_stride = token_stride = width = 0
     if bias is not None:
-        bias_stride, bias_p = _of_rows(bias, "bias", torch.float32, rows, vocab, dev), bias.data_ptr()
+        bias_stride, bias_p = _of_rows(bias, "bias", torch.float32, rows, vocab, index), bias.data_ptr()
     if allowed is not None:
-        allowed_stride, allowed_p = _of_rows(allowed, "allowed", torch.int32, rows, (vocab + 31) // 32, dev), allowed.data_ptr()
-    per_row = (None, None, None, None)
+        allowed_stride, allowed_p = _of_rows(allowed, "allowed", torch.int32, rows, (vocab + 31) // 32, index), allowed.data_ptr()
     if tokens is not None:
         if tokens.dim() != 2:
             raise ValueError("tokens: [rows, width] of torch.int32 is needed")
         width = tokens.shape[1]
-        token_stride = _of_rows(tokens, "tokens", torch.int32, rows, width, dev)
-        per_row = (_of_row(lens, "lens", torch.int32, rows, dev), _of_row(repetition, "repetition", torch.float32, rows, dev),
-                   _of_row(presence, "presence", torch.float32, rows, dev), _of_row(frequency, "frequency", torch.float32, rows, dev))
-        if width > 0:                                              # (else nothing has been said)
+        token_stride = _of_rows(tokens, "tokens", torch.int32, rows, width, index)
+        lens_p, repetition_p = _of_row(lens, "lens", torch.int32, rows, index), _of_row(repetition, "repetition", torch.float32, rows, index)
+        presence_p, frequency_p = _of_row(presence, "presence", torch.float32, rows, index), _of_row(frequency, "frequency", torch.float32, rows, index)
+        if width > 0:
             token_p = tokens.data_ptr()
-        else:
-            per_row = (None, None, None, None)
+        else:                                                      # nothing has been said
+            lens_p = repetition_p = presence_p = frequency_p = None
     elif lens is not None or repetition is not None or presence is not None or frequency is not None:
         raise ValueError("lens, repetition, presence and frequency come with tokens")
-    _check(lib().ouro_constrain_logits(logits.data_ptr(), _DTYPES[logits.dtype], logits.stride(0), rows, vocab, token_p, token_stride, width, *per_row, bias_p,
-                                       bias_stride, allowed_p, allowed_stride, out.data_ptr(), out.stride(0), current_stream(dev.index)))
+    _check(lib().ouro_constrain_logits(logits.data_ptr(), dtype, stride, rows, vocab, token_p, token_stride, width, lens_p, repetition_p, presence_p, frequency_p,
+                                       bias_p, bias_stride, allowed_p, allowed_stride, out.data_ptr(), out_stride, current_stream(index)))
     return out
