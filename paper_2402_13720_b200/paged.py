@@ -154,11 +154,11 @@ class PagedCache:
 
     def _new_rows(self, q, k, v):
         """Distances between the rows of new queries, and of new keys and values."""
-        if q.dim() != 3 or k.dim() != 3 or v.dim() != 3:
+        of_q, of_k, of_v = q.shape, k.shape, v.shape
+        if not len(of_q) == len(of_k) == len(of_v) == 3:
             raise ValueError("q, k and v: [rows, heads, head_dim] is needed")
         q_stride, k_stride = self._rows(q, "q"), self._rows(k, "k", self.n_kv_heads)
-        rows = len(q)
-        if self._rows(v, "v", self.n_kv_heads) != k_stride or len(k) != rows or len(v) != rows:
+        if self._rows(v, "v", self.n_kv_heads) != k_stride or not of_q[0] == of_k[0] == of_v[0]:
             raise ValueError("q, k and v need the same number of rows, k and v the same distance between them")
         return q_stride, k_stride
 
@@ -166,7 +166,7 @@ class PagedCache:
         """Rotates the queries q [rows, heads, head_dim] (returned; ``out`` may be q) and the keys k [rows, kv heads, head_dim], and writes keys
         and values to their slots; rows with a negative slot are padding."""
         q_stride, k_stride = self._new_rows(q, k, v)
-        rows, heads = q.shape[0], q.shape[1]
+        rows, heads, _ = q.shape
         out = self._out(out, q)
         if cos.dim() != 2 or cos.dtype is not torch.float32 or cos.shape != sin.shape or cos.shape[-1] * 2 != self.head_dim or not (cos.is_contiguous() and sin.is_contiguous()) \
                 or sin.dtype is not torch.float32 or cos.device != self.device or sin.device != self.device:
@@ -179,7 +179,7 @@ class PagedCache:
     def append_rotary(self, layer: int, q, k, v, slots, positions, rotary, out=None):
         """``append`` with the positions of a ``rotary.Rotary``: interleaved pairs, part of the head, stretched contexts; no tables."""
         q_stride, k_stride = self._new_rows(q, k, v)
-        rows, heads = q.shape[0], q.shape[1]
+        rows, heads, _ = q.shape
         out = self._out(out, q)
         if rotary.head_dim != self.head_dim or rotary.turns.get_device() != self._index:
             raise ValueError(f"rotary: positions for heads of {self.head_dim} on {self.device} are needed")
