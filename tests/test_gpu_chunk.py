@@ -221,6 +221,20 @@ def test_chunk_what_is_masked_may_be_anything(dtype, page):
 
 
 @gpu
+@pytest.mark.parametrize("D", [32, 64, 96, 128])
+def test_chunk_products_of_f32_lose_nothing(D):
+    """A product made of parts is good to 2^-20 and sums of a few in the contractions to 2^-21, of |q| |k| scale at most in a score; that is 3 x 2^-21 relative in a
+    probability, twice in the quotient: 2^-18 with what sums in 32 bits add.  Products with values, the exponentials and the other sums: 2^-17."""
+    c = Call([(300, 150), (700, 40), (64, 64)], 4, 2, D, 16, F32)
+    out, _ = c.run(want_lse=True)
+    want, _, lse = c.expected()
+    rows = ~torch.isnan(lse[:, 0])
+    size = float(c.q.norm(dim=-1).max() * c.k.norm(dim=-1).max()) / math.sqrt(D)
+    most = float(c.v.abs().max())
+    assert float((out[rows].double() - want[rows]).abs().max()) <= most * (2.0 ** -18 * size + 2.0 ** -17)
+
+
+@gpu
 @pytest.mark.parametrize("dtype,page", [(F32, 16), (BF16, 16), (BF16, 20)])
 def test_chunk_missing_pages_are_left_out(dtype, page):
     c = Call([(333, 50), (200, 200)], 4, 2, 64, page, dtype)
