@@ -51,9 +51,9 @@ struct ChunkRuns {
 
   // Whether items of so many keys are worth cuts, and with them a second launch.
   static bool may_cut(int keys) { return (keys + KEYS - 1) / KEYS >= (SNAP > 1 ? 2 * SNAP + 2 : 4); }
-  __device__ __forceinline__ explicit ChunkRuns(const ChunkParams &params) : p(params) {}
+  __host__ __device__ __forceinline__ explicit ChunkRuns(const ChunkParams &params) : p(params) {}
   // What is known of a sequence; no tokens outside the table.
-  __device__ __forceinline__ int enter(ChunkWalk &w) const {       // (its row of the table)
+  __host__ __device__ __forceinline__ int enter(ChunkWalk &w) const {       // (its row of the table)
     int sid = p.seqs ? p.seqs[w.s] : w.s;
     const bool known = sid >= 0 && sid < p.max_seqs;
     if (!known) sid = 0;
@@ -68,28 +68,31 @@ struct ChunkRuns {
   __device__ __forceinline__ void touch() const {
     asm volatile("" ::"l"(p.table), "l"(p.lens), "l"(p.seqs), "l"(p.starts), "l"(p.q), "r"(p.n), "r"(p.group), "r"(p.cap), "r"(p.unit_of.mul), "r"(p.shift), "r"(p.wait_limit));
   }
-  __device__ __forceinline__ bool wrong(const ChunkWalk &w) const { return w.start < 0 || w.m < 0 || w.start > p.rows - w.m; }
+  __host__ __device__ __forceinline__ bool wrong(const ChunkWalk &w) const { return w.start < 0 || w.m < 0 || w.start > p.rows - w.m; }
   // Keys that row r (of the sequence's m * group) sees; below 1: none.
-  __device__ __forceinline__ int sees(const ChunkWalk &w, int r) const { return w.len - w.m + 1 + p.group_of.quot(r); }
-  __device__ __forceinline__ int units_of(const ChunkWalk &w, int rt) const {
+  __host__ __device__ __forceinline__ int sees(const ChunkWalk &w, int r) const { return w.len - w.m + 1 + p.group_of.quot(r); }
+  __host__ __device__ __forceinline__ int units_of(const ChunkWalk &w, int rt) const {
     const int last = min(w.m * p.group - 1, rt * R + R - 1);
     return max(1, (sees(w, last) + KEYS - 1) / KEYS);
   }
-  // Cost of the first k tiles of a head.
-  __device__ __forceinline__ int upto(const ChunkWalk &w, int k) const {
+  // Cost of the first k tiles of a head.  It grows from the first tile on that sees a key: what a sequence has of new tokens beyond its length may be far more than a row
+  // of the table holds, and what it costs must not grow with their square.
+  __host__ __device__ __forceinline__ int upto(const ChunkWalk &w, int k) const {
     const uint32_t first = p.group * (max(w.len - w.m, 0) + ITEM_COST * KEYS) + R;
-    return (int)(((uint64_t)(uint32_t)k * first + (uint64_t)(uint32_t)k * (uint32_t)(k - 1) * (R / 2)) >> p.shift);
+    const uint32_t seeing = max(k - (int)((uint32_t)max(w.m - w.len, 0) * p.group / R), 0);
+    return (int)(((uint64_t)(uint32_t)k * first + (uint64_t)seeing * (seeing - 1) * (R / 2)) >> p.shift);
   }
   // What the host sets for a launch; tiles: of all sequences at most.
   static void set(ChunkParams &p, int grid, int64_t tiles) {
     p.unit_of.set(KEYS * p.group);
     p.grid_of.set(grid);
     p.snap = may_cut(p.cap) ? SNAP : INT32_MAX;
+    // (a tile sees cap keys at most: its first + seeing * R is group * (len + ITEM_COST * KEYS) + 2 R or less)
     const int64_t most = tiles * p.Hkv * ((int64_t)p.group * (p.cap + ITEM_COST * KEYS) + 2 * R);
     for (p.shift = 0; most >> p.shift >= (int64_t)1 << 30;) ++p.shift;
   }
   // The beginning of the next item that there is, or the end.
-  __device__ __forceinline__ void next_item(ChunkWalk &w) const {
+  __host__ __device__ __forceinline__ void next_item(ChunkWalk &w) const {
     w.unit = 0;
     if (++w.rt < w.tiles) {
       w.units = units_of(w, w.rt);
@@ -108,7 +111,7 @@ struct ChunkRuns {
       return;
     }
   }
-  __device__ __forceinline__ void next(ChunkWalk &w) const {
+  __host__ __device__ __forceinline__ void next(ChunkWalk &w) const {
     if (++w.unit >= w.units) next_item(w);
   }
   // All threads of the CTA: where its run begins and ends (places[2]), by a warp each.  cost, known: [n].  Lists that are wrong leave nothing to do, and the

@@ -22,7 +22,7 @@ struct Div {
     mul = x == 1 ? 0 : (uint32_t)((((uint64_t)1 << (31 + bits)) + x - 1) / x);
     shift = bits ? bits - 1 : 0;
   }
-  __device__ __forceinline__ int quot(int n) const { return mul ? (int)(__umulhi((uint32_t)n, mul) >> shift) : n; }
+  __host__ __device__ __forceinline__ int quot(int n) const { return mul ? (int)((uint32_t)(((uint64_t)(uint32_t)n * mul) >> 32) >> shift) : n; }
 };
 
 struct AttnParams {

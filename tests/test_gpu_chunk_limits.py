@@ -1,0 +1,24 @@
+"""Attention of chunks where a call's sizes are far from one another: many more new rows than a row of the table holds.  Tolerances as in test_gpu_chunk.py."""
+import pytest
+import torch
+
+from test_gpu_chunk import BF16, F32, Call
+
+gpu = pytest.mark.gpu
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("chunks,H,Hkv,page,max_pages", [([(16, 46500)], 64, 8, 16, 1), ([(100, 24000), (40, 3)], 64, 8, 8, 16), ([(9, 17000), (64, 64)], 64, 1, 16, 4),
+                                                         ([(0, 100000), (30, 70000), (64, 2)], 16, 8, 12, 6), ([(60, 166000)], 64, 8, 16, 4)])
+def test_chunk_more_new_rows_than_there_is_room_for(chunks, H, Hkv, page, max_pages, dtype):
+    """Rows that see no key give zeros, however many they are, and the others what they see."""
+    c = Call(chunks, H, Hkv, 32, page, dtype, max_pages=max_pages)
+    out = torch.full_like(c.q, 7.0)
+    out, lse = c.run(want_lse=True, out=out)
+    c.check(out, lse, c.expected())
+    for i, (n, m) in enumerate(chunks):
+        blind = max(m - n, 0)
+        at = slice(int(c.starts[i]), int(c.starts[i]) + blind)
+        assert bool((out[at] == 0).all()) and bool(torch.isneginf(lse[at]).all())
+    c.cache.check()
