@@ -526,7 +526,7 @@ extern "C" int ouro_paged_chunk_attention(const ouro_paged_cache *c, int32_t lay
   if (((int64_t)p.cap + 1024) * p.group > paged::MAX_TOKENS) return paged::refuse(CALL, "(max_pages * page_size + 1024) * n_heads / n_kv_heads is above 2^31 - 65536");
   // units of the finest kind at most: every tile may see all keys of the longest sequence
   const int64_t tiles = ((int64_t)rows * p.group + R - 1) / R + (n < rows ? n : rows), item = ((int64_t)p.cap + KEYS - 1) / KEYS + 8;
-  if (tiles > ((int64_t)1 << 40) / item / c->n_kv_heads) return paged::refuse(CALL, "the sequences' work may be above 2^40 units");
+  if (tiles > Share::MAX_ITEMS / c->n_kv_heads || tiles > ((int64_t)1 << 40) / item / c->n_kv_heads) return paged::refuse(CALL, "the sequences' work may be above 2^40 units or 2^30 tiles");
   const paged::Layout l = paged::layout(*c);
   p.k = (const uint8_t *)c->k + (int64_t)layer * c->layer_stride * esize;
   p.v = (const uint8_t *)c->v + (int64_t)layer * c->layer_stride * esize;

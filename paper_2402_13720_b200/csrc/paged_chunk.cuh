@@ -76,13 +76,15 @@ struct ChunkRuns {
     return max(1, (sees(w, last) + KEYS - 1) / KEYS);
   }
   // Cost of the first k tiles of a head.  It grows from the first tile on that sees a key: what a sequence has of new tokens beyond its length may be far more than a row
-  // of the table holds, and what it costs must not grow with their square.
+  // of the table holds, and what it costs must not grow with their square.  Whatever has a tile costs something, or the first run would begin behind it.
   __host__ __device__ __forceinline__ int upto(const ChunkWalk &w, int k) const {
     const uint32_t first = p.group * (max(w.len - w.m, 0) + ITEM_COST * KEYS) + R;
     const uint32_t seeing = max(k - (int)((uint32_t)max(w.m - w.len, 0) * p.group / R), 0);
-    return (int)(((uint64_t)(uint32_t)k * first + (uint64_t)seeing * (seeing - 1) * (R / 2)) >> p.shift);
+    return max((int)(((uint64_t)(uint32_t)k * first + (uint64_t)seeing * (seeing - 1) * (R / 2)) >> p.shift), min(k, 1));
   }
   // What the host sets for a launch; tiles: of all sequences at most.
+  // tiles * Hkv is at most MAX_ITEMS, so that the sum of costs, each up to 1 more than its part of `most`, stays below 2^31.
+  static constexpr int64_t MAX_ITEMS = (int64_t)1 << 30;
   static void set(ChunkParams &p, int grid, int64_t tiles) {
     p.unit_of.set(KEYS * p.group);
     p.grid_of.set(grid);

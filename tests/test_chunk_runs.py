@@ -95,3 +95,19 @@ def test_runs(lib, tc, chunks, Hkv, group, cap):
 @pytest.mark.parametrize("chunks,Hkv,group,cap", CROWDED)
 def test_runs_of_more_new_rows_than_there_is_room_for(lib, tc, chunks, Hkv, group, cap):
     play(lib, tc, chunks, Hkv, group, cap)
+
+
+# A table whose rows have room for a very long text, short sequences, and many rows.
+WIDE = [
+    ([(1, 1), (3, 2), (5000, 4000)], 8, 1, 1 << 30),
+    ([(1, 1)] * 1024, 32, 1, 1 << 30),
+    ([(2, 2), (0, 0), (7, 7), (1 << 20, 1 << 16), (1, 1)], 4, 2, 1 << 29),
+    ([(1, 1), (100, 60000), (5, 5)], 128, 1, 1 << 28),
+]
+
+
+@pytest.mark.parametrize("tc", [True, False])
+@pytest.mark.parametrize("chunks,Hkv,group,cap", WIDE)
+def test_runs_of_short_sequences_in_a_wide_table(lib, tc, chunks, Hkv, group, cap):
+    for grid in (1, 3, None):
+        play(lib, tc, chunks, Hkv, group, cap, grid)

@@ -1,4 +1,4 @@
-"""Attention of chunks where a call's sizes are far from one another: many more new rows than a row of the table holds.  Tolerances as in test_gpu_chunk.py."""
+"""Attention of chunks where a call's sizes are far from one another: many more new rows than a row of the table holds, short sequences in a table for very long ones.  Tolerances as in test_gpu_chunk.py."""
 import pytest
 import torch
 
@@ -21,4 +21,15 @@ def test_chunk_more_new_rows_than_there_is_room_for(chunks, H, Hkv, page, max_pa
         blind = max(m - n, 0)
         at = slice(int(c.starts[i]), int(c.starts[i]) + blind)
         assert bool((out[at] == 0).all()) and bool(torch.isneginf(lse[at]).all())
+    c.cache.check()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("chunks,H,Hkv,page,max_pages", [([(1, 1), (3, 2), (5000, 4000)], 8, 8, 1024, 1 << 20), ([(2, 2), (0, 0), (7, 7), (900, 800), (1, 1)], 8, 4, 512, 1 << 20),
+                                                         ([(1, 1)] * 200, 32, 32, 1024, 1 << 17), ([(5, 5), (30, 9)], 2, 2, 1 << 15, 1 << 15)])
+def test_chunk_short_sequences_in_a_wide_table(chunks, H, Hkv, page, max_pages, dtype):
+    c = Call(chunks, H, Hkv, 32, page, dtype, max_pages=max_pages)
+    out, lse = c.run(want_lse=True, out=torch.full_like(c.q, 7.0))
+    c.check(out, lse, c.expected())
     c.cache.check()
