@@ -167,15 +167,8 @@ struct ChunkRuns {
         w.m = seq.m;
         w.tiles = (w.m * p.group + R - 1) / R;
         const int each = upto(w, w.tiles);
-        w.head = min((int)((float)x / (float)each), p.Hkv - 1);    // (off by one at most)
+        w.head = (uint32_t)x / (uint32_t)each;
         x -= w.head * each;
-        if (x < 0) {
-          --w.head;
-          x += each;
-        } else if (x >= each) {
-          ++w.head;
-          x -= each;
-        }
         int n = w.tiles;
         while (n > 1) {                                            // 32 places at a time
           const int step = (n + 31) / 32, i = lane * step;

@@ -1,7 +1,8 @@
-"""Attention of chunks where a call's sizes are far from one another: many more new rows than a row of the table holds, short sequences in a table for very long ones.  Tolerances as in test_gpu_chunk.py."""
+"""Attention of chunks where a call's sizes are far from one another: many more new rows than a row of the table holds, short sequences in a table for very long ones, millions of heads.  Tolerances as in test_gpu_chunk.py."""
 import pytest
 import torch
 
+from paper_2402_13720_b200 import paged
 from test_gpu_chunk import BF16, F32, Call
 
 gpu = pytest.mark.gpu
@@ -33,3 +34,19 @@ def test_chunk_short_sequences_in_a_wide_table(chunks, H, Hkv, page, max_pages, 
     out, lse = c.run(want_lse=True, out=torch.full_like(c.q, 7.0))
     c.check(out, lse, c.expected())
     c.cache.check()
+
+
+@gpu
+@pytest.mark.parametrize("dtype,page", [(F32, 1), (BF16, 1), (BF16, 8)])
+def test_chunk_millions_of_heads(dtype, page):
+    """A text of one token gives its value, whichever of the heads; 2^24 and more are not all numbers of 32-bit floating point."""
+    heads = (1 << 24) + 12345
+    k, v = (torch.zeros((1, 1, page, heads, 32), dtype=dtype, device="cuda:0") for _ in range(2))
+    v[0, 0, 0].copy_(torch.arange(heads, device="cuda:0")[:, None] % 251 + 1)
+    cache = paged.PagedCache(max_seqs=1, max_pages=1, k=k, v=v)
+    cache.table.zero_()
+    cache.lens.fill_(1)
+    out = torch.zeros((1, heads, 32), dtype=dtype, device="cuda:0")
+    cache.attend_chunk(0, torch.ones_like(out), torch.tensor([0, 1], dtype=torch.int32, device="cuda:0"), out=out)
+    cache.check()
+    assert torch.equal(out[0], v[0, 0, 0])
