@@ -54,8 +54,9 @@ class BeamDecoder:
         y = x * torch.rsqrt((x * x).mean(-1, keepdim=True) + self.m.rms_eps)
         return (gain.float() * y).to(self.m.torch_dtype)
 
-    def _layers(self, tokens, slots, positions, attend):
-        """Rows of tokens through the model; attend(layer, q): attention of the rotated queries [rows, heads, head_dim].  Logits [rows, vocab]."""
+    def _layers(self, tokens, slots, positions, attend, first):
+        """Rows of tokens through the model; attend(layer, q): attention of the rotated queries [rows, heads, head_dim].  Logits of the rows from `first` on, None where
+        that is none of them."""
         m, c = self.m, self.cache
         heads, kv = m.n_heads, m.n_kv_heads
         x = self.w["embed"][tokens.long()].float()
@@ -70,16 +71,16 @@ class BeamDecoder:
             x = x + (attend(l, q).reshape(x.shape[0], -1) @ lw["wo"].T).float()
             g, u = (self._norm(x, lw["ffn_norm"]) @ self.gate_up[l].T).float().chunk(2, -1)
             x = x + ((torch.nn.functional.silu(g) * u).to(m.torch_dtype) @ lw["w_down"].T).float()
-        return self._norm(x, self.w["final_norm"]) @ self.w["lm_head"].T
+        return self._norm(x[first:], self.w["final_norm"]) @ self.w["lm_head"].T if first < x.shape[0] else None
 
-    def forward(self, tokens: torch.Tensor, seqs: torch.Tensor) -> torch.Tensor:
-        """tokens [n, t], t <= 16: the t newest of each of the sequences.  Extends the cache by them; logits [n * t, vocab]."""
+    def forward(self, tokens: torch.Tensor, seqs: torch.Tensor, first: int = 0) -> torch.Tensor | None:
+        """tokens [n, t], t <= 16: the t newest of each of the sequences.  Extends the cache by them; logits [n * t, vocab], those in front of row `first` left out."""
         n, t = tokens.shape
         slots, positions = self.cache.extend(seqs, torch.full((n,), t, dtype=torch.int32, device=self.device), t)
         shape = (n, t, self.m.n_heads, self.m.head_dim)
-        return self._layers(tokens.reshape(-1), slots.view(-1), positions.view(-1), lambda l, q: self.cache.attend(l, q.view(shape), seqs))
+        return self._layers(tokens.reshape(-1), slots.view(-1), positions.view(-1), lambda l, q: self.cache.attend(l, q.view(shape), seqs), first)
 
-    def forward_chunks(self, tokens: torch.Tensor, lens, seqs: torch.Tensor) -> torch.Tensor:
+    def forward_chunks(self, tokens: torch.Tensor, lens, seqs: torch.Tensor, first: int = 0) -> torch.Tensor | None:
         """The same with lens[i] >= 1 new tokens of sequence seqs[i], one sequence's after the other's in tokens [sum of lens]; logits [sum of lens, vocab]."""
         lens = np.asarray(lens, dtype=np.int32)
         ends = np.cumsum(lens, dtype=np.int32)
@@ -89,15 +90,23 @@ class BeamDecoder:
         if width * lens.size > int(ends[-1]):                       # rows of different lengths: the padding goes
             rows = torch.as_tensor(np.concatenate([i * width + np.arange(k) for i, k in enumerate(lens)]), device=self.device)
             slots, positions = slots.view(-1)[rows], positions.view(-1)[rows]
-        return self._layers(tokens, slots.view(-1), positions.view(-1), lambda l, q: self.cache.attend_chunk(l, q, starts, seqs))
+        return self._layers(tokens, slots.view(-1), positions.view(-1), lambda l, q: self.cache.attend_chunk(l, q, starts, seqs), first)
 
-    def _read(self, ids: torch.Tensor):
-        """Caches a text as sequence 0, a chunk at a time.  Logits of every chunk."""
+    def _read(self, ids: torch.Tensor, first: int):
+        """Caches a text as sequence 0, a chunk at a time.  Logits behind its tokens from the first-th on; None where it has none.  Of what lies in front of them
+        nothing is kept, and the output matrix is not asked (but for what shares its sixteen rows of a chunk with the first)."""
         out = []
         for a in range(0, ids.numel(), self.chunk):
             piece = ids[a: a + self.chunk]
-            out.append(self.forward(piece[None], self.all[:1]) if self.chunk <= OURO_MAX_NEW else self.forward_chunks(piece, [piece.numel()], self.all[:1]))
-        return out
+            skip = max(first - a, 0)
+            whole = skip // OURO_MAX_NEW * OURO_MAX_NEW if skip < piece.numel() else skip
+            if self.chunk <= OURO_MAX_NEW:
+                logits = self.forward(piece[None], self.all[:1], whole)
+            else:
+                logits = self.forward_chunks(piece, [piece.numel()], self.all[:1], whole)
+            if logits is not None:
+                out.append(logits[skip - whole:])
+        return torch.cat(out) if out else None
 
     def _text(self, prompt, more=(), new: int = 0):
         """A prompt, and what follows it (`more`, or `new` tokens to come), as int32 arrays of tokens that the model has: the embedding is indexed with them."""
@@ -127,7 +136,7 @@ class BeamDecoder:
         ruled = any(x is not None for x in rules.values())
         c.reset()
         ids = torch.as_tensor(prompt, device=self.device)
-        logits = self._read(ids)[-1][-1:]                           # the prompt, once
+        logits = self._read(ids, prompt.size - 1)                   # the prompt, once
         c.fork(torch.zeros_like(self.all), self.all)                # all beams begin there
         n_top = min(B, m.vocab)
         first = token_logprobs(self._constrain(logits, ids[None], rules) if ruled else logits, None, n_top)
@@ -154,8 +163,7 @@ class BeamDecoder:
         prompt, cont = self._text(prompt, continuation)
         self.cache.reset()
         ids = torch.as_tensor(np.concatenate([prompt, cont])[:-1], device=self.device)
-        logits = torch.cat(self._read(ids))
-        s = token_logprobs(logits[prompt.size - 1:], torch.as_tensor(cont, device=self.device))
+        s = token_logprobs(self._read(ids, prompt.size - 1), torch.as_tensor(cont, device=self.device))
         self.cache.check()
         return s.logprob, s.entropy
 
@@ -167,7 +175,7 @@ class BeamDecoder:
         texts = [self._text(prompt, c) for c in continuations]
         prompt, conts = texts[0][0], [c for _, c in texts]
         self.cache.reset()
-        self._read(torch.as_tensor(prompt[:-1], device=self.device))
+        self._read(torch.as_tensor(prompt[:-1], device=self.device), prompt.size)
         seqs = self.all[: len(conts)]
         self.cache.fork(torch.zeros_like(seqs), seqs)
         rows = np.concatenate([np.concatenate([prompt[-1:], c[:-1]]) for c in conts])
