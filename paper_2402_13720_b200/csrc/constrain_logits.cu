@@ -205,8 +205,8 @@ extern "C" int ouro_constrain_logits(const void *logits, int32_t dtype, int64_t 
     return paged::refuse(call, "lens and penalties come with tokens");
   }
   const int words = (vocab + 31) / 32;
-  if (bias && bias_stride != 0 && bias_stride < vocab) return paged::refuse(call, "bias_stride is neither 0 nor a row's length");
-  if (allowed && allowed_stride != 0 && allowed_stride < words) return paged::refuse(call, "allowed_stride is neither 0 nor a row's length");
+  if (bias && rows > 1 && bias_stride != 0 && bias_stride < vocab) return paged::refuse(call, "bias_stride is neither 0 nor a row's length");
+  if (allowed && rows > 1 && allowed_stride != 0 && allowed_stride < words) return paged::refuse(call, "allowed_stride is neither 0 nor a row's length");
   int dev = 0, sms = 0;
   if (!paged::device(&dev, &sms)) return paged::refuse(call, "no usable current device", OURO_ECUDA);
   ConstrainParams p{};
