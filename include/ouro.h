@@ -304,7 +304,8 @@ typedef struct {
   size_t workspace_bytes;
 } ouro_paged_cache;                                              /* all pointers are device memory */
 
-/* Bytes of workspace (0: the description is invalid).  Calls that share a workspace must not overlap on the GPU. */
+/* Bytes of workspace (0: the description is invalid): for the two attentions' pieces (head_dim 128: 42.6 MB, 64: 21.6, whichever calls are made), more where
+ * the page calls' lists are longer than those.  Calls that share a workspace must not overlap on the GPU. */
 size_t ouro_paged_workspace_bytes(const ouro_paged_cache *cache);
 /* No sequences, all pages free, status and workspace cleared.  To be called once before any other call on the cache and its workspace. */
 int ouro_paged_reset(const ouro_paged_cache *cache, void *cuda_stream);
@@ -351,10 +352,15 @@ int ouro_paged_attention(const ouro_paged_cache *cache, int32_t layer, const int
  * rows starts_dev[i] .. starts_dev[i+1]-1 (starts_dev [n+1], not descending, within 0 .. rows; none is allowed).  Of m new tokens the t-th sees the keys
  * 0 .. lens - m + t.  out [rows, n_heads, head_dim], lse_dev [rows, n_heads] (may be NULL): rows of no sequence are left as they are.  Tokens that see no
  * key, missing pages and sequences outside the table as above; starts that descend or leave 0 .. rows make the call do nothing (OURO_EINVAL in the cache's
- * status).  seqs_dev may name a sequence twice.  Two launches (one where no sequence can have 256 keys, bf16: 384); a page_size that is a multiple of 8 is faster in bf16.  Sums and maxima are held in 32 bits; f32
- * products are made of parts with 11 bits each, to 2^-21; an infinity among the queries, keys and values that a token sees gives infinities or NaN; in
- * bf16 a probability may go into the second product rounded to bf16, so that an output is off by up to 2^-8 of its probabilities' weighted |values| besides
- * its own rounding.  rows * n_heads / n_kv_heads and (max_pages * page_size + 1024) * n_heads / n_kv_heads are at most 2^31 - 65536, n_heads / n_kv_heads 65536. */
+ * status).  seqs_dev may name a sequence twice.
+ * bf16 with a page_size that is a multiple of 8 goes to the tensor cores' bf16 contractions; everything else takes another kernel, in bf16 three to fifteen times
+ * as long.  Two launches (one where max_pages * page_size is at most 192, or 320 for the former).  Sums and maxima are held in 32 bits.  In bf16 a probability may
+ * go into the second product rounded to bf16, so that an output is off by up to 2^-8 of its probabilities' weighted |values| besides its own rounding
+ * (ouro_paged_attention keeps two parts of it).  f32 products are made of parts with 11 bits each, to 2^-21; a query of 2^128 (1 - 2^-12) or more counts as
+ * infinite.  An infinity among the queries, keys and values that a token sees gives infinities or NaN, with one exception: in bf16 a score of -inf is that of a
+ * key that is not there, and a token that has no other score gives zeros (lse -inf).
+ * rows * n_heads / n_kv_heads and (max_pages * page_size + 1024) * n_heads / n_kv_heads are at most 2^31 - 65536, n_heads / n_kv_heads 65536; calls that
+ * may be more than 2^30 tiles of query rows or 2^40 units of 64 keys are refused. */
 int ouro_paged_chunk_attention(const ouro_paged_cache *cache, int32_t layer, const int32_t *seqs_dev, const int32_t *starts_dev, int32_t n, int32_t rows,
                                const void *q_dev, int64_t q_stride, int32_t n_heads, float scale, void *out_dev, float *lse_dev, void *cuda_stream);
 
@@ -373,8 +379,8 @@ int ouro_paged_append_rotary(const ouro_paged_cache *cache, int32_t layer, const
 
 /* Test aid: how often the attention kernels' bounded waits for their own copies and contractions poll, in calls made from now on in this process (default
  * 1 << 22; negative restores it).  0 makes a wait for what is not there yet give up at once: the kernels return normally with wrong outputs, ouro_paged_status returns
- * OURO_ETIMEOUT, and the next call with the default is right again.  (Caches in f32 and with a page_size that is no multiple of 16 wait without a limit of
- * their own: for copies that each thread has issued itself.) */
+ * OURO_ETIMEOUT, and the next call with the default is right again.  (Caches in f32, and those with a page_size that is no multiple of 16, or of 8 for
+ * ouro_paged_chunk_attention, wait without a limit of their own: for copies that each thread has issued itself.) */
 int ouro_paged_debug_set_wait_limit(int64_t polls);
 
 /* What a row of logits says about a token: logits [rows, vocab] (OURO_F32 or OURO_BF16), rows row_stride elements apart.
@@ -391,7 +397,8 @@ int ouro_token_logprobs(const void *logits_dev, int32_t dtype, int64_t row_strid
  *   vocabulary count for nothing):  y = y > 0 ? y / repetition[row] (a product with the rounded reciprocal) : y * repetition[row], then y -= frequency[row] * c + presence[row];
  *   y += bias[row, token] (rows bias_stride apart, 0: one row for all);
  *   y = -inf, whatever it was, where bit token % 32 of word token / 32 of the row's allowed_dev (rows allowed_stride apart, 0: one row for all) is 0.
- * repetition, presence, frequency [rows] f32; width is at most 2^23 - 1.  Every array but logits and out may be NULL (repetition 1, the others 0 or allowed); lens and penalties come with tokens. */
+ * repetition, presence, frequency [rows] f32; width is at most 2^23 - 1.  All penalties count the same tokens: where repetition is for the prompt too
+ * and the others for what was generated, it takes a call for each.  Every array but logits and out may be NULL (repetition 1, the others 0 or allowed); lens and penalties come with tokens. */
 int ouro_constrain_logits(const void *logits_dev, int32_t dtype, int64_t row_stride, int32_t rows, int32_t vocab, const int32_t *tokens_dev,
                           int64_t token_stride, int32_t width, const int32_t *lens_dev, const float *repetition_dev, const float *presence_dev,
                           const float *frequency_dev, const float *bias_dev, int64_t bias_stride, const uint32_t *allowed_dev, int64_t allowed_stride,

@@ -43,7 +43,8 @@ class PagedCache:
 
     def __init__(self, n_layers: int = 0, n_pages: int = 0, page_size: int = 0, n_kv_heads: int = 0, head_dim: int = 0, dtype: str | torch.dtype = "bf16", *,
                  max_seqs: int, max_pages: int, k: torch.Tensor | None = None, v: torch.Tensor | None = None, device="cuda:0"):
-        """The sizes, from which pages are allocated (zeros), or tensors ``k`` and ``v`` of the caller, whose strides are kept (the last is 1)."""
+        """The sizes, from which pages are allocated (zeros), or tensors ``k`` and ``v`` of the caller, whose strides are kept (the last is 1).  Besides the pages a
+        cache has a workspace for its calls: 43 MB with heads of 128, 22 with 64."""
         if (k is None) != (v is None):
             raise ValueError("k and v come together")
         if k is None:

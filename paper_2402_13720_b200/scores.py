@@ -67,7 +67,8 @@ def constrain_logits(logits: torch.Tensor, *, tokens: torch.Tensor | None = None
                      allowed: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
     """logits [rows, vocab], f32 or bf16, rows at any distance.  A token that is c > 0 times among the first lens [rows] (None: all) of the row's ``tokens``
     [rows, width] int32 is divided (above 0) or multiplied by ``repetition`` and lowered by ``frequency`` * c + ``presence`` ([rows] f32 each); ``bias`` [vocab] or
-    [rows, vocab] f32 is added; what ``allowed`` ([words] or [rows, words] int32, see ``allowed_words``) does not allow becomes -inf.  ``out`` may be logits.
+    [rows, vocab] f32 is added; what ``allowed`` ([words] or [rows, words] int32, see ``allowed_words``) does not allow becomes -inf.  All penalties count the same tokens
+    (to count others for ``repetition`` than for the rest, call twice).  ``out`` may be logits.
     Enqueued on torch's current stream."""
     dtype, index = _DTYPES.get(logits.dtype), logits.get_device()
     if logits.dim() != 2 or dtype is None or index < 0:
