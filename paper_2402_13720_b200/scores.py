@@ -39,7 +39,7 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None, n_t
 
 def allowed_words(mask: torch.Tensor) -> torch.Tensor:
     """A mask [.., vocab] of truth values (True: may come) as the words [.., ceil(vocab / 32)] int32 that ``constrain_logits`` takes."""
-    bits = torch.nn.functional.pad(mask, (0, -mask.shape[-1] % 32)).unflatten(-1, (-1, 32))
+    bits = torch.nn.functional.pad(mask.bool(), (0, -mask.shape[-1] % 32)).unflatten(-1, (-1, 32))
     words = (bits.long() << torch.arange(32, device=mask.device)).sum(-1)
     return torch.where(words >= 1 << 31, words - (1 << 32), words).int()
 
