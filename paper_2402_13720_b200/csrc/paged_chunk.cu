@@ -9,10 +9,12 @@
 // Products of f32 are three contractions (mma.sync, 8 deep, 11 bits an operand): x y = X Y + X y' + x' Y with the upper and the lower 11 bits of each, and x' y'
 // (2^-22 of the product at most, of either sign) left out.  The tensor cores round their sums towards 0, which counts in long chains (one for a score,
 // one for an output: 2.5e-6 of the norm off, 44 us for 46 below): the small products and every 32 dims, or 64 keys, of the large ones have sums of their own, which are added up in
-// 32 bits.  Outputs are as near to 64 bits as those of 32-bit multiply-adds (5.7e-7 of their norm for 7.9e-7).  4096 tokens, four heads of 128: 372 us, 46
+// 32 bits.  How far outputs are from 64 bits, of their norm, and those of 32-bit multiply-adds: heads of 32 6.7e-7 for 5.3e-7, 64 6.8e-7 for 6.4e-7, 96 6.0e-7 for 7.8e-7, 128
+// 6.4e-7 for 9.1e-7 (sequences of 700 and 1500: what is left out of products is the same for all heads, what sums lose grows with them).  4096 tokens, four heads of 128: 372 us, 46
 // TFLOP/s; multiply-adds by four rows and four keys a thread 503, bound by what came from shared memory; the contractions alone would take 180.  Two CTAs an SM
 // are eight warps, too few to hide one another's chains of loads, parts and contractions.  A call of few units is best dealt out one by one (five prompts of the
-// `small` shape, up to 411 tokens: 46 us).
+// `small` shape, up to 411 tokens: 46 us).  bf16 in pages that are no multiple of 8 tokens passes here as f32 does, but for parts that 8 bits have not: 7B shape, 2048 tokens 531 us (62 on
+// the tcgen05 kernel in pages of 16), 70B shape, one prompt of 4096 3.8 ms (0.30), 1.1B shape, mixed batch 82 (26): 45 to 72 TFLOP/s.
 #include <cfloat>
 
 #include "paged_chunk.cuh"

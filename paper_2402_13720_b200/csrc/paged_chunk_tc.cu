@@ -9,7 +9,7 @@
 //                  waits for it; V is the MN-major operand and is never transposed.
 // TMEM is full with that: two S of 64 columns, four P of 32, two O of 128.
 // P is rounded to bf16 once.  It could go in as two bf16 parts, as it does in paged_attention_tc.cu, which is bound by memory; here that would be half as
-// many contractions again.  The rounding errors of P are independent and average out as the values do: outputs are 2.9e-3 of their norm off, of which their own
+// many contractions again.  The rounding errors of P are independent and average out as the values do: outputs are 2.2e-3 of their norm off, of which their own
 // rounding is 1.7e-3.
 // Warps 0-3 and 4-7 are the rows of A and B, who also bring their queries; warps 8 and 9 issue the contractions of A and of B; warp 10 fetches keys and values (TMA
 // straight from the pages, boxes of 8 to 64 rows of a page); warp 11 sees to the values at a sequence's end and at the causal edge before they are contracted.
@@ -27,8 +27,8 @@ constexpr int TILE = 128, R = 2 * TILE;            // query rows of a tile, of a
 constexpr int KEYS = 64;                           // of a unit
 constexpr int ROW_WARPS = 8, MMA_WARP = ROW_WARPS, FETCH_WARP = MMA_WARP + 2, VALUE_WARP = FETCH_WARP + 1,
               THREADS = 32 * (VALUE_WARP + 1);
-// us with an item's cost of 2, 4, 5, 6, 8 units: 1.1B shape, mixed batch 27.7, 30.0, 28.1, 29.4, 29.3; 7B shape, 2048 tokens 67.4, 59.5, 59.5, 71.0, 67.9; 70B shape, five
-// prompts 914, 780, 780, 903, 918 (5 and 4 on a later kernel than the others, which had 887 with 4).
+// us with an item's cost of 2, 4, 5, 6, 8 units: 1.1B shape, mixed batch 27.4, 29.1, 27.3, 27.4, 28.9; 7B shape, 2048 tokens 58.0, 55.8, 56.2, 56.8, 58.0; 34B shape, 61 behind
+// 24000 56.4, 55.2, 55.6, 55.7, 55.9; 70B shape, five prompts, with pauses between them 815, 776, 778, 782, 795.
 constexpr int ITEM_COST = 5, SNAP = 2, MIN_RUN = 4;
 typedef paged::ChunkRuns<R, KEYS, ITEM_COST, SNAP, MIN_RUN> Share;
 constexpr float GROWTH = 8.f;                      // (log2) a maximum may grow by this before sums and outputs are rescaled
